@@ -362,7 +362,7 @@ def run(state):
     y, total, rstd = qb.qblora_rms_norm_fwd(st["x"], st["w"], EPS, residual=st["res"], keep=kind == "norm_train")
     out = {"y": y, "sum": total} if st["res"] is not None else {"y": y}
     if kind == "norm_train":
-        out["dx"], out["dw"] = qb.qblora_rms_norm_bwd(total, st["w"], rstd, st["dy"], dsum=st["dsum"])
+        out["dx"], out["dw"] = qb.qblora_rms_norm_bwd(total, st["w"], rstd, st["dy"], dtotal=st["dsum"])
     return out
 
 
