@@ -397,6 +397,147 @@ int qblora_linear_decode(const qblora_qweight* qw, const void* pack, const qblor
 size_t qblora_decode_pack_bytes(const qblora_qweight* qw);
 int qblora_decode_pack(const qblora_qweight* qw, void* pack, void* stream);
 
+/* ---- between the projections of a decoder layer ------------------------------------------------------------------------
+ *
+ * What a layer computes between its quantized projections: the norm in front of them, rotary positions, the paged cache of
+ * keys and values, and attention over it.  The conventions of the top hold; activations, norm weights and the cache are
+ * bf16, statistics and sums fp32.  These calls take device addresses of bf16 and 32-bit arrays at any multiple of their
+ * element size, unless stated otherwise.  Whatever the device-side integers (lengths, slots, page numbers, table entries)
+ * hold, no call reads or writes outside the buffers described by its arguments.
+ */
+
+/*
+ * The paged cache of one layer.  A page holds `page` consecutive positions of one request: 16, 32, 64, 128 or 256.
+ *   k   [pages, heads, head_dim / 8, page, 8]:  eight features of a position lie together
+ *   v   [pages, heads, page / 8, head_dim, 8]:  eight positions of a feature lie together
+ * which are the 16-byte operands of the attention's matrix instructions, so that it reads the cache in whole lines without a
+ * transpose.  Both 16-byte aligned.  head_dim: 64, 128 or 256.  A slot is page_number * page + place in the page.
+ */
+typedef struct qblora_kv_cache {
+    int32_t pages;
+    int32_t page;
+    int32_t heads;        /* key / value heads */
+    int32_t head_dim;
+    qblora_bf16* k;
+    qblora_bf16* v;
+} qblora_kv_cache;
+
+/*
+ * Block tables, slots and positions of one step, from the lengths of its requests: request i has context[i] positions in
+ * the cache and fresh[i] new tokens behind them (values below 0 count as 0).
+ *   pages     request i holds ceil(context[i] / page) pages, listed in its row of `table` (int32 [n, width]); it gets
+ *             further ones, up to min(ceil((context[i] + fresh[i]) / page), width) in all, from free_pages (int32 [n_free]),
+ *             taken in order, request by request.  They are written into the row; where free_pages is used up -1 is.
+ *             Other entries stay.
+ *   taken     int32 [1]: pages wanted in all.  More than n_free means that the last of them were not to be had.
+ *   starts    int32 [n + 1]: index of each request's first new token; starts[n] tokens in all, at most `tokens`.
+ *   positions int32 [tokens]: position of each new token in its request; 0 behind the last.
+ *   slots     int64 [tokens]: where its key and value go; -1 where there is no page, and behind the last token.
+ * `context` and the free list are not changed: a step that is accepted adds fresh to context and drops the first `taken`
+ * free pages.  page as for the cache; tokens <= 2^31 - 1.  n = 0 and tokens = 0 are fine.
+ */
+int qblora_page_tables(const int32_t* context, const int32_t* fresh, int32_t n, int32_t page, const int32_t* free_pages,
+                       int32_t n_free, int32_t* table, int32_t width, int64_t tokens, int32_t* starts, int32_t* positions,
+                       int64_t* slots, int32_t* taken, void* stream);
+
+/*
+ * Rotary positions.  The first `rot` features of a head (even, at most head_dim) are rot / 2 pairs, features (j, j + rot/2)
+ * or, interleaved, (2j, 2j + 1); pair j of a token at position p is turned by the angle p * freq[j] and multiplied by
+ * `scale`; the other features are copied.
+ *   freq     fp32 [rot / 2], device; 4-byte aligned
+ *   q, k     bf16: token t, head h at q + t*ldq + h*head_dim (k likewise); k may be NULL (then k_out is ignored).  The
+ *            outputs may be the inputs themselves (same strides), but must not overlap them otherwise.
+ * The angle is formed in 64 bits and reduced to one turn before sine and cosine: at position 10^6 an fp32 angle is off by
+ * 0.03 of a radian.  _bwd is the transposed operator, a turn the other way round: gradients in, gradients out.
+ * T = 0 is a no-op.
+ */
+typedef struct qblora_rope {
+    int32_t rot;
+    int32_t interleaved;
+    float scale;
+    const float* freq;
+} qblora_rope;
+int qblora_rope_fwd(const qblora_rope* rope, const qblora_bf16* q, int64_t ldq, int32_t heads, const qblora_bf16* k,
+                    int64_t ldk, int32_t kv_heads, int32_t head_dim, const int32_t* positions, int64_t T,
+                    qblora_bf16* q_out, int64_t ldq_out, qblora_bf16* k_out, int64_t ldk_out, void* stream);
+int qblora_rope_bwd(const qblora_rope* rope, const qblora_bf16* dq, int64_t lddq, int32_t heads, const qblora_bf16* dk,
+                    int64_t lddk, int32_t kv_heads, int32_t head_dim, const int32_t* positions, int64_t T,
+                    qblora_bf16* dq_out, int64_t lddq_out, qblora_bf16* dk_out, int64_t lddk_out, void* stream);
+
+/*
+ * The serving form: q is turned into q_out, k is turned and written with v to slots[t] of the cache.  A slot outside the
+ * cache writes nothing; two tokens of one call must not share a slot.
+ */
+int qblora_rope_cache(const qblora_rope* rope, const qblora_bf16* q, int64_t ldq, int32_t heads, const qblora_bf16* k,
+                      int64_t ldk, const qblora_bf16* v, int64_t ldv, const int32_t* positions, const int64_t* slots,
+                      int64_t T, qblora_bf16* q_out, int64_t ldq_out, const qblora_kv_cache* cache, void* stream);
+
+/*
+ * Frequencies of the pairs for a rotated width, on the host: f_j = base^(-2j / rot), and for contexts `factor` times as
+ * long as the `original` one
+ *   QBLORA_ROPE_LINEAR    f_j / factor: positions are squeezed
+ *   QBLORA_ROPE_BASE      base * factor^(rot / (rot - 2)) in the place of base: the slowest pair is slowed by the factor,
+ *                         the fastest keeps its frequency
+ *   QBLORA_ROPE_BY_PARTS  with t_j = original * f_j / (2 pi) turns within the original context and
+ *                         g = clamp((t_j - low) / (high - low), 0, 1):  f_j * (g + (1 - g) / factor)
+ * freq: host, fp32 [rot / 2], computed in 64 bits.  *scale (may be NULL): 0.1 * ln(factor) + 1 by parts, else 1; q and k
+ * are both multiplied by it.  `original`, low and high are read by parts only (low < high).
+ */
+enum { QBLORA_ROPE_PLAIN = 0, QBLORA_ROPE_LINEAR = 1, QBLORA_ROPE_BASE = 2, QBLORA_ROPE_BY_PARTS = 3 };
+int qblora_rope_frequencies(int32_t rot, double base, int32_t kind, double factor, double original, double low, double high,
+                            float* freq, float* scale);
+
+/*
+ * Attention of the new tokens over the paged cache.  Request i has context[i] positions in front of its new tokens
+ * starts[i] .. starts[i+1] - 1 (int32 [n + 1], as qblora_page_tables writes them); its positions are in the pages that row i
+ * of `table` (int32 [n, width]) lists, those of the new tokens among them.  For new token t at position
+ * p = context[i] + t - starts[i], query head h and the key / value head h / (heads / cache->heads):
+ *   out[t, h] = sum_j e_j v_j / sum_j e_j,  e_j = exp(scale * q[t, h] . k_j),  over the positions j it sees:
+ *   0 <= j <= p, j > p - window (window = 0: no limit), and j in a page that the table lists (entries outside 0 .. pages-1
+ *   and columns past `width` list none).
+ * A token that sees nothing gets zeros (and lse = -inf).  What unseen positions hold does not matter, NaN and infinities
+ * included.  Sums and statistics in fp32; the weights e_j, at most 1 there, are rounded to bf16 for the second product
+ * (the sum in the denominator is of the unrounded ones).
+ *   q    bf16: token t, head h at q + t*ldq + h*head_dim; 16-byte aligned, ldq % 8 == 0
+ *   out  bf16, likewise; rows of tokens that belong to no request are not written
+ *   lse  fp32 [T, heads] or NULL: log sum_j e_j
+ *   max_new  the most new tokens of any request, as far as the caller knows: it chooses the kernel, and a wrong value costs
+ *        time, not correctness
+ *   workspace  at least qblora_paged_attention_workspace_bytes(), 16-byte aligned: partial results of long contexts
+ * heads % cache->heads == 0.  T = 0 and n = 0 are no-ops.
+ */
+size_t qblora_paged_attention_workspace_bytes(const qblora_kv_cache* cache, int32_t heads, int32_t max_new);
+int qblora_paged_attention(const qblora_bf16* q, int64_t ldq, int32_t heads, const qblora_kv_cache* cache,
+                           const int32_t* table, int32_t width, const int32_t* starts, const int32_t* context, int32_t n,
+                           int64_t T, float scale, int32_t window, int32_t max_new, qblora_bf16* out, int64_t ldo, float* lse,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Addition of the residual and root-mean-square norm over rows of d features:
+ *   total = bf16(x + residual);  r = 1 / sqrt(mean(total^2) + eps);  y = bf16(total * r * w).
+ * The norm is of the sum as it is kept, so that the backward pass, which has nothing else, differentiates what was computed.
+ *   x, residual  bf16 [T, d]; residual may be NULL (total = x, and the argument `total` is ignored)
+ *   w            bf16 [d]; d <= 16384
+ *   total, y     bf16 [T, d]; total may be x or residual, y may be x
+ *   rstd         fp32 [T] or NULL: r, for the backward pass
+ */
+int qblora_rms_norm_fwd(const qblora_bf16* x, const qblora_bf16* residual, const qblora_bf16* w, int64_t T, int32_t d,
+                        float eps, qblora_bf16* total, qblora_bf16* y, float* rstd, void* stream);
+
+/*
+ * Its backward pass: with h = total * rstd and g = dy * w,
+ *   dx = rstd * (g - h * mean(g * h)) + dtotal   (the gradient of x and of residual alike),   dw = sum_t dy * h.
+ *   dtotal  bf16 [T, d] or NULL: the gradient that reaches the sum by its other use
+ *   dx      bf16 [T, d]; may be dy or dtotal
+ *   dw      fp32 [d] or NULL; overwritten.  Needs `workspace` of qblora_rms_norm_bwd_workspace_bytes(), 16-byte aligned; its
+ *           sums are taken in a fixed order, a repeated call repeats its bits.
+ * T = 0: dw = 0.
+ */
+size_t qblora_rms_norm_bwd_workspace_bytes(int64_t T, int32_t d);
+int qblora_rms_norm_bwd(const qblora_bf16* total, const qblora_bf16* w, const float* rstd, const qblora_bf16* dy,
+                        const qblora_bf16* dtotal, int64_t T, int32_t d, qblora_bf16* dx, float* dw, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
 /*
  * Measurement hook.  Registers a pair of caller-created hipEvent_t (passed as void*) that the next
  * calls record on their stream immediately before and after ONE part of the work, so that a

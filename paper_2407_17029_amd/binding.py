@@ -22,6 +22,7 @@ QUANT_ABSMAX_CODEBOOK, QUANT_MINMAX_INT4 = 0, 1
 SCALES_FP32, SCALES_E4M3_GROUPED = 0, 1
 MERGE_BETA_SHIFT, MERGE_REQUANT_MINMAX = 0, 1
 OP_AVGPOOL_REPEAT, OP_TRUNCATE_PAD0, OP_SAMPLE_ZEROFILL = 0, 1, 2
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = 0, 1, 2, 3
 
 EXPORTS = ["qblora_quantize_blockwise", "qblora_dequantize_bf16", "qblora_linear_fwd_workspace_bytes",
            "qblora_linear_bwd_workspace_bytes", "qblora_linear_fwd", "qblora_linear_bwd",
@@ -33,7 +34,10 @@ EXPORTS = ["qblora_quantize_blockwise", "qblora_dequantize_bf16", "qblora_linear
            "qablora_linear_bwd", "qblora_merge_bf16",
            "qblora_linear_decode_workspace_bytes", "qblora_linear_decode_tokens_workspace_bytes", "qblora_linear_decode",
            "qblora_decode_pack_bytes", "qblora_decode_pack",
-           "qblora_noalloc_scratch_bytes", "qblora_linear_fwd_noalloc", "qblora_dense_min_tokens"]
+           "qblora_noalloc_scratch_bytes", "qblora_linear_fwd_noalloc", "qblora_dense_min_tokens",
+           "qblora_page_tables", "qblora_rope_fwd", "qblora_rope_bwd", "qblora_rope_cache", "qblora_rope_frequencies",
+           "qblora_paged_attention_workspace_bytes", "qblora_paged_attention", "qblora_rms_norm_fwd",
+           "qblora_rms_norm_bwd_workspace_bytes", "qblora_rms_norm_bwd"]
 
 PROFILE_FWD_GEMM, PROFILE_BWD_GEMM, PROFILE_MERGE, PROFILE_QUANTIZE = 0, 1, 2, 3
 PROFILE_ADAPTER_FWD, PROFILE_ADAPTER_BWD, PROFILE_ADAPTER_GRADS, PROFILE_GRAD_REDUCE = 4, 5, 6, 7
@@ -53,11 +57,22 @@ class CAdapter(C.Structure):
                 ("A", C.c_void_p), ("B", C.c_void_p), ("scale_op", C.c_int32)]
 
 
+class CKVCache(C.Structure):
+    _fields_ = [("pages", C.c_int32), ("page", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p)]
+
+
+class CRope(C.Structure):
+    _fields_ = [("rot", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_float), ("freq", C.c_void_p)]
+
+
 # The same layouts for struct.pack: one call instead of a descriptor access per field (a description of a weight took 9 us
 # of the 10 that a small inference call spent in Python, now 2).
 _QWEIGHT, _ADAPTER = struct.Struct("=5i64s4x7Qi4x"), struct.Struct("=3if2Qi4x")
 _FLOAT32 = np.dtype(np.float32)
 assert _QWEIGHT.size == C.sizeof(CQWeight) and _ADAPTER.size == C.sizeof(CAdapter)
+_KV_CACHE, _ROPE = struct.Struct("=4i2Q"), struct.Struct("=2if4xQ")
+assert _KV_CACHE.size == C.sizeof(CKVCache) and _ROPE.size == C.sizeof(CRope)
 
 
 class QBLoRAError(RuntimeError):
@@ -126,6 +141,20 @@ def lib():
                                               C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.qblora_dense_min_tokens.restype = C.c_int64
         L.qblora_dense_min_tokens.argtypes = []
+        p, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
+        L.qblora_page_tables.argtypes = [p, p, i32, i32, p, i32, p, i32, i64, p, p, p, p, p]
+        for name in ("qblora_rope_fwd", "qblora_rope_bwd"):
+            getattr(L, name).argtypes = [p, p, i64, i32, p, i64, i32, i32, p, i64, p, i64, p, i64, p]
+        L.qblora_rope_cache.argtypes = [p, p, i64, i32, p, i64, p, i64, p, p, i64, p, i64, p, p]
+        L.qblora_rope_frequencies.argtypes = [i32, C.c_double, i32, C.c_double, C.c_double, C.c_double, C.c_double, p, p]
+        L.qblora_paged_attention_workspace_bytes.restype = C.c_size_t
+        L.qblora_paged_attention_workspace_bytes.argtypes = [p, i32, i32]
+        L.qblora_paged_attention.argtypes = [p, i64, i32, p, p, i32, p, p, i32, i64, C.c_float, i32, i32, p, i64, p, p,
+                                             C.c_size_t, p]
+        L.qblora_rms_norm_fwd.argtypes = [p, p, p, i64, i32, C.c_float, p, p, p, p]
+        L.qblora_rms_norm_bwd_workspace_bytes.restype = C.c_size_t
+        L.qblora_rms_norm_bwd_workspace_bytes.argtypes = [i64, i32]
+        L.qblora_rms_norm_bwd.argtypes = [p, p, p, p, p, i64, i32, p, p, p, C.c_size_t, p]
         L.qblora_noalloc_scratch_bytes.restype = C.c_size_t
         L.qblora_noalloc_scratch_bytes.argtypes = []
         L.qblora_linear_fwd_noalloc.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
@@ -557,3 +586,200 @@ def qblora_linear_decode(qw: QWeight, X: torch.Tensor, Y: torch.Tensor = None, w
     rc = lib().qblora_linear_decode(q, _ptr(pack), _ptr(X), T, _ptr(Y), _ptr(ws), ws.numel(), _stream())
     _check(rc, "qblora_linear_decode")
     return Y
+
+
+# ---- between the projections of a decoder layer ---------------------------------------------------------
+
+
+def _device_array(t, dtype, shape=None) -> bool:
+    return t.is_cuda and t.dtype == dtype and t.is_contiguous() and (shape is None or t.shape == shape)
+
+
+def _heads(t) -> bool:
+    """bf16 [tokens, heads, head_dim] on the device: any stride between tokens, heads one behind the other."""
+    return (t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3
+            and (t.numel() == 0 or (t.stride(2) == 1 or t.shape[2] == 1) and (t.stride(1) == t.shape[2] or t.shape[1] == 1)))
+
+
+def _token_stride(t) -> int:
+    """Elements from one token to the next (a single token has none: any stride that is long enough does)."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), -(-t.shape[1] * t.shape[2] // 8) * 8)
+
+
+def _cache(k_cache, v_cache) -> bytes:
+    """The description of a paged cache: keys [pages, heads, head_dim / 8, page, 8], values [pages, heads, page / 8,
+    head_dim, 8]."""
+    pages, heads, octets, page, eight = k_cache.shape
+    assert eight == 8 and _device_array(k_cache, torch.bfloat16)
+    assert _device_array(v_cache, torch.bfloat16, (pages, heads, page // 8, octets * 8, 8))
+    return _KV_CACHE.pack(pages, page, heads, octets * 8, k_cache.data_ptr(), v_cache.data_ptr())
+
+
+def qblora_page_tables(context: torch.Tensor, fresh: torch.Tensor, page: int, free_pages: torch.Tensor, table: torch.Tensor,
+                       tokens: int, starts: torch.Tensor = None, positions: torch.Tensor = None,
+                       slots: torch.Tensor = None, taken: torch.Tensor = None):
+    """Adds a step's pages to the block table (in place) and returns (starts, positions, slots, taken) of its new tokens;
+    `tokens`: the room for them."""
+    n, width = table.shape
+    dev = table.device
+    assert all(_device_array(t, torch.int32) for t in (context, fresh, free_pages, table))
+    assert context.shape == (n,) and fresh.shape == (n,)
+    if starts is None:
+        starts = torch.empty(n + 1, dtype=torch.int32, device=dev)
+    if positions is None:
+        positions = torch.empty(tokens, dtype=torch.int32, device=dev)
+    if slots is None:
+        slots = torch.empty(tokens, dtype=torch.int64, device=dev)
+    if taken is None:
+        taken = torch.empty(1, dtype=torch.int32, device=dev)
+    assert _device_array(starts, torch.int32, (n + 1,)) and _device_array(positions, torch.int32, (tokens,))
+    assert _device_array(slots, torch.int64, (tokens,)) and _device_array(taken, torch.int32, (1,))
+    rc = lib().qblora_page_tables(_ptr(context), _ptr(fresh), n, page, _ptr(free_pages), free_pages.numel(), _ptr(table),
+                                  width, tokens, _ptr(starts), _ptr(positions), _ptr(slots), _ptr(taken), _stream())
+    _check(rc, "qblora_page_tables")
+    return starts, positions, slots, taken
+
+
+def qblora_rope_frequencies(rot: int, base: float = 10000.0, kind: int = ROPE_PLAIN, factor: float = 1.0,
+                            original: float = 4096.0, low: float = 1.0, high: float = 32.0, device="cuda"):
+    """(frequencies fp32 [rot / 2] on `device`, factor on q and k) for the scaling `kind` (ROPE_*)."""
+    freq = np.empty(max(rot // 2, 0), np.float32)
+    scale = C.c_float()
+    rc = lib().qblora_rope_frequencies(rot, base, kind, factor, original, low, high, freq.ctypes.data_as(C.c_void_p),
+                                       C.byref(scale))
+    _check(rc, "qblora_rope_frequencies")
+    return torch.from_numpy(freq).to(device), scale.value
+
+
+def _rope(freq, interleaved, scale) -> bytes:
+    assert _device_array(freq, torch.float32) and freq.dim() == 1
+    return _ROPE.pack(2 * freq.numel(), int(interleaved), scale, freq.data_ptr())
+
+
+def _rope_call(name, q, k, positions, freq, interleaved, scale, q_out, k_out):
+    T, heads, dim = q.shape
+    assert _heads(q) and _device_array(positions, torch.int32, (T,))
+    if q_out is None:
+        q_out = torch.empty((T, heads, dim), dtype=torch.bfloat16, device=q.device)
+    assert _heads(q_out) and q_out.shape == q.shape
+    ldk = ldk_out = kv_heads = 0
+    if k is not None:
+        kv_heads = k.shape[1]
+        assert _heads(k) and k.shape == (T, kv_heads, dim)
+        if k_out is None:
+            k_out = torch.empty((T, kv_heads, dim), dtype=torch.bfloat16, device=q.device)
+        assert _heads(k_out) and k_out.shape == k.shape
+        ldk, ldk_out = _token_stride(k), _token_stride(k_out)
+    rc = getattr(lib(), name)(_rope(freq, interleaved, scale), _ptr(q), _token_stride(q), heads, _ptr(k), ldk, kv_heads, dim,
+                              _ptr(positions), T, _ptr(q_out), _token_stride(q_out), _ptr(k_out), ldk_out, _stream())
+    _check(rc, name)
+    return q_out, k_out
+
+
+def qblora_rope_fwd(q: torch.Tensor, k, positions: torch.Tensor, freq: torch.Tensor, interleaved: bool = False,
+                    scale: float = 1.0, q_out: torch.Tensor = None, k_out: torch.Tensor = None):
+    """Rotary positions on q [T, heads, head_dim] and k [T, kv_heads, head_dim] (or None)."""
+    return _rope_call("qblora_rope_fwd", q, k, positions, freq, interleaved, scale, q_out, k_out)
+
+
+def qblora_rope_bwd(dq: torch.Tensor, dk, positions: torch.Tensor, freq: torch.Tensor, interleaved: bool = False,
+                    scale: float = 1.0, dq_out: torch.Tensor = None, dk_out: torch.Tensor = None):
+    """The gradients of q and k from those of the rotated ones."""
+    return _rope_call("qblora_rope_bwd", dq, dk, positions, freq, interleaved, scale, dq_out, dk_out)
+
+
+def qblora_rope_cache(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor,
+                      freq: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, interleaved: bool = False,
+                      scale: float = 1.0, q_out: torch.Tensor = None):
+    """The rotated q; the rotated k and v go to their slots of the paged cache."""
+    T, heads, dim = q.shape
+    cache = _cache(k_cache, v_cache)
+    assert _heads(q) and _heads(k) and _heads(v)
+    assert dim == v_cache.shape[3] and k.shape == v.shape == (T, k_cache.shape[1], dim)
+    assert _device_array(positions, torch.int32, (T,)) and _device_array(slots, torch.int64, (T,))
+    if q_out is None:
+        q_out = torch.empty((T, heads, dim), dtype=torch.bfloat16, device=q.device)
+    assert _heads(q_out) and q_out.shape == q.shape
+    rc = lib().qblora_rope_cache(_rope(freq, interleaved, scale), _ptr(q), _token_stride(q), heads, _ptr(k), _token_stride(k),
+                                 _ptr(v), _token_stride(v), _ptr(positions), _ptr(slots), T, _ptr(q_out),
+                                 _token_stride(q_out), cache, _stream())
+    _check(rc, "qblora_rope_cache")
+    return q_out
+
+
+def qblora_paged_attention_workspace_bytes(k_cache: torch.Tensor, v_cache: torch.Tensor, heads: int, max_new: int) -> int:
+    return int(lib().qblora_paged_attention_workspace_bytes(_cache(k_cache, v_cache), heads, max_new))
+
+
+def qblora_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor,
+                           starts: torch.Tensor, context: torch.Tensor, scale: float, window: int = 0, max_new: int = None,
+                           out: torch.Tensor = None, lse: torch.Tensor = None, workspace: torch.Tensor = None):
+    """Attention of the new tokens q [T, heads, head_dim] of a batch over their requests' pages.  max_new: the most new
+    tokens of a request, as far as it is known (default: T)."""
+    T, heads, dim = q.shape
+    n, width = table.shape
+    cache = _cache(k_cache, v_cache)
+    assert _heads(q) and dim == v_cache.shape[3] and _device_array(table, torch.int32)
+    assert _device_array(starts, torch.int32, (n + 1,)) and _device_array(context, torch.int32, (n,))
+    if max_new is None:
+        max_new = T
+    if out is None:
+        out = torch.empty((T, heads, dim), dtype=torch.bfloat16, device=q.device)
+    assert _heads(out) and out.shape == q.shape
+    assert lse is None or _device_array(lse, torch.float32, (T, heads))
+    ws = _workspace(lambda: lib().qblora_paged_attention_workspace_bytes(cache, heads, max_new), q.device, workspace)
+    rc = lib().qblora_paged_attention(_ptr(q), _token_stride(q), heads, cache, _ptr(table), width, _ptr(starts), _ptr(context),
+                                      n, T, scale, window, max_new, _ptr(out), _token_stride(out), _ptr(lse), _ptr(ws),
+                                      ws.numel() * ws.element_size(), _stream())
+    _check(rc, "qblora_paged_attention")
+    return out
+
+
+def qblora_rms_norm_fwd(x: torch.Tensor, w: torch.Tensor, eps: float, residual: torch.Tensor = None, keep: bool = False,
+                        total: torch.Tensor = None, y: torch.Tensor = None, rstd: torch.Tensor = None):
+    """(y, total, rstd): the norm of total = x + residual (x itself without one); rstd, for the backward pass, is None unless
+    `keep` is set or a tensor is given."""
+    T, d = x.shape
+    assert _device_array(x, torch.bfloat16) and _device_array(w, torch.bfloat16, (d,))
+    assert residual is None or _device_array(residual, torch.bfloat16, (T, d))
+    if y is None:
+        y = torch.empty_like(x)
+    if residual is None:
+        total = x
+    elif total is None:
+        total = torch.empty_like(x)
+    if keep and rstd is None:
+        rstd = torch.empty(T, dtype=torch.float32, device=x.device)
+    assert _device_array(y, torch.bfloat16, (T, d)) and _device_array(total, torch.bfloat16, (T, d))
+    assert rstd is None or _device_array(rstd, torch.float32, (T,))
+    rc = lib().qblora_rms_norm_fwd(_ptr(x), _ptr(residual), _ptr(w), T, d, eps, _ptr(total), _ptr(y), _ptr(rstd), _stream())
+    _check(rc, "qblora_rms_norm_fwd")
+    return y, total, rstd
+
+
+def qblora_rms_norm_bwd_workspace_bytes(T: int, d: int) -> int:
+    return int(lib().qblora_rms_norm_bwd_workspace_bytes(T, d))
+
+
+def qblora_rms_norm_bwd(total: torch.Tensor, w: torch.Tensor, rstd: torch.Tensor, dy: torch.Tensor,
+                        dtotal: torch.Tensor = None, need_dw: bool = True, dx: torch.Tensor = None, dw: torch.Tensor = None,
+                        workspace: torch.Tensor = None):
+    """(dx, dw): the gradients of the sum (x and residual alike) and of the weight."""
+    T, d = total.shape
+    dev = total.device
+    assert _device_array(total, torch.bfloat16) and _device_array(w, torch.bfloat16, (d,))
+    assert _device_array(rstd, torch.float32, (T,)) and _device_array(dy, torch.bfloat16, (T, d))
+    assert dtotal is None or _device_array(dtotal, torch.bfloat16, (T, d))
+    if dx is None:
+        dx = torch.empty((T, d), dtype=torch.bfloat16, device=dev)
+    if need_dw and dw is None:
+        dw = torch.empty(d, dtype=torch.float32, device=dev)
+    assert _device_array(dx, torch.bfloat16, (T, d)) and (dw is None or _device_array(dw, torch.float32, (d,)))
+    ws, nbytes = None, 0
+    if need_dw:
+        ws = _workspace(lambda: lib().qblora_rms_norm_bwd_workspace_bytes(T, d), dev, workspace)
+        nbytes = ws.numel() * ws.element_size()
+    rc = lib().qblora_rms_norm_bwd(_ptr(total), _ptr(w), _ptr(rstd), _ptr(dy), _ptr(dtotal), T, d, _ptr(dx),
+                                   _ptr(dw if need_dw else None), _ptr(ws), nbytes, _stream())
+    _check(rc, "qblora_rms_norm_bwd")
+    return dx, (dw if need_dw else None)

@@ -1,0 +1,221 @@
+// Addition of the residual and root-mean-square norm, forward and backward (qblora_rms_norm_fwd / _bwd).
+//
+//   total = bf16(x + residual),  r = 1 / sqrt(mean(total^2) + eps),  y = total * r * w
+//   dx = r (g - h mean(g h)) + dtotal,  dw = sum_t dy h,  with h = total * r, g = dy * w
+//
+// Bound by HBM: one pass over each array.  A workgroup holds a row in registers, 8 features a thread and chunk, so the mean
+// is known before anything is written; the only other traffic is dw.  Rows of any length and alignment: a 16-byte access
+// takes any address in one instruction, and the features behind the last whole chunk go one by one.
+#include "decoder.h"
+
+namespace qblora {
+
+namespace {
+
+// chunk c of a row of d: eight bf16 as four dwords, 0 behind the end
+__device__ __forceinline__ uint4 load_chunk(const qblora_bf16* row, int c, int d) {
+    if (8 * c + 8 <= d) {
+        const bf16x8_any v = *reinterpret_cast<const bf16x8_any*>(row + 8 * c);
+        return make_uint4(v[0], v[1], v[2], v[3]);
+    }
+    uint32_t w[4] = {0, 0, 0, 0};
+    for (int j = 0; j < 8; ++j)
+        if (8 * c + j < d) w[j / 2] |= (uint32_t)row[8 * c + j] << (16 * (j & 1));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store_chunk(qblora_bf16* row, int c, int d, uint4 v) {
+    if (8 * c + 8 <= d) {
+        bf16x8_any o = {v.x, v.y, v.z, v.w};
+        *reinterpret_cast<bf16x8_any*>(row + 8 * c) = o;
+        return;
+    }
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    for (int j = 0; j < 8; ++j)
+        if (8 * c + j < d) row[8 * c + j] = (qblora_bf16)(w[j / 2] >> (16 * (j & 1)));
+}
+__device__ __forceinline__ uint32_t word(const uint4& v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
+__device__ __forceinline__ void set_word(uint4& v, int j, uint32_t x) {
+    if (j == 0) v.x = x; else if (j == 1) v.y = x; else if (j == 2) v.z = x; else v.w = x;
+}
+
+// sum over the workgroup; `slots`: one float a wave, not reused before the next barrier but one
+__device__ __forceinline__ float block_sum(float v, float* slots) {
+    for (int s = 32; s; s >>= 1) v += __shfl_xor(v, s);
+    const int waves = blockDim.x >> 6;
+    if (waves == 1) return v;
+    if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0f;
+    for (int w = 0; w < waves; ++w) v += slots[w];
+    return v;
+}
+
+template <int NC>
+__global__ __launch_bounds__(1024) void k_rms_norm(NormDesc a) {
+    __shared__ float slots[16];
+    const int64_t row = blockIdx.x;
+    const int d = a.d, chunks = (d + 7) >> 3;
+    const qblora_bf16* x = a.x + row * d;
+    uint4 v[NC], w[NC];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = threadIdx.x + i * blockDim.x;
+        v[i] = w[i] = make_uint4(0, 0, 0, 0);
+        if (c < chunks) {
+            v[i] = load_chunk(x, c, d);
+            w[i] = load_chunk(a.w, c, d);
+        }
+    }
+    if (a.residual) {
+        const qblora_bf16* res = a.residual + row * d;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = threadIdx.x + i * blockDim.x;
+            if (c >= chunks) continue;
+            const uint4 r = load_chunk(res, c, d);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t p = word(v[i], j), q = word(r, j);
+                set_word(v[i], j, pack_bf16(bf16_lo(p) + bf16_lo(q), bf16_hi(p) + bf16_hi(q)));
+            }
+            store_chunk(a.total + row * d, c, d, v[i]);
+        }
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float lo = bf16_lo(word(v[i], j)), hi = bf16_hi(word(v[i], j));
+            sum = __fmaf_rn(lo, lo, sum);
+            sum = __fmaf_rn(hi, hi, sum);
+        }
+    const float mean = block_sum(sum / (float)d, slots);                 // each thread's part of it: their sum may pass fp32
+    const float r = 1.0f / __fsqrt_rn(mean + a.eps);
+    if (a.rstd && threadIdx.x == 0) a.rstd[row] = r;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = threadIdx.x + i * blockDim.x;
+        if (c >= chunks) continue;
+        uint4 o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t p = word(v[i], j), q = word(w[i], j);
+            set_word(o, j, pack_bf16(bf16_lo(p) * r * bf16_lo(q), bf16_hi(p) * r * bf16_hi(q)));
+        }
+        store_chunk(a.y + row * d, c, d, o);
+    }
+}
+
+template <int NC>
+__global__ __launch_bounds__(1024) void k_rms_norm_bwd(NormBackDesc a) {
+    __shared__ float slots[2][16];
+    const int d = a.d, chunks = (d + 7) >> 3;
+    uint4 w[NC];
+    float dw[NC][8];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = threadIdx.x + i * blockDim.x;
+        w[i] = c < chunks ? load_chunk(a.w, c, d) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dw[i][j] = 0.0f;
+    }
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x, turn ^= 1) {
+        const float r = a.rstd[row];
+        uint4 t[NC], y[NC], e[NC];
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = threadIdx.x + i * blockDim.x;
+            t[i] = y[i] = e[i] = make_uint4(0, 0, 0, 0);
+            if (c < chunks) {
+                t[i] = load_chunk(a.total + row * d, c, d);
+                y[i] = load_chunk(a.dy + row * d, c, d);
+                if (a.dtotal) e[i] = load_chunk(a.dtotal + row * d, c, d);
+            }
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t tp = word(t[i], j / 2), yp = word(y[i], j / 2), wp = word(w[i], j / 2);
+                const float h = ((j & 1) ? bf16_hi(tp) : bf16_lo(tp)) * r, dy = (j & 1) ? bf16_hi(yp) : bf16_lo(yp);
+                dw[i][j] = __fmaf_rn(dy, h, dw[i][j]);
+                sum = __fmaf_rn(dy * ((j & 1) ? bf16_hi(wp) : bf16_lo(wp)), h, sum);
+            }
+        const float mean = block_sum(sum / (float)d, slots[turn]);
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = threadIdx.x + i * blockDim.x;
+            if (c >= chunks) continue;
+            uint4 o;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t tp = word(t[i], j), yp = word(y[i], j), wp = word(w[i], j), ep = word(e[i], j);
+                const float lo = __fmaf_rn(-bf16_lo(tp) * r, mean, bf16_lo(yp) * bf16_lo(wp));
+                const float hi = __fmaf_rn(-bf16_hi(tp) * r, mean, bf16_hi(yp) * bf16_hi(wp));
+                set_word(o, j, pack_bf16(__fmaf_rn(r, lo, bf16_lo(ep)), __fmaf_rn(r, hi, bf16_hi(ep))));
+            }
+            store_chunk(a.dx + row * d, c, d, o);
+        }
+    }
+    if (!a.part) return;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = threadIdx.x + i * blockDim.x;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (8 * c + j < d) a.part[(int64_t)blockIdx.x * d + 8 * c + j] = dw[i][j];
+    }
+}
+
+// dw[c] = sum over the rows of `part`, 16 columns and 16 rows at a time
+__global__ __launch_bounds__(256) void k_rms_norm_dw(const float* __restrict__ part, int rows, int d, float* __restrict__ dw) {
+    __shared__ float sums[16][17];
+    const int c = blockIdx.x * 16 + (threadIdx.x & 15), r0 = threadIdx.x >> 4;
+    float s = 0.0f;
+    if (c < d)
+        for (int r = r0; r < rows; r += 16) s += part[(int64_t)r * d + c];
+    sums[r0][threadIdx.x & 15] = s;
+    __syncthreads();
+    if (r0 == 0 && c < d) {
+        s = 0.0f;
+        for (int i = 0; i < 16; ++i) s += sums[i][threadIdx.x & 15];
+        dw[c] = s;
+    }
+}
+
+int threads_of(int d) {
+    const int chunks = (d + 7) / 8, t = (chunks + 63) / 64 * 64;
+    return t < 1024 ? t : 1024;
+}
+
+}  // namespace
+
+int launch_rms_norm(const NormDesc& a, hipStream_t st) {
+    const int threads = threads_of(a.d), nc = ((a.d + 7) / 8 + threads - 1) / threads;
+    const dim3 grid((unsigned)a.T);
+    if (nc == 1) hipLaunchKernelGGL(k_rms_norm<1>, grid, dim3(threads), 0, st, a);
+    else hipLaunchKernelGGL(k_rms_norm<2>, grid, dim3(threads), 0, st, a);
+    return launch_status();
+}
+
+int64_t rms_norm_bwd_parts(int64_t T, int d) {
+    const int64_t full = 256 * 1024 / threads_of(d), some = (T + 7) / 8;
+    return some < full ? some : full;
+}
+
+int launch_rms_norm_bwd(const NormBackDesc& a, hipStream_t st) {
+    const int threads = threads_of(a.d), nc = ((a.d + 7) / 8 + threads - 1) / threads;
+    const int rows = (int)rms_norm_bwd_parts(a.T, a.d);
+    if (rows) {
+        const dim3 grid(rows);
+        if (nc == 1) hipLaunchKernelGGL(k_rms_norm_bwd<1>, grid, dim3(threads), 0, st, a);
+        else hipLaunchKernelGGL(k_rms_norm_bwd<2>, grid, dim3(threads), 0, st, a);
+    }
+    if (a.dw) hipLaunchKernelGGL(k_rms_norm_dw, dim3((a.d + 15) / 16), dim3(256), 0, st, a.part, rows, a.d, a.dw);
+    return launch_status();
+}
+
+}  // namespace qblora
