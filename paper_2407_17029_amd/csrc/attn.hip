@@ -12,10 +12,16 @@
 // of one row: that is the operand of O^T = V^T P^T as it stands.  The four waves of a workgroup take turns on the positions
 // and are joined in LDS.
 //
+// k_attn_many takes 128 rows, 32 a wave, and is bound by the matrix pipe and by the exponentials beside it.  64 positions at a
+// time go through LDS, in the order of the pages (copies of 1 KB that need no registers, two tiles in turn, one barrier a
+// tile); scores are transposed here too, so that a row's maximum and sum are a lane's own but for one exchange of halves.
+//
 // Work: requests differ by orders of magnitude, and only the device knows their lengths.  Every workgroup adds up the work
 // of all requests, which gives the number of positions that a workgroup takes if there are to be `target` of them, and finds
-// its own (request, 16 rows, range of positions) from the prefix sums.  A context that is cut this way leaves partial results
+// its own (request, rows, range of positions) from the prefix sums.  A context that is cut this way leaves partial results
 // in the workspace, which k_attn_join adds up.
+#include <climits>
+
 #include "decoder.h"
 
 namespace qblora {
@@ -25,9 +31,15 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kFewRows = 16;
 constexpr int kBlock = 32;                     // positions of a step
-constexpr int kFewTarget = 1024;               // workgroups that share the work
-constexpr int kFewMin = 8;                     // least blocks of a workgroup
+constexpr int kManyRows = 128;
 constexpr float kNegInf = -__builtin_inff();
+constexpr float kSlack = 8.0f;                 // a maximum may grow by 2^8 before what was summed is rescaled
+
+// Which requests a kernel takes, by their rows, and how it shares their work out: units of `rows` rows, `target` workgroups
+// a key / value head, at least `least` blocks each.
+struct Share { int rows, target, least; int64_t over, upto; float* part; };
+constexpr int kFewTarget = 1024, kFewLeast = 8;
+constexpr int kManyTarget = 512, kManyLeast = 16;
 
 struct Unit { int request, tile, split, splits, slot; };
 
@@ -38,27 +50,27 @@ __device__ __forceinline__ Span span_of(const AttnDesc& d, int i) {
 }
 
 struct Cost { int tiles, blocks; };
-__device__ __forceinline__ Cost cost_of(const AttnDesc& d, int i, int rows) {
+__device__ __forceinline__ Cost cost_of(const AttnDesc& d, int i, const Share& w) {
     const Span s = span_of(d, i);
-    if (s.fresh == 0) return {0, 0};
+    const int64_t rows = (int64_t)s.fresh * d.group;
+    if (rows <= w.over || rows > w.upto) return {0, 0};
     const int limit = d.width << d.page_shift;
     const int hi = min(s.context + s.fresh, limit), lo = d.window ? max(s.context + 1 - d.window, 0) : 0;
     const int blocks = hi > lo ? (hi + kBlock - 1) / kBlock - lo / kBlock : 1;
-    return {(int)(((int64_t)s.fresh * d.group + rows - 1) / rows), blocks};
+    return {(int)((rows + w.rows - 1) / w.rows), blocks};
 }
 
 // The work of workgroup unit `want` (units counted over requests, tiles and splits, or with `joins` over the tiles of split
 // requests alone); false: there is none.  All threads call it.
 struct Finder {
-    int64_t sums[kWaves];
-    int found[6];
+    int64_t sums[kWaves], ends[2][kWaves];
+    int found[5];
 };
-__device__ __forceinline__ bool find_unit(const AttnDesc& d, int rows, int target, int least, bool joins, int64_t want,
-                                          Finder& f, Unit& u) {
+__device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share, bool joins, int64_t want, Finder& f, Unit& u) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int64_t all = 0;
     for (int i = tid; i < d.n; i += kThreads) {
-        const Cost c = cost_of(d, i, rows);
+        const Cost c = cost_of(d, i, share);
         all += (int64_t)c.tiles * c.blocks;
     }
     for (int s = 32; s; s >>= 1) all += __shfl_xor(all, s);
@@ -67,14 +79,14 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, int rows, int targe
     __syncthreads();
     all = 0;
     for (int w = 0; w < kWaves; ++w) all += f.sums[w];
-    const int64_t per = max((all + target - 1) / target, (int64_t)least);       // blocks of a workgroup
+    const int64_t per = max((all + share.target - 1) / share.target, (int64_t)share.least);       // blocks of a workgroup
     int64_t units = 0, slots = 0;                                               // in front of this round's requests
     for (int base = 0; base < d.n; base += kThreads) {
         const int i = base + tid;
         int64_t mine = 0, cut = 0;
         int tiles = 0, splits = 1;
         if (i < d.n) {
-            const Cost c = cost_of(d, i, rows);
+            const Cost c = cost_of(d, i, share);
             tiles = c.tiles;
             splits = (int)((c.blocks + per - 1) / per);
             cut = splits > 1 ? (int64_t)tiles * splits : 0;
@@ -85,15 +97,14 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, int rows, int targe
             const int64_t x = __shfl_up(a, s), y = __shfl_up(b, s);
             if (lane >= s) { a += x; b += y; }
         }
-        __shared__ int64_t ends[2][kWaves];
         __syncthreads();
-        if (lane == 63) { ends[0][wave] = a; ends[1][wave] = b; }
+        if (lane == 63) { f.ends[0][wave] = a; f.ends[1][wave] = b; }
         __syncthreads();
         int64_t u0 = units, s0 = slots;
         for (int w = 0; w < kWaves; ++w) {
             if (w == wave) { a += u0; b += s0; }
-            u0 += ends[0][w];
-            s0 += ends[1][w];
+            u0 += f.ends[0][w];
+            s0 += f.ends[1][w];
         }
         units = u0;
         slots = s0;
@@ -134,19 +145,21 @@ __device__ __forceinline__ Tile tile_of(const AttnDesc& d, const Span& s, int ti
 
 __device__ __forceinline__ bool not_finite(uint32_t pair) { return (((pair & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0; }
 
-// bf16 ones where an element of the pair is NaN (kind 0), +inf (1) or -inf (2)
-__device__ __forceinline__ uint32_t indicator(uint32_t pair, int kind) {
-    uint32_t out = 0;
-    for (int h = 0; h < 2; ++h) {
-        const uint32_t x = (pair >> (16 * h)) & 0xffffu;
-        const bool is = kind == 0 ? (x & 0x7fffu) > 0x7f80u : x == (kind == 1 ? 0x7f80u : 0xff80u);
-        if (is) out |= 0x3f80u << (16 * h);
-    }
-    return out;
-}
+// all bits of an element or none
+__device__ __forceinline__ uint32_t mask_of(uint32_t bits) { return (bits & 1u) * 0xffffu | (bits >> 1 & 1u) * 0xffff0000u; }
 __device__ __forceinline__ uint32_t without_not_finite(uint32_t pair) {
     const uint32_t bad = ((pair & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
     return pair & ~((bad >> 15) * 0xffffu);
+}
+
+// an infinity or NaN, or 0
+__device__ __forceinline__ float if_not_finite(qblora_bf16 x) { return (x & 0x7f80u) == 0x7f80u ? __uint_as_float((uint32_t)x << 16) : 0.0f; }
+// feature 0 of a position's value (feature f is 8 f elements further); null where no page is listed
+template <int D>
+__device__ __forceinline__ const qblora_bf16* value_row(const AttnDesc& d, const int32_t* table, int kvh, int pos) {
+    const int id = table[pos >> d.page_shift], in_page = pos & ((1 << d.page_shift) - 1);
+    if ((uint32_t)id >= (uint32_t)d.pages) return nullptr;
+    return d.vc + (((int64_t)id * d.kv_heads + kvh) * D << d.page_shift) + (in_page >> 3) * D * 8 + (in_page & 7);
 }
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -158,14 +171,14 @@ struct FewShared {
 };
 
 template <int D>
-__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_few(AttnDesc d, int target) {
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_few(AttnDesc d, Share share) {
     constexpr int KS = D / 32, DT = D / 16;
     __shared__ Finder finder;
     __shared__ FewShared<D> sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, col = lane & 15;
     const int kvh = blockIdx.x % d.kv_heads;
     Unit u;
-    if (!find_unit(d, kFewRows, target, kFewMin, false, blockIdx.x / d.kv_heads, finder, u)) return;
+    if (!find_unit(d, share, false, blockIdx.x / d.kv_heads, finder, u)) return;
     const Span s = span_of(d, u.request);
     const Tile t = tile_of(d, s, u.tile, kFewRows);
     const int b_first = t.pos0 / kBlock, b_last = (t.pos1 + kBlock - 1) / kBlock;
@@ -195,6 +208,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_few(AttnDesc
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = f32x4{0, 0, 0, 0};
     float m = kNegInf, l = 0.0f;
+    int odd0 = INT_MAX, odd1 = 0;                                      // positions among which values are not finite
 
     int ids0 = -1, ids1 = -1;                                          // pages of the steps' halves, a step a lane
     uint4 kf[2][KS], vf[DT];
@@ -289,40 +303,32 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_few(AttnDesc
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[i][j] *= a;
         if (masked) {
-            // Values that no row sees count as 0 whatever they are: 0 * NaN would spread.  Those that some rows see and
-            // others do not are 0 as well where they are not finite, and come in through products of indicators.
-            uint32_t keep[4], vis[4];
+            // Values that no row sees count as 0 whatever they are: 0 * NaN would spread.  So do those of the other
+            // positions that are not finite, which some rows may see and others not; they are added behind the loop.
             bool odd = false;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                keep[j] = ((any >> (2 * j)) & 1 ? 0xffffu : 0u) | ((any >> (2 * j + 1)) & 1 ? 0xffff0000u : 0u);
-                vis[j] = ((seen >> (2 * j)) & 1 ? 0x3f80u : 0u) | ((seen >> (2 * j + 1)) & 1 ? 0x3f800000u : 0u);
-            }
-#pragma unroll
             for (int i = 0; i < DT; ++i) {
-                vf[i] = make_uint4(vf[i].x & keep[0], vf[i].y & keep[1], vf[i].z & keep[2], vf[i].w & keep[3]);
-                odd |= not_finite(vf[i].x) || not_finite(vf[i].y) || not_finite(vf[i].z) || not_finite(vf[i].w);
+                const uint4 v = make_uint4(vf[i].x & mask_of(any), vf[i].y & mask_of(any >> 2), vf[i].z & mask_of(any >> 4), vf[i].w & mask_of(any >> 6));
+                odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
+                vf[i] = make_uint4(without_not_finite(v.x), without_not_finite(v.y), without_not_finite(v.z), without_not_finite(v.w));
             }
             if (__any(odd)) {
-                const bf16x8 seen_ones = __builtin_bit_cast(bf16x8, make_uint4(vis[0], vis[1], vis[2], vis[3]));
-#pragma unroll
-                for (int i = 0; i < DT; ++i) {
-                    const uint4 v = vf[i];
-#pragma unroll
-                    for (int kind = 0; kind < 3; ++kind) {
-                        const uint4 is = make_uint4(indicator(v.x, kind), indicator(v.y, kind), indicator(v.z, kind), indicator(v.w, kind));
-                        const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, is), seen_ones, f32x4{0, 0, 0, 0}, 0, 0, 0);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (n[j] > 0.0f) o[i][j] += kind == 0 ? __builtin_nanf("") : kind == 1 ? -kNegInf : kNegInf;
-                    }
-                    vf[i] = make_uint4(without_not_finite(v.x), without_not_finite(v.y), without_not_finite(v.z), without_not_finite(v.w));
-                }
+                odd0 = min(odd0, base);
+                odd1 = base + kBlock;
             }
         }
 #pragma unroll
         for (int i = 0; i < DT; ++i) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[i]), pf, o[i], 0, 0, 0);
         if (step + 1 < steps) load_values(step + 1, id0, id1);
+    }
+
+    for (int pos = odd0; pos < min(odd1, t.pos1); ++pos) {
+        const qblora_bf16* v = value_row<D>(d, table, kvh, pos);
+        if (!v || !real || pos > here || pos <= row_low) continue;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[i][j] += if_not_finite(v[(16 * i + 4 * g + j) * 8]);
     }
 
     l += __shfl_xor(l, 16);
@@ -332,7 +338,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_few(AttnDesc
 #pragma unroll
         for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4*>(&sh.o[wave][col][16 * i + 4 * g]) = o[i];
     __syncthreads();
-    float* part = u.splits > 1 ? d.part + ((int64_t)u.slot * d.kv_heads + kvh) * (kFewRows * (D + 2)) : nullptr;
+    float* part = u.splits > 1 ? share.part + ((int64_t)u.slot * d.kv_heads + kvh) * (kFewRows * (D + 2)) : nullptr;
     for (int i = tid; i < t.rows * (D / 4); i += kThreads) {
         const int r = i / (D / 4), f = 4 * (i % (D / 4));
         float top = kNegInf;
@@ -344,7 +350,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_few(AttnDesc
             const float a = exp2_of(sh.m[w][r] - use);
             sum = __fmaf_rn(sh.l[w][r], a, sum);
             const f32x4 x = *reinterpret_cast<const f32x4*>(&sh.o[w][r][f]);
-            for (int j = 0; j < 4; ++j) v[j] += sh.m[w][r] == kNegInf ? 0.0f : x[j] * a;
+            for (int j = 0; j < 4; ++j) v[j] = __fmaf_rn(x[j], a, v[j]);
         }
         if (part) {
             *reinterpret_cast<f32x4*>(part + r * D + f) = v;
@@ -358,62 +364,374 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_few(AttnDesc
     }
 }
 
-// Adds up the partial results of a split tile: weights 2^(m - max m).
-template <int D, int ROWS>
-__global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, int target, int least) {
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+// 64 lanes x 16 bytes from anywhere to lds_base + 16 * lane
+__device__ __forceinline__ void gather_to_lds(const void* p, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_base), "v"(p) : "memory");
+}
+// the same from uniform_base + lane_offset
+__device__ __forceinline__ void copy_to_lds(const void* uniform_base, uint32_t lane_offset, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds_base), "v"(lane_offset), "s"(uniform_base) : "memory");
+}
+__device__ __forceinline__ void wait_for_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// of both halves of the wave
+__device__ __forceinline__ float max_of_halves(float x) {
+    const uint32_t u = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_of_halves(float x) {
+    const uint32_t u = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_many(AttnDesc d, Share share) {
+    // positions of a tile: 64, or 32 where the registers hold no more beside 256 features
+    constexpr int kTile = D > 128 ? 32 : 64, KS = D / 16, DT = D / 32, TT = kTile / 32, PS = kTile / 16;
+    constexpr int kTileBytes = kTile * D * 2;
+    constexpr int kCopies = kTileBytes / 1024 / kWaves;                // of keys, and again of values, a wave and tile
     __shared__ Finder finder;
+    __shared__ __attribute__((aligned(16))) unsigned char buf[2][2][kTileBytes];          // [turn][keys, values]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
     const int kvh = blockIdx.x % d.kv_heads;
     Unit u;
-    if (!find_unit(d, ROWS, target, least, true, blockIdx.x / d.kv_heads, finder, u)) return;
+    if (!find_unit(d, share, false, blockIdx.x / d.kv_heads, finder, u)) return;
     const Span s = span_of(d, u.request);
-    const Tile t = tile_of(d, s, u.tile, ROWS);
+    const int tiles = (int)(((int64_t)s.fresh * d.group + kManyRows - 1) / kManyRows);
+    const Tile t = tile_of(d, s, tiles - 1 - u.tile, kManyRows);       // the longest ranges first
+    const int limit = d.width << d.page_shift;
+    const int n_first = t.pos0 / kTile, n_last = (t.pos1 + kTile - 1) / kTile;
+    const int per = (max(n_last - n_first, 0) + u.splits - 1) / u.splits;
+    const int n0 = n_first + u.split * per, n1 = min(n0 + per, n_last);
+
+    // the wave's rows, and what of the positions all of them see
+    const int w_rows = min(32, t.rows - 32 * wave);
+    const int row = t.row0 + 32 * wave + col, token = row / d.group, head = kvh * d.group + row % d.group;
+    const bool real = col < w_rows;
+    const int here = s.context + token, row_low = d.window ? here - d.window : -1;
+    const int first = s.context + (t.row0 + 32 * wave) / d.group, last = s.context + (t.row0 + 32 * wave + max(w_rows, 1) - 1) / d.group;
+    const int full0 = d.window ? max(last + 1 - d.window, 0) : 0, full1 = min(first + 1, limit);
+    const int see0 = d.window ? max(first + 1 - d.window, 0) : 0, see1 = w_rows > 0 ? min(last + 1, limit) : 0;
+
+    // rows: operand B, row = lane & 31, features 16 i + 8 h ..; a negative scale is the rows' sign, one of 0 makes them 0
+    const float c = d.scale_log2 == 0.0f ? 1.0f : fabsf(d.scale_log2);
+    const uint32_t flip = d.scale_log2 < 0.0f ? 0x80008000u : 0u, keep_q = d.scale_log2 == 0.0f ? 0u : 0xffffffffu;
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (real) v = *reinterpret_cast<const uint4*>(d.q + (int64_t)(s.start + token) * d.ldq + (int64_t)head * D + 16 * i + 8 * h);
+        v = make_uint4((v.x ^ flip) & keep_q, (v.y ^ flip) & keep_q, (v.z ^ flip) & keep_q, (v.w ^ flip) & keep_q);
+        qf[i] = __builtin_bit_cast(bf16x8, v);
+    }
+
+    const int shift = d.page_shift, page = 1 << shift;
+    const int64_t page_elems = (int64_t)d.kv_heads * D << shift, head_elems = ((int64_t)kvh * D) << shift;
+    const int32_t* table = d.table + (int64_t)u.request * d.width;
+    const uint32_t lds = lds_address(buf);
+
+    auto page_id = [&](int tile) {                                     // of the tile's position `lane` (and again behind 32)
+        const int pos = tile * kTile + lane % kTile;
+        return tile < n1 && pos < t.pos1 ? table[pos >> shift] : -1;
+    };
+    // copies of a tile with these pages; which of its positions are listed
+    auto copy = [&](int tile, int id, int turn) {
+        const bool ok = (uint32_t)id < (uint32_t)d.pages;
+        id = ok ? id : 0;
+        const int in_page = (tile * kTile + lane % kTile) & (page - 1);
+        const qblora_bf16* k = d.kc + id * page_elems + head_elems + (((lane / kTile) << shift) + in_page) * 8;
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const int part = wave * kCopies + i;
+            gather_to_lds(k + (part * (64 / kTile) << shift) * 8, lds + (uint32_t)(turn * 2 * kTileBytes + part * 1024));
+        }
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const int part = wave * kCopies + i, octet = part / (D / 64), f0 = part % (D / 64) * 64;
+            const int o_id = __builtin_amdgcn_readlane(id, 8 * octet);
+            const int o_page = ((tile * kTile + 8 * octet) & (page - 1)) >> 3;
+            const qblora_bf16* v = d.vc + o_id * page_elems + head_elems + (o_page * D + f0) * 8;
+            copy_to_lds(v, 16 * lane, lds + (uint32_t)(turn * 2 * kTileBytes + kTileBytes + part * 1024));
+        }
+        return __ballot(ok);
+    };
+
+    f32x16 o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
+    float m = kNegInf, l = 0.0f;                                       // l: of this lane's positions
+    int odd0 = INT_MAX, odd1 = 0;                                      // positions among which values are not finite
+
+    // position of row `col` of a 32 x 32 tile, so that a lane's scores are of eight consecutive positions twice
+    const int perm = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
+    uint64_t listed = 0, next_listed = 0;
+    int id = page_id(n0);
+    if (n0 < n1) {
+        listed = copy(n0, id, 0);
+        id = page_id(n0 + 1);
+    }
+    for (int tile = n0, turn = 0; tile < n1; ++tile, turn ^= 1) {
+        wait_for_copies();
+        __syncthreads();                                               // the tile is there, and the other one is free
+        if (tile + 1 < n1) {
+            const int now = id;
+            id = page_id(tile + 2);
+            next_listed = copy(tile + 1, now, turn ^ 1);
+        }
+        const int base = tile * kTile;
+        if (base < see1 && base + kTile > see0) {
+            const unsigned char* kb = buf[turn][0] + (h * kTile + perm) * 16;
+            const unsigned char* vb = buf[turn][1] + (h * D + col) * 16;
+            f32x16 sc[TT];
+#pragma unroll
+            for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sc[tt][j] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+#pragma unroll
+                for (int tt = 0; tt < TT; ++tt)
+                    sc[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kb + 2 * i * kTile * 16 + tt * 512)), qf[i], sc[tt], 0, 0, 0);
+                if (D > 128 && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // no more operands ahead than registers
+            }
+            const bool masked = base < full0 || base + kTile > full1 || ~listed != 0;
+            uint32_t seen = 0xffffffffu, any = 0xffffffffu;            // bit 8 s + j: position 16 s + 8 h + j of the tile
+            if (masked) {
+                seen = any = 0;
+#pragma unroll
+                for (int s4 = 0; s4 < PS; ++s4) {
+                    const uint32_t here8 = (uint32_t)(listed >> (16 * s4 + 8 * h)) & 0xffu;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int pos = base + 16 * s4 + 8 * h + j;
+                        if (pos >= see0 && pos < see1) any |= 1u << (8 * s4 + j);
+                        if (pos <= here && pos > row_low) seen |= 1u << (8 * s4 + j);
+                    }
+                    any &= ~(0xffu << (8 * s4)) | here8 << (8 * s4);
+                }
+                seen &= any;
+#pragma unroll
+                for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sc[tt][j] = (seen >> (16 * tt + j)) & 1 ? sc[tt][j] : kNegInf;
+            }
+            float top = sc[0][0];
+#pragma unroll
+            for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) top = fmaxf(top, sc[tt][j]);
+            top = max_of_halves(top);                                  // m, top: maxima of the products, not scaled yet
+            if (__any(top * c > m * c + kSlack || m == kNegInf)) {
+                const float m_new = fmaxf(m, top), a = exp2_of((m - (m_new == kNegInf ? 0.0f : m_new)) * c);
+                m = m_new;
+                l *= a;
+#pragma unroll
+                for (int i = 0; i < DT; ++i)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[i][j] *= a;
+            }
+            // The exponents c (s - m), as c s - (c m) in one operation while the rounding of c m, 2^-24 of it, is nothing
+            const float m_use = m == kNegInf ? 0.0f : m, mc = m_use * c;
+            if (__any(fabsf(mc) > 1024.0f)) {
+#pragma unroll
+                for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sc[tt][j] = (sc[tt][j] - m_use) * c;
+            } else {
+#pragma unroll
+                for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sc[tt][j] = __fmaf_rn(sc[tt][j], c, -mc);
+            }
+            bf16x8 pf[PS];
+#pragma unroll
+            for (int s4 = 0; s4 < PS; ++s4) {
+                uint32_t pw[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float p0 = exp2_of(sc[s4 >> 1][8 * (s4 & 1) + 2 * j]);
+                    const float p1 = exp2_of(sc[s4 >> 1][8 * (s4 & 1) + 2 * j + 1]);
+                    l += p0 + p1;
+                    pw[j] = pack_bf16(p0, p1);
+                }
+                pf[s4] = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+            }
+            if (!masked) {
+#pragma unroll
+                for (int s4 = 0; s4 < PS; ++s4) {
+#pragma unroll
+                    for (int i = 0; i < DT; ++i)
+                        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                            __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(vb + (2 * s4 * D + 32 * i) * 16)), pf[s4], o[i], 0, 0, 0);
+                    if (D > 128) __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+                // as in k_attn_few: values that no row sees are 0, and what is not finite is added behind the loop
+                bool odd = false;
+#pragma unroll
+                for (int s4 = 0; s4 < PS; ++s4) {
+                    const uint32_t bits = any >> (8 * s4), k0 = mask_of(bits), k1 = mask_of(bits >> 2), k2 = mask_of(bits >> 4), k3 = mask_of(bits >> 6);
+#pragma unroll
+                    for (int i = 0; i < DT; ++i) {
+                        uint4 v = *reinterpret_cast<const uint4*>(vb + (2 * s4 * D + 32 * i) * 16);
+                        v = make_uint4(v.x & k0, v.y & k1, v.z & k2, v.w & k3);
+                        odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
+                        v = make_uint4(without_not_finite(v.x), without_not_finite(v.y), without_not_finite(v.z), without_not_finite(v.w));
+                        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pf[s4], o[i], 0, 0, 0);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (__any(odd)) {
+                    odd0 = min(odd0, base);
+                    odd1 = base + kTile;
+                }
+            }
+        }
+        listed = next_listed;
+    }
+
+    // (the lane's row again: the loop has no registers to keep it in)
+    const int h2 = (int)opaque_bits((uint32_t)h), r = 32 * wave + (int)opaque_bits((uint32_t)col), to = (t.row0 + r) / d.group, q_head = kvh * d.group + (t.row0 + r) % d.group;
+    for (int pos = odd0; pos < min(odd1, see1); ++pos) {
+        const qblora_bf16* v = value_row<D>(d, table, kvh, pos);
+        if (!v || r >= t.rows || pos > s.context + to || (d.window && pos <= s.context + to - d.window)) continue;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[i][j] += if_not_finite(v[(32 * i + 8 * (j >> 2) + 4 * h2 + (j & 3)) * 8]);
+    }
+
+    l = sum_of_halves(l);
+    m *= c;
+    if (r >= t.rows) return;
+    if (u.splits > 1) {
+        float* part = share.part + ((int64_t)u.slot * d.kv_heads + kvh) * (kManyRows * (D + 2));
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                *reinterpret_cast<float4*>(part + r * D + 32 * i + 8 * b + 4 * h2) = make_float4(o[i][4 * b], o[i][4 * b + 1], o[i][4 * b + 2], o[i][4 * b + 3]);
+        if (h2 == 0) { part[kManyRows * D + r] = m; part[kManyRows * (D + 1) + r] = l; }
+        return;
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    qblora_bf16* out = d.out + (int64_t)(s.start + to) * d.ldo + (int64_t)q_head * D;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+            *reinterpret_cast<uint2*>(out + 32 * i + 8 * b + 4 * h2) =
+                make_uint2(pack_bf16(o[i][4 * b] * inv, o[i][4 * b + 1] * inv), pack_bf16(o[i][4 * b + 2] * inv, o[i][4 * b + 3] * inv));
+    if (h2 == 0 && d.lse) d.lse[(int64_t)(s.start + to) * d.heads + q_head] = (m + __builtin_log2f(l)) * 0.69314718055994530942f;
+}
+
+// Adds up the partial results of a split tile, weights 2^(m - max m): a workgroup takes every gridDim.y-th row, four
+// features a thread, and what threads are left over share the parts.
+template <int D, int ROWS, bool LAST_FIRST>
+__global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share share) {
+    constexpr int kQuads = D / 4, kGroups = kThreads / kQuads, kMost = kFewTarget;
+    __shared__ Finder finder;
+    __shared__ float weight[kMost];
+    __shared__ float top_of[kWaves], sum_of[kWaves];
+    __shared__ f32x4 sums[kGroups][kQuads];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, quad = tid % kQuads, grp = tid / kQuads;
+    const int kvh = blockIdx.x % d.kv_heads;
+    Unit u;
+    if (!find_unit(d, share, true, blockIdx.x / d.kv_heads, finder, u)) return;
+    const Span s = span_of(d, u.request);
+    const int tiles = (int)(((int64_t)s.fresh * d.group + ROWS - 1) / ROWS);
+    const Tile t = tile_of(d, s, LAST_FIRST ? tiles - 1 - u.tile : u.tile, ROWS);
     constexpr int64_t kPart = ROWS * (D + 2);
     const int64_t step = kPart * d.kv_heads;
-    const float* part = d.part + ((int64_t)u.slot * d.kv_heads + kvh) * kPart;
-    for (int i = threadIdx.x; i < t.rows * D; i += kThreads) {
-        const int r = i / D, f = i % D;
+    const float* part = share.part + ((int64_t)u.slot * d.kv_heads + kvh) * kPart;
+    for (int r = blockIdx.y; r < t.rows; r += gridDim.y) {
         float top = kNegInf;
-        for (int k = 0; k < u.splits; ++k) top = fmaxf(top, part[k * step + ROWS * D + r]);
-        const float use = top == kNegInf ? 0.0f : top;
-        float sum = 0.0f, v = 0.0f;
-        for (int k = 0; k < u.splits; ++k) {
-            const float mk = part[k * step + ROWS * D + r], a = exp2_of(mk - use);
-            sum = __fmaf_rn(part[k * step + ROWS * (D + 1) + r], a, sum);
-            if (mk != kNegInf) v = __fmaf_rn(part[k * step + i], a, v);
+        for (int k = tid; k < u.splits; k += kThreads) {
+            weight[k] = part[k * step + ROWS * D + r];
+            top = fmaxf(top, weight[k]);
         }
-        const int64_t tok = s.start + (t.row0 + r) / d.group, h = kvh * d.group + (t.row0 + r) % d.group;
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        d.out[tok * d.ldo + h * D + f] = (qblora_bf16)pack_bf16(v * inv, 0.0f);
-        if (f == 0 && d.lse) d.lse[tok * d.heads + h] = (top + __builtin_log2f(sum)) * 0.69314718055994530942f;
+        for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+        if (lane == 0) top_of[wave] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
+        const float use = top == kNegInf ? 0.0f : top;
+        float sum = 0.0f;
+        for (int k = tid; k < u.splits; k += kThreads) {
+            weight[k] = exp2_of(weight[k] - use);
+            sum = __fmaf_rn(part[k * step + ROWS * (D + 1) + r], weight[k], sum);
+        }
+        for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x);
+        if (lane == 0) sum_of[wave] = sum;
+        __syncthreads();
+        sum = (sum_of[0] + sum_of[1]) + (sum_of[2] + sum_of[3]);
+        f32x4 v = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int k = grp; k < u.splits; k += kGroups) {
+            const float a = weight[k];
+            const f32x4 x = *reinterpret_cast<const f32x4*>(part + k * step + r * D + 4 * quad);
+            for (int j = 0; j < 4; ++j) v[j] = __fmaf_rn(x[j], a, v[j]);
+        }
+        sums[grp][quad] = v;
+        __syncthreads();
+        if (grp == 0) {
+            for (int g = 1; g < kGroups; ++g) v += sums[g][quad];
+            const int64_t tok = s.start + (t.row0 + r) / d.group, h = kvh * d.group + (t.row0 + r) % d.group;
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            *reinterpret_cast<uint2*>(d.out + tok * d.ldo + h * D + 4 * quad) =
+                make_uint2(pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv));
+            if (quad == 0 && d.lse) d.lse[tok * d.heads + h] = (top + __builtin_log2f(sum)) * 0.69314718055994530942f;
+        }
+        __syncthreads();
     }
 }
 
-// units over all key / value heads
-int target_of(int kv_heads) { return (kFewTarget + kv_heads - 1) / kv_heads; }
+// `target` counts workgroups over all key / value heads
+int target_of(int target, int kv_heads) { return (target + kv_heads - 1) / kv_heads; }
+size_t part_floats(int target, int kv_heads, int rows, int head_dim) {
+    return (size_t)2 * target_of(target, kv_heads) * kv_heads * rows * (head_dim + 2);
+}
+// More rows than this in a request, if the caller knows of any, and they go through LDS.
+bool many_rows(int group, int max_new) { return (int64_t)group * max_new > kFewRows; }
 
 template <int D>
-int launch_few(const AttnDesc& d, hipStream_t st) {
-    const int target = target_of(d.kv_heads);
-    const int64_t tiles = (int64_t)d.T * d.group / kFewRows + d.n, grid = (tiles + target) * d.kv_heads;
-    if (grid > INT32_MAX) return QBLORA_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(k_attn_few<D>, dim3((unsigned)grid), dim3(kThreads), 0, st, d, target);
-    const int64_t joins = (tiles < target ? tiles : target) * d.kv_heads;
-    hipLaunchKernelGGL((k_attn_join<D, kFewRows>), dim3((unsigned)joins), dim3(kThreads), 0, st, d, target, kFewMin);
+int launch(const AttnDesc& d, hipStream_t st) {
+    const bool many = many_rows(d.group, d.max_new);
+    Share few{kFewRows, target_of(kFewTarget, d.kv_heads), kFewLeast, 0, many ? (int64_t)kFewRows : INT64_MAX, d.part};
+    const int64_t few_tiles = many ? d.n : (int64_t)d.T * d.group / kFewRows + d.n, few_grid = (few_tiles + few.target) * d.kv_heads;
+    Share lot{kManyRows, target_of(kManyTarget, d.kv_heads), kManyLeast, kFewRows, INT64_MAX,
+              d.part + part_floats(kFewTarget, d.kv_heads, kFewRows, D)};
+    const int64_t lot_tiles = (int64_t)d.T * d.group / kManyRows + d.n, lot_grid = (lot_tiles + lot.target) * d.kv_heads;
+    if (few_grid > INT32_MAX || lot_grid > INT32_MAX) return QBLORA_ERR_UNSUPPORTED;
+    const auto least = [&](int64_t tiles, const Share& w) { return (unsigned)((tiles < w.target ? tiles : w.target) * d.kv_heads); };
+    if (many) hipLaunchKernelGGL(k_attn_many<D>, dim3((unsigned)lot_grid), dim3(kThreads), 0, st, d, lot);
+    hipLaunchKernelGGL(k_attn_few<D>, dim3((unsigned)few_grid), dim3(kThreads), 0, st, d, few);
+    if (many) hipLaunchKernelGGL((k_attn_join<D, kManyRows, true>), dim3(least(lot_tiles, lot), 16), dim3(kThreads), 0, st, d, lot);
+    hipLaunchKernelGGL((k_attn_join<D, kFewRows, false>), dim3(least(few_tiles, few), d.group < kFewRows ? d.group : kFewRows), dim3(kThreads),
+                       0, st, d, few);
     return launch_status();
 }
 
 }  // namespace
 
 size_t attention_part_bytes(int head_dim, int kv_heads, int group, int max_new) {
-    (void)group; (void)max_new;
-    return (size_t)2 * target_of(kv_heads) * kv_heads * kFewRows * (head_dim + 2) * sizeof(float);
+    size_t floats = part_floats(kFewTarget, kv_heads, kFewRows, head_dim);
+    if (many_rows(group, max_new)) floats += part_floats(kManyTarget, kv_heads, kManyRows, head_dim);
+    return floats * sizeof(float);
 }
 
 int launch_attention(const AttnDesc& d, hipStream_t st) {
     switch (d.head_dim) {
-        case 64: return launch_few<64>(d, st);
-        case 128: return launch_few<128>(d, st);
-        default: return launch_few<256>(d, st);
+        case 64: return launch<64>(d, st);
+        case 128: return launch<128>(d, st);
+        default: return launch<256>(d, st);
     }
 }
 
