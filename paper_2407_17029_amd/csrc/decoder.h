@@ -6,6 +6,7 @@ namespace qblora {
 
 // Eight bf16 at any address: a global access takes any in one instruction.
 typedef uint32_t bf16x8_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t bf16x4_any __attribute__((ext_vector_type(2), aligned(2)));
 
 __device__ __forceinline__ float bf16_lo(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }

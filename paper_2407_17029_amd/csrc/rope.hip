@@ -3,8 +3,12 @@
 //
 //   pair (a, b) of a head at position p:  a' = scale (a cos x - b sin x),  b' = scale (b cos x + a sin x),  x = p * freq
 //
-// Bound by HBM, each element read and written once, or by the launch with few tokens.  A workgroup takes kTokens tokens,
-// forms their sines and cosines once for all heads in LDS, and moves 8 features a thread.
+// Bound by HBM, each element read and written once, or by the launch with few tokens.  k_rope: a thread keeps the sines and
+// cosines of its 16 features (eight pairs) in registers and takes one head after another, four in flight, 16 bytes an
+// access.  Tokens of a prompt that go to the cache come eight to a workgroup, neighbouring lanes one behind the other, so that
+// eight keys' 16-byte octets are one 128-byte line of their page and eight values of a feature one 16-byte store; single
+// tokens come one to a workgroup, which is four times as many of them.  k_rope_any: parts of a head that are no multiple of
+// 16 features.
 #include "decoder.h"
 
 namespace qblora {
@@ -12,6 +16,7 @@ namespace qblora {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kManyTokens = 256;               // from here on, tokens that go to the cache are taken for prompts
 
 // cos and sin of p * freq: in 64 bits down to one turn, then by the hardware's functions of turns
 __device__ __forceinline__ void turn(int32_t p, float freq, float scale, float& c, float& s) {
@@ -75,10 +80,148 @@ __global__ __launch_bounds__(kThreads) void k_rope_any(RopeDesc d) {
     }
 }
 
+constexpr int kHeads = 4;                      // in flight
+
+struct RopeGrid { int qk_blocks, v_blocks; };  // of blockIdx.y
+
+template <int TB, bool PAIRS>
+__global__ __launch_bounds__(kThreads) void k_rope(RopeDesc d, RopeGrid grid) {
+    const int tid = threadIdx.x;
+    const int64_t t0 = (int64_t)blockIdx.x * TB;
+    if ((int)blockIdx.y < grid.qk_blocks) {
+        const int units = d.head_dim >> 4, turning = d.rot >> 4, lanes = kThreads / (TB * units);
+        const int tb = tid % TB, u = tid / TB % units, hl = tid / (TB * units);
+        const int64_t t = t0 + tb;
+        if (hl >= lanes || t >= d.T) return;
+        const bool turns = u < turning;
+        // the unit's two chunks of eight features
+        const int c0 = !PAIRS && turns ? u : 2 * u, c1 = !PAIRS && turns ? u + turning : 2 * u + 1;
+        float cs[8], sn[8];
+        if (turns) {
+            const int32_t p = d.positions[t];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                turn(p, d.freq[8 * u + j], d.scale, cs[j], sn[j]);
+                sn[j] *= d.sign;
+            }
+        }
+        const int64_t slot = d.kc ? d.slots[t] : -1;
+        const int all = d.heads + d.kv_heads;
+        for (int h0 = hl + (int)blockIdx.y * lanes * kHeads; h0 < all; h0 += grid.qk_blocks * lanes * kHeads) {
+            bf16x8_any x[kHeads][2];
+#pragma unroll
+            for (int i = 0; i < kHeads; ++i) {
+                const int h = h0 + i * lanes;
+                if (h >= all) continue;
+                const qblora_bf16* in = h < d.heads ? d.q + t * d.ldq + h * d.head_dim : d.k + t * d.ldk + (h - d.heads) * d.head_dim;
+                x[i][0] = *reinterpret_cast<const bf16x8_any*>(in + 8 * c0);
+                x[i][1] = *reinterpret_cast<const bf16x8_any*>(in + 8 * c1);
+            }
+#pragma unroll
+            for (int i = 0; i < kHeads; ++i) {
+                const int h = h0 + i * lanes;
+                if (h >= all) continue;
+                bf16x8_any y[2] = {x[i][0], x[i][1]};
+                if (turns) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (PAIRS) {                                   // a dword is a pair
+#pragma unroll
+                            for (int c = 0; c < 2; ++c) {
+                                const float a = bf16_lo(x[i][c][j]), b = bf16_hi(x[i][c][j]);
+                                y[c][j] = pack_bf16(__fmaf_rn(a, cs[4 * c + j], -(b * sn[4 * c + j])), __fmaf_rn(b, cs[4 * c + j], a * sn[4 * c + j]));
+                            }
+                        } else {                                       // the two chunks are eight pairs
+                            const float a0 = bf16_lo(x[i][0][j]), a1 = bf16_hi(x[i][0][j]), b0 = bf16_lo(x[i][1][j]), b1 = bf16_hi(x[i][1][j]);
+                            const float k0 = cs[2 * j], k1 = cs[2 * j + 1], s0 = sn[2 * j], s1 = sn[2 * j + 1];
+                            y[0][j] = pack_bf16(__fmaf_rn(a0, k0, -(b0 * s0)), __fmaf_rn(a1, k1, -(b1 * s1)));
+                            y[1][j] = pack_bf16(__fmaf_rn(b0, k0, a0 * s0), __fmaf_rn(b1, k1, a1 * s1));
+                        }
+                    }
+                }
+                qblora_bf16 *o0, *o1;
+                if (h >= d.heads && d.kc) {
+                    if (!in_cache(d, slot)) continue;
+                    int place;
+                    qblora_bf16* out = d.kc + page_of(d, slot, h - d.heads, place);
+                    o0 = out + key_at(d, place, 8 * c0);
+                    o1 = out + key_at(d, place, 8 * c1);
+                } else {
+                    qblora_bf16* out = h < d.heads ? d.q_out + t * d.ldq_out + h * d.head_dim : d.k_out + t * d.ldk_out + (h - d.heads) * d.head_dim;
+                    o0 = out + 8 * c0;
+                    o1 = out + 8 * c1;
+                }
+                *reinterpret_cast<bf16x8_any*>(o0) = y[0];
+                *reinterpret_cast<bf16x8_any*>(o1) = y[1];
+            }
+        }
+        return;
+    }
+
+    // values: four features a thread, and the run of tokens whose slots follow each other up to the end of an octet
+    const int first = ((int)blockIdx.y - grid.qk_blocks) * kThreads + tid, step = grid.v_blocks * kThreads;
+    const int quads = d.kv_heads * d.head_dim / 4;
+    for (int b = 0; b < TB && t0 + b < d.T; ++b) {
+        const int64_t t = t0 + b, slot = d.slots[t];
+        if (!in_cache(d, slot)) continue;
+        int run = 1;
+        if (TB > 1) {
+            if (t > 0 && (slot & 7) && d.slots[t - 1] == slot - 1) continue;             // in another token's run
+            while (((slot + run) & 7) && t + run < d.T && d.slots[t + run] == slot + run) ++run;
+        }
+        for (int i = first; i < quads; i += step) {
+            const int f = 4 * i % d.head_dim, h = 4 * i / d.head_dim;
+            int place;
+            qblora_bf16* out = d.vc + page_of(d, slot, h, place);
+            out += value_at(d, place, f);
+            const qblora_bf16* in = d.v + t * d.ldv + 4 * i;
+            if (run == 8) {
+                bf16x4_any x[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = *reinterpret_cast<const bf16x4_any*>(in + k * d.ldv);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    bf16x8_any y;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t lo = x[2 * k][j >> 1], hi = x[2 * k + 1][j >> 1];
+                        y[k] = j & 1 ? (lo >> 16) | (hi & 0xffff0000u) : (lo & 0xffffu) | (hi << 16);
+                    }
+                    *reinterpret_cast<bf16x8_any*>(out + 8 * j) = y;
+                }
+            } else {
+                for (int k = 0; k < run; ++k) {
+                    const bf16x4_any x = *reinterpret_cast<const bf16x4_any*>(in + k * d.ldv);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) out[8 * j + k] = (qblora_bf16)(j & 1 ? x[j >> 1] >> 16 : x[j >> 1]);
+                }
+            }
+        }
+    }
+}
+
 }  // namespace
 
 int launch_rope(const RopeDesc& d, hipStream_t st) {
-    hipLaunchKernelGGL(k_rope_any, dim3((unsigned)d.T), dim3(kThreads), 0, st, d);
+    const int units = d.head_dim / 16, all = d.heads + d.kv_heads;
+    if (d.head_dim % 16 != 0 || d.rot % 16 != 0 || units > kThreads / 8) {
+        hipLaunchKernelGGL(k_rope_any, dim3((unsigned)d.T), dim3(kThreads), 0, st, d);
+        return launch_status();
+    }
+    const bool prompts = d.kc && d.T >= kManyTokens;
+    const int tb = prompts ? 8 : 1, lanes = kThreads / (tb * units);
+    // workgroups of a token (or eight): one pass over the heads each, few tokens; two passes, many
+    const int groups = (all + lanes * kHeads - 1) / (lanes * kHeads);
+    RopeGrid g{groups, 0};
+    if (d.vc) g.v_blocks = (d.kv_heads * d.head_dim / 4 + kThreads - 1) / kThreads;
+    const dim3 grid((unsigned)((d.T + tb - 1) / tb), g.qk_blocks + g.v_blocks), threads(kThreads);
+    if (tb == 8) {
+        if (d.interleaved) hipLaunchKernelGGL((k_rope<8, true>), grid, threads, 0, st, d, g);
+        else hipLaunchKernelGGL((k_rope<8, false>), grid, threads, 0, st, d, g);
+    } else {
+        if (d.interleaved) hipLaunchKernelGGL((k_rope<1, true>), grid, threads, 0, st, d, g);
+        else hipLaunchKernelGGL((k_rope<1, false>), grid, threads, 0, st, d, g);
+    }
     return launch_status();
 }
 
