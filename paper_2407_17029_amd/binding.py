@@ -589,30 +589,36 @@ def qblora_linear_decode(qw: QWeight, X: torch.Tensor, Y: torch.Tensor = None, w
 
 
 # ---- between the projections of a decoder layer ---------------------------------------------------------
+#
+# These calls take a few microseconds on the GPU while a batch decodes, less than careless marshalling costs: each tensor is
+# looked at once, and what is made here is not looked at again.
+
+_BF16, _F32, _I32, _I64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
 
 
-def _device_array(t, dtype, shape=None) -> bool:
-    return t.is_cuda and t.dtype == dtype and t.is_contiguous() and (shape is None or t.shape == shape)
+def _address(t, dtype, *shape) -> int:
+    """Of a contiguous device array of this type and shape."""
+    assert t.dtype is dtype and t.is_cuda and t.is_contiguous() and t.shape == shape
+    return t.data_ptr()
 
 
-def _heads(t) -> bool:
-    """bf16 [tokens, heads, head_dim] on the device: any stride between tokens, heads one behind the other."""
-    return (t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3
-            and (t.numel() == 0 or (t.stride(2) == 1 or t.shape[2] == 1) and (t.stride(1) == t.shape[2] or t.shape[1] == 1)))
-
-
-def _token_stride(t) -> int:
-    """Elements from one token to the next (a single token has none: any stride that is long enough does)."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), -(-t.shape[1] * t.shape[2] // 8) * 8)
+def _heads(t, T, heads, dim) -> int:
+    """Elements from one token of a bf16 [T, heads, dim] to the next: any number, heads one behind the other."""
+    assert t.dtype is _BF16 and t.is_cuda and t.shape == (T, heads, dim)
+    if t.is_contiguous():
+        return heads * dim
+    token, head, feature = t.stride()
+    assert (feature == 1 or dim == 1) and (head == dim or heads == 1)
+    return token if T > 1 else max(token, heads * dim)
 
 
 def _cache(k_cache, v_cache) -> bytes:
     """The description of a paged cache: keys [pages, heads, head_dim / 8, page, 8], values [pages, heads, page / 8,
     head_dim, 8]."""
     pages, heads, octets, page, eight = k_cache.shape
-    assert eight == 8 and _device_array(k_cache, torch.bfloat16)
-    assert _device_array(v_cache, torch.bfloat16, (pages, heads, page // 8, octets * 8, 8))
-    return _KV_CACHE.pack(pages, page, heads, octets * 8, k_cache.data_ptr(), v_cache.data_ptr())
+    assert eight == 8
+    return _KV_CACHE.pack(pages, page, heads, octets * 8, _address(k_cache, _BF16, pages, heads, octets, page, 8),
+                          _address(v_cache, _BF16, pages, heads, page // 8, octets * 8, 8))
 
 
 def qblora_page_tables(context: torch.Tensor, fresh: torch.Tensor, page: int, free_pages: torch.Tensor, table: torch.Tensor,
@@ -621,22 +627,25 @@ def qblora_page_tables(context: torch.Tensor, fresh: torch.Tensor, page: int, fr
     """Adds a step's pages to the block table (in place) and returns (starts, positions, slots, taken) of its new tokens;
     `tokens`: the room for them."""
     n, width = table.shape
+    n_free = free_pages.shape[0]
     dev = table.device
-    assert all(_device_array(t, torch.int32) for t in (context, fresh, free_pages, table))
-    assert context.shape == (n,) and fresh.shape == (n,)
-    if starts is None:
-        starts = torch.empty(n + 1, dtype=torch.int32, device=dev)
-    if positions is None:
-        positions = torch.empty(tokens, dtype=torch.int32, device=dev)
+    if starts is None and positions is None and taken is None:           # one allocation for the three of a type
+        starts, positions, taken = torch.empty(n + tokens + 2, dtype=_I32, device=dev).split_with_sizes((n + 1, tokens, 1))
+        p_starts = starts.data_ptr()
+        p_positions, p_taken = p_starts + 4 * (n + 1), p_starts + 4 * (n + 1 + tokens)
+    else:
+        starts = torch.empty(n + 1, dtype=_I32, device=dev) if starts is None else starts
+        positions = torch.empty(tokens, dtype=_I32, device=dev) if positions is None else positions
+        taken = torch.empty(1, dtype=_I32, device=dev) if taken is None else taken
+        p_starts, p_positions, p_taken = (_address(starts, _I32, n + 1), _address(positions, _I32, tokens),
+                                          _address(taken, _I32, 1))
     if slots is None:
-        slots = torch.empty(tokens, dtype=torch.int64, device=dev)
-    if taken is None:
-        taken = torch.empty(1, dtype=torch.int32, device=dev)
-    assert _device_array(starts, torch.int32, (n + 1,)) and _device_array(positions, torch.int32, (tokens,))
-    assert _device_array(slots, torch.int64, (tokens,)) and _device_array(taken, torch.int32, (1,))
-    rc = lib().qblora_page_tables(_ptr(context), _ptr(fresh), n, page, _ptr(free_pages), free_pages.numel(), _ptr(table),
-                                  width, tokens, _ptr(starts), _ptr(positions), _ptr(slots), _ptr(taken), _stream())
-    _check(rc, "qblora_page_tables")
+        slots = torch.empty(tokens, dtype=_I64, device=dev)
+    rc = lib().qblora_page_tables(_address(context, _I32, n), _address(fresh, _I32, n), n, page,
+                                  _address(free_pages, _I32, n_free), n_free, _address(table, _I32, n, width), width, tokens,
+                                  p_starts, p_positions, _address(slots, _I64, tokens), p_taken, _stream())
+    if rc:
+        _check(rc, "qblora_page_tables")
     return starts, positions, slots, taken
 
 
@@ -652,27 +661,32 @@ def qblora_rope_frequencies(rot: int, base: float = 10000.0, kind: int = ROPE_PL
 
 
 def _rope(freq, interleaved, scale) -> bytes:
-    assert _device_array(freq, torch.float32) and freq.dim() == 1
-    return _ROPE.pack(2 * freq.numel(), int(interleaved), scale, freq.data_ptr())
+    half, = freq.shape
+    return _ROPE.pack(2 * half, interleaved, scale, _address(freq, _F32, half))
 
 
 def _rope_call(name, q, k, positions, freq, interleaved, scale, q_out, k_out):
     T, heads, dim = q.shape
-    assert _heads(q) and _device_array(positions, torch.int32, (T,))
+    ldq, ld_out = _heads(q, T, heads, dim), heads * dim
     if q_out is None:
-        q_out = torch.empty((T, heads, dim), dtype=torch.bfloat16, device=q.device)
-    assert _heads(q_out) and q_out.shape == q.shape
-    ldk = ldk_out = kv_heads = 0
-    if k is not None:
+        q_out = torch.empty((T, heads, dim), dtype=_BF16, device=q.device)
+    else:
+        ld_out = _heads(q_out, T, heads, dim)
+    if k is None:
+        kv_heads = ldk = ldk_out = p_k = p_k_out = 0
+        k_out = None
+    else:
         kv_heads = k.shape[1]
-        assert _heads(k) and k.shape == (T, kv_heads, dim)
+        ldk, ldk_out = _heads(k, T, kv_heads, dim), kv_heads * dim
         if k_out is None:
-            k_out = torch.empty((T, kv_heads, dim), dtype=torch.bfloat16, device=q.device)
-        assert _heads(k_out) and k_out.shape == k.shape
-        ldk, ldk_out = _token_stride(k), _token_stride(k_out)
-    rc = getattr(lib(), name)(_rope(freq, interleaved, scale), _ptr(q), _token_stride(q), heads, _ptr(k), ldk, kv_heads, dim,
-                              _ptr(positions), T, _ptr(q_out), _token_stride(q_out), _ptr(k_out), ldk_out, _stream())
-    _check(rc, name)
+            k_out = torch.empty((T, kv_heads, dim), dtype=_BF16, device=q.device)
+        else:
+            ldk_out = _heads(k_out, T, kv_heads, dim)
+        p_k, p_k_out = k.data_ptr(), k_out.data_ptr()
+    rc = getattr(lib(), name)(_rope(freq, interleaved, scale), q.data_ptr(), ldq, heads, p_k, ldk, kv_heads, dim,
+                              _address(positions, _I32, T), T, q_out.data_ptr(), ld_out, p_k_out, ldk_out, _stream())
+    if rc:
+        _check(rc, name)
     return q_out, k_out
 
 
@@ -693,17 +707,19 @@ def qblora_rope_cache(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positio
                       scale: float = 1.0, q_out: torch.Tensor = None):
     """The rotated q; the rotated k and v go to their slots of the paged cache."""
     T, heads, dim = q.shape
-    cache = _cache(k_cache, v_cache)
-    assert _heads(q) and _heads(k) and _heads(v)
-    assert dim == v_cache.shape[3] and k.shape == v.shape == (T, k_cache.shape[1], dim)
-    assert _device_array(positions, torch.int32, (T,)) and _device_array(slots, torch.int64, (T,))
+    kv_heads = k_cache.shape[1]
+    assert dim == 8 * k_cache.shape[2]
+    ldq, ld_out = _heads(q, T, heads, dim), heads * dim
     if q_out is None:
-        q_out = torch.empty((T, heads, dim), dtype=torch.bfloat16, device=q.device)
-    assert _heads(q_out) and q_out.shape == q.shape
-    rc = lib().qblora_rope_cache(_rope(freq, interleaved, scale), _ptr(q), _token_stride(q), heads, _ptr(k), _token_stride(k),
-                                 _ptr(v), _token_stride(v), _ptr(positions), _ptr(slots), T, _ptr(q_out),
-                                 _token_stride(q_out), cache, _stream())
-    _check(rc, "qblora_rope_cache")
+        q_out = torch.empty((T, heads, dim), dtype=_BF16, device=q.device)
+    else:
+        ld_out = _heads(q_out, T, heads, dim)
+    rc = lib().qblora_rope_cache(_rope(freq, interleaved, scale), q.data_ptr(), ldq, heads, k.data_ptr(),
+                                 _heads(k, T, kv_heads, dim), v.data_ptr(), _heads(v, T, kv_heads, dim),
+                                 _address(positions, _I32, T), _address(slots, _I64, T), T, q_out.data_ptr(), ld_out,
+                                 _cache(k_cache, v_cache), _stream())
+    if rc:
+        _check(rc, "qblora_rope_cache")
     return q_out
 
 
@@ -718,20 +734,28 @@ def qblora_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torc
     tokens of a request, as far as it is known (default: T)."""
     T, heads, dim = q.shape
     n, width = table.shape
+    assert dim == 8 * k_cache.shape[2]
     cache = _cache(k_cache, v_cache)
-    assert _heads(q) and dim == v_cache.shape[3] and _device_array(table, torch.int32)
-    assert _device_array(starts, torch.int32, (n + 1,)) and _device_array(context, torch.int32, (n,))
+    ldq, ld_out = _heads(q, T, heads, dim), heads * dim
     if max_new is None:
         max_new = T
+    dev = q.device
     if out is None:
-        out = torch.empty((T, heads, dim), dtype=torch.bfloat16, device=q.device)
-    assert _heads(out) and out.shape == q.shape
-    assert lse is None or _device_array(lse, torch.float32, (T, heads))
-    ws = _workspace(lambda: lib().qblora_paged_attention_workspace_bytes(cache, heads, max_new), q.device, workspace)
-    rc = lib().qblora_paged_attention(_ptr(q), _token_stride(q), heads, cache, _ptr(table), width, _ptr(starts), _ptr(context),
-                                      n, T, scale, window, max_new, _ptr(out), _token_stride(out), _ptr(lse), _ptr(ws),
-                                      ws.numel() * ws.element_size(), _stream())
-    _check(rc, "qblora_paged_attention")
+        out = torch.empty((T, heads, dim), dtype=_BF16, device=dev)
+    else:
+        ld_out = _heads(out, T, heads, dim)
+    L = lib()
+    if workspace is None:
+        nbytes = L.qblora_paged_attention_workspace_bytes(cache, heads, max_new)
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    rc = L.qblora_paged_attention(q.data_ptr(), ldq, heads, cache, _address(table, _I32, n, width), width,
+                                  _address(starts, _I32, n + 1), _address(context, _I32, n), n, T, scale, window, max_new,
+                                  out.data_ptr(), ld_out, None if lse is None else _address(lse, _F32, T, heads),
+                                  workspace.data_ptr(), nbytes, _stream())
+    if rc:
+        _check(rc, "qblora_paged_attention")
     return out
 
 
@@ -740,20 +764,19 @@ def qblora_rms_norm_fwd(x: torch.Tensor, w: torch.Tensor, eps: float, residual: 
     """(y, total, rstd): the norm of total = x + residual (x itself without one); rstd, for the backward pass, is None unless
     `keep` is set or a tensor is given."""
     T, d = x.shape
-    assert _device_array(x, torch.bfloat16) and _device_array(w, torch.bfloat16, (d,))
-    assert residual is None or _device_array(residual, torch.bfloat16, (T, d))
-    if y is None:
-        y = torch.empty_like(x)
+    p_x, p_residual = _address(x, _BF16, T, d), None
+    y = torch.empty_like(x) if y is None else y
     if residual is None:
         total = x
-    elif total is None:
-        total = torch.empty_like(x)
+    else:
+        p_residual = _address(residual, _BF16, T, d)
+        total = torch.empty_like(x) if total is None else total
     if keep and rstd is None:
-        rstd = torch.empty(T, dtype=torch.float32, device=x.device)
-    assert _device_array(y, torch.bfloat16, (T, d)) and _device_array(total, torch.bfloat16, (T, d))
-    assert rstd is None or _device_array(rstd, torch.float32, (T,))
-    rc = lib().qblora_rms_norm_fwd(_ptr(x), _ptr(residual), _ptr(w), T, d, eps, _ptr(total), _ptr(y), _ptr(rstd), _stream())
-    _check(rc, "qblora_rms_norm_fwd")
+        rstd = torch.empty(T, dtype=_F32, device=x.device)
+    rc = lib().qblora_rms_norm_fwd(p_x, p_residual, _address(w, _BF16, d), T, d, eps, _address(total, _BF16, T, d),
+                                   _address(y, _BF16, T, d), None if rstd is None else _address(rstd, _F32, T), _stream())
+    if rc:
+        _check(rc, "qblora_rms_norm_fwd")
     return y, total, rstd
 
 
@@ -767,19 +790,17 @@ def qblora_rms_norm_bwd(total: torch.Tensor, w: torch.Tensor, rstd: torch.Tensor
     """(dx, dw): the gradients of the sum (x and residual alike) and of the weight."""
     T, d = total.shape
     dev = total.device
-    assert _device_array(total, torch.bfloat16) and _device_array(w, torch.bfloat16, (d,))
-    assert _device_array(rstd, torch.float32, (T,)) and _device_array(dy, torch.bfloat16, (T, d))
-    assert dtotal is None or _device_array(dtotal, torch.bfloat16, (T, d))
-    if dx is None:
-        dx = torch.empty((T, d), dtype=torch.bfloat16, device=dev)
-    if need_dw and dw is None:
-        dw = torch.empty(d, dtype=torch.float32, device=dev)
-    assert _device_array(dx, torch.bfloat16, (T, d)) and (dw is None or _device_array(dw, torch.float32, (d,)))
-    ws, nbytes = None, 0
+    p_total = _address(total, _BF16, T, d)
+    dx = torch.empty((T, d), dtype=_BF16, device=dev) if dx is None else dx
+    p_dw = ws = None
+    nbytes = 0
     if need_dw:
+        dw = torch.empty(d, dtype=_F32, device=dev) if dw is None else dw
+        p_dw = _address(dw, _F32, d)
         ws = _workspace(lambda: lib().qblora_rms_norm_bwd_workspace_bytes(T, d), dev, workspace)
         nbytes = ws.numel() * ws.element_size()
-    rc = lib().qblora_rms_norm_bwd(_ptr(total), _ptr(w), _ptr(rstd), _ptr(dy), _ptr(dtotal), T, d, _ptr(dx),
-                                   _ptr(dw if need_dw else None), _ptr(ws), nbytes, _stream())
+    rc = lib().qblora_rms_norm_bwd(p_total, _address(w, _BF16, d), _address(rstd, _F32, T), _address(dy, _BF16, T, d),
+                                   None if dtotal is None else _address(dtotal, _BF16, T, d), T, d, _address(dx, _BF16, T, d),
+                                   p_dw, _ptr(ws), nbytes, _stream())
     _check(rc, "qblora_rms_norm_bwd")
     return dx, (dw if need_dw else None)

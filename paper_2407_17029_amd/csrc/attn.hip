@@ -6,13 +6,13 @@
 // A row is a query head of a new token; the rows of one request that share a key / value head go together, token by token
 // (row r: token r / group, head r % group of the group), so that the cache is read once for all of them.
 //
-// k_attn_few takes 16 rows, the width of the matrix instruction, and is bound by the stream of the cache: a wave takes 32
+// attend_few takes 16 rows, the width of the matrix instruction, and is bound by the stream of the cache: a wave takes 32
 // positions at a time straight from the pages into registers, in the operand order that the cache is stored in, with the
 // next 32 in flight behind them.  Scores are formed transposed, S^T = K Q^T, so that a lane holds eight consecutive positions
 // of one row: that is the operand of O^T = V^T P^T as it stands.  The four waves of a workgroup take turns on the positions
 // and are joined in LDS.
 //
-// k_attn_many takes 128 rows, 32 a wave, and is bound by the matrix pipe and by the exponentials beside it.  64 positions at a
+// attend_many takes 128 rows, 32 a wave, and is bound by the matrix pipe and by the exponentials beside it.  64 positions at a
 // time go through LDS, in the order of the pages (copies of 1 KB that need no registers, two tiles in turn, one barrier a
 // tile); scores are transposed here too, so that a row's maximum and sum are a lane's own but for one exchange of halves.
 //
@@ -21,6 +21,7 @@
 // its own (request, rows, range of positions) from the prefix sums.  A context that is cut this way leaves partial results
 // in the workspace, which k_attn_join adds up.
 #include <climits>
+#include <type_traits>
 
 #include "decoder.h"
 
@@ -35,18 +36,31 @@ constexpr int kManyRows = 128;
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kSlack = 8.0f;                 // a maximum may grow by 2^8 before what was summed is rescaled
 
-// Which requests a kernel takes, by their rows, and how it shares their work out: units of `rows` rows, `target` workgroups
-// a key / value head, at least `least` blocks each.
-struct Share { int rows, target, least; int64_t over, upto; float* part; };
+// Which requests a form takes, by their rows, and how their work is shared out: units of `rows` rows, about `target` of them
+// for a key / value head, at least `least` blocks each.  Tiles that are cut leave their parts in `part` and themselves in
+// `cut`, `cuts` counts those.
+struct CutTile { int token0, rem0, rows, splits, slot, pad[3]; };
+struct Share { int rows, target, least; int64_t over, upto; int* cuts; CutTile* cut; float* part; };
 constexpr int kFewTarget = 1024, kFewLeast = 8;
 constexpr int kManyTarget = 512, kManyLeast = 16;
+static_assert(2 * kFewTarget < 1 << 15 && 2 * kManyTarget < 1 << 15, "parts and cut tiles are counted in halves of a word");
 
-struct Unit { int request, tile, split, splits, slot; };
+// A workgroup's rows and range of positions; slot: its place among the parts, cut: its tile's among those that are cut
+// x / group for x < 128 + group: the magic number is 2^32 / group + 1, whose excess is less than x * group / 2^32 < 1
+__device__ __forceinline__ int quotient(const AttnDesc& d, int x) { return d.group == 1 ? x : (int)__umulhi((uint32_t)x, d.group_magic); }
+
+struct Unit { int request, tile, split, splits, slot, cut; };
 
 struct Span { int start, fresh, context; };
 __device__ __forceinline__ Span span_of(const AttnDesc& d, int i) {
     const int s0 = min(max(d.starts[i], 0), d.T), s1 = min(max(d.starts[i + 1], s0), d.T);
     return {s0, s1 - s0, min(max(d.context[i], 0), 1 << 30)};
+}
+
+// of a request that the whole wave works on
+__device__ __forceinline__ Span uniform_span_of(const AttnDesc& d, int i) {
+    const Span s = span_of(d, i);
+    return {__builtin_amdgcn_readfirstlane(s.start), __builtin_amdgcn_readfirstlane(s.fresh), __builtin_amdgcn_readfirstlane(s.context)};
 }
 
 struct Cost { int tiles, blocks; };
@@ -60,87 +74,139 @@ __device__ __forceinline__ Cost cost_of(const AttnDesc& d, int i, const Share& w
     return {(int)((rows + w.rows - 1) / w.rows), blocks};
 }
 
-// The work of workgroup unit `want` (units counted over requests, tiles and splits, or with `joins` over the tiles of split
-// requests alone); false: there is none.  All threads call it.
+// sum over the lanes up to this one
+__device__ __forceinline__ int scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);    // from 1, 2, 4 and 8 lanes before, in rows of 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);    // the last lane of a row to the next one
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);    // lane 31 to the upper half
+    return x;
+}
+__device__ __forceinline__ int64_t sum_of_wave(int64_t x) {
+    if (__all((uint64_t)x < 1u << 25)) return __builtin_amdgcn_readlane(scan((int)x), 63);
+    for (int s = 32; s; s >>= 1) x += __shfl_xor(x, s);
+    return x;
+}
+
+// Blocks of a unit, from the blocks of all tiles
+__device__ __forceinline__ int64_t blocks_per_unit(int64_t all, const Share& w) {
+    const int64_t per = all >> 32 ? (all + w.target - 1) / w.target : (int64_t)(((uint32_t)all + (uint64_t)w.target - 1) >> 32 ? (all + w.target - 1) / w.target
+                                                                                  : ((uint32_t)all + w.target - 1) / (uint32_t)w.target);
+    return max(per, (int64_t)w.least);
+}
+struct Units { int tiles, splits, count, cuts; };                      // cuts: parts, and cut tiles in the upper half
+__device__ __forceinline__ Units units_of(const Cost& c, int64_t per) {
+    Units u;
+    u.tiles = c.tiles;
+    u.splits = c.blocks > per ? (int)((uint32_t)(c.blocks - 1) / (uint32_t)per) + 1 : 1;
+    u.count = u.tiles * u.splits;
+    u.cuts = u.splits > 1 ? u.count + (u.tiles << 16) : 0;
+    return u;
+}
+
+// The unit number `want` of the batch; false: there are not so many.  With `first`, the number of cut tiles is left where
+// k_attn_join looks for it.  All threads call it.  Up to 64 requests every wave finds it by itself, a request a lane; more
+// are taken 256 at a time.
 struct Finder {
-    int64_t sums[kWaves], ends[2][kWaves];
-    int found[5];
+    int64_t sums[kWaves];
+    int ends[2][kWaves], found[6];
 };
-__device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share, bool joins, int64_t want, Finder& f, Unit& u) {
+__device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share, int want, bool first, Finder& f, Unit& u) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (d.n <= 64) {
+        Cost c{0, 0};
+        if (lane < d.n) c = cost_of(d, lane, share);
+        const Units v = units_of(c, blocks_per_unit(sum_of_wave((int64_t)c.tiles * c.blocks), share));
+        const int a = scan(v.count), b = scan(v.cuts);
+        if (first && tid == 63) *share.cuts = b >> 16;
+        const uint64_t hit = __ballot(v.count && a - v.count <= want && want < a);
+        if (!hit) return false;
+        const int at = __builtin_ctzll(hit);
+        const int count = __builtin_amdgcn_readlane(v.count, at), number = want - (__builtin_amdgcn_readlane(a, at) - count);
+        const int before = __builtin_amdgcn_readlane(b - v.cuts, at);
+        u.request = at;
+        u.splits = __builtin_amdgcn_readlane(v.splits, at);
+        u.tile = number / u.splits;
+        u.split = number - u.tile * u.splits;
+        u.slot = (before & 0xffff) + number;
+        u.cut = (before >> 16) + u.tile;
+        return true;
+    }
     int64_t all = 0;
     for (int i = tid; i < d.n; i += kThreads) {
         const Cost c = cost_of(d, i, share);
         all += (int64_t)c.tiles * c.blocks;
     }
-    for (int s = 32; s; s >>= 1) all += __shfl_xor(all, s);
+    all = sum_of_wave(all);
     if (lane == 0) f.sums[wave] = all;
     if (tid == 0) f.found[0] = -1;
     __syncthreads();
     all = 0;
     for (int w = 0; w < kWaves; ++w) all += f.sums[w];
-    const int64_t per = max((all + share.target - 1) / share.target, (int64_t)share.least);       // blocks of a workgroup
-    int64_t units = 0, slots = 0;                                               // in front of this round's requests
+    const int64_t per = blocks_per_unit(all, share);
+    int units = 0, cuts = 0;                                           // in front of these 256 requests
     for (int base = 0; base < d.n; base += kThreads) {
         const int i = base + tid;
-        int64_t mine = 0, cut = 0;
-        int tiles = 0, splits = 1;
-        if (i < d.n) {
-            const Cost c = cost_of(d, i, share);
-            tiles = c.tiles;
-            splits = (int)((c.blocks + per - 1) / per);
-            cut = splits > 1 ? (int64_t)tiles * splits : 0;
-            mine = joins ? (splits > 1 ? tiles : 0) : (int64_t)tiles * splits;
-        }
-        int64_t a = mine, b = cut;
-        for (int s = 1; s < 64; s <<= 1) {
-            const int64_t x = __shfl_up(a, s), y = __shfl_up(b, s);
-            if (lane >= s) { a += x; b += y; }
-        }
+        Cost c{0, 0};
+        if (i < d.n) c = cost_of(d, i, share);
+        const Units v = units_of(c, per);
+        int a = scan(v.count), b = scan(v.cuts);
         __syncthreads();
         if (lane == 63) { f.ends[0][wave] = a; f.ends[1][wave] = b; }
         __syncthreads();
-        int64_t u0 = units, s0 = slots;
         for (int w = 0; w < kWaves; ++w) {
-            if (w == wave) { a += u0; b += s0; }
-            u0 += f.ends[0][w];
-            s0 += f.ends[1][w];
+            if (w == wave) { a += units; b += cuts; }
+            units += f.ends[0][w];
+            cuts += f.ends[1][w];
         }
-        units = u0;
-        slots = s0;
-        if (mine && a - mine <= want && want < a) {
-            const int at = (int)(want - (a - mine));
+        if (v.count && a - v.count <= want && want < a) {
+            const int number = want - (a - v.count), before = b - v.cuts;
             f.found[0] = i;
-            f.found[1] = joins ? at : at / splits;
-            f.found[2] = joins ? 0 : at % splits;
-            f.found[3] = splits;
-            f.found[4] = (int)(b - cut) + (joins ? at * splits : at);
+            f.found[1] = number / v.splits;
+            f.found[2] = number % v.splits;
+            f.found[3] = v.splits;
+            f.found[4] = (before & 0xffff) + number;
+            f.found[5] = (before >> 16) + number / v.splits;
         }
         __syncthreads();
-        if (f.found[0] >= 0) break;
+        if (f.found[0] >= 0 && !first) break;
     }
+    if (first && tid == 0) *share.cuts = cuts >> 16;
     u.request = __builtin_amdgcn_readfirstlane(f.found[0]);
     if (u.request < 0) return false;
     u.tile = __builtin_amdgcn_readfirstlane(f.found[1]);
     u.split = __builtin_amdgcn_readfirstlane(f.found[2]);
     u.splits = __builtin_amdgcn_readfirstlane(f.found[3]);
     u.slot = __builtin_amdgcn_readfirstlane(f.found[4]);
+    u.cut = __builtin_amdgcn_readfirstlane(f.found[5]);
     return true;
 }
 
-// the rows of a tile and the positions that any of them sees
-struct Tile { int row0, rows, pos0, pos1, full0, full1; };       // full: positions that every row sees, as far as lengths go
+// the rows of a tile (row0 is row `rem0` of token `token0`) and the positions that any of them sees
+struct Tile { int row0, token0, rem0, rows, pos0, pos1, full0, full1; };       // full: positions that every row sees, as far as lengths go
 __device__ __forceinline__ Tile tile_of(const AttnDesc& d, const Span& s, int tile, int rows) {
     Tile t;
     t.row0 = tile * rows;
+    t.token0 = t.row0 / d.group;
+    t.rem0 = t.row0 - t.token0 * d.group;
     t.rows = min(rows, s.fresh * d.group - t.row0);
-    const int first = s.context + t.row0 / d.group, last = s.context + (t.row0 + t.rows - 1) / d.group;
+    const int first = s.context + t.token0, last = first + quotient(d, t.rem0 + t.rows - 1);
     const int limit = d.width << d.page_shift;
     t.pos1 = min(last + 1, limit);
     t.pos0 = d.window ? max(first + 1 - d.window, 0) : 0;
     t.full1 = min(first + 1, limit);
     t.full0 = d.window ? max(last + 1 - d.window, 0) : 0;
     return t;
+}
+
+// A cut tile goes to where k_attn_join finds it.
+__device__ __forceinline__ void note_cut(const Share& share, const Unit& u, int kvh, const Span& s, const Tile& t) {
+    if (u.splits > 1 && u.split == 0 && kvh == 0 && threadIdx.x == 0) {
+        CutTile c{s.start + t.token0, t.rem0, t.rows, u.splits, u.slot, {0, 0, 0}};
+        share.cut[u.cut] = c;
+    }
 }
 
 __device__ __forceinline__ bool not_finite(uint32_t pair) { return (((pair & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0; }
@@ -171,24 +237,23 @@ struct FewShared {
 };
 
 template <int D>
-__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_few(AttnDesc d, Share share) {
+__device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share, int block, Finder& finder, FewShared<D>& sh) {
     constexpr int KS = D / 32, DT = D / 16;
-    __shared__ Finder finder;
-    __shared__ FewShared<D> sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, col = lane & 15;
-    const int kvh = blockIdx.x % d.kv_heads;
+    const int kvh = block % d.kv_heads;
     Unit u;
-    if (!find_unit(d, share, false, blockIdx.x / d.kv_heads, finder, u)) return;
-    const Span s = span_of(d, u.request);
+    if (!find_unit(d, share, block / d.kv_heads, block == 0, finder, u)) return;
+    const Span s = uniform_span_of(d, u.request);
     const Tile t = tile_of(d, s, u.tile, kFewRows);
+    note_cut(share, u, kvh, s, t);
     const int b_first = t.pos0 / kBlock, b_last = (t.pos1 + kBlock - 1) / kBlock;
     const int per = (max(b_last - b_first, 0) + u.splits - 1) / u.splits;
     const int b0 = b_first + u.split * per, b1 = min(b0 + per, b_last);
 
     // rows: operand B, row = lane & 15, features 32 s + 8 g ..
     bf16x8 qf[KS];
-    const int row = t.row0 + col;
-    const int token = row / d.group, head = kvh * d.group + row % d.group;
+    const int among = t.rem0 + col, ahead = quotient(d, among);            // tokens behind the tile's first
+    const int token = t.token0 + ahead, head = kvh * d.group + among - ahead * d.group;
     const int here = s.context + token;
     const bool real = col < t.rows;
 #pragma unroll
@@ -356,7 +421,8 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_few(AttnDesc
             *reinterpret_cast<f32x4*>(part + r * D + f) = v;
             if (f == 0) { part[kFewRows * D + r] = top; part[kFewRows * (D + 1) + r] = sum; }
         } else {
-            const int64_t tok = s.start + (t.row0 + r) / d.group, h = kvh * d.group + (t.row0 + r) % d.group;
+            const int ahead = quotient(d, t.rem0 + r);
+            const int64_t tok = s.start + t.token0 + ahead, h = kvh * d.group + t.rem0 + r - ahead * d.group;
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
             *reinterpret_cast<uint2*>(d.out + tok * d.ldo + h * D + f) = make_uint2(pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv));
             if (f == 0 && d.lse) d.lse[tok * d.heads + h] = (top + __builtin_log2f(sum)) * 0.69314718055994530942f;
@@ -390,20 +456,26 @@ __device__ __forceinline__ float sum_of_halves(float x) {
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_many(AttnDesc d, Share share) {
+struct ManyShared {                                                    // [turn][keys, values]
+    static constexpr int kTile = D > 128 ? 32 : 64;
+    __attribute__((aligned(16))) unsigned char buf[2][2][kTile * D * 2];
+};
+
+template <int D>
+__device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& share, int block, Finder& finder, ManyShared<D>& sh) {
     // positions of a tile: 64, or 32 where the registers hold no more beside 256 features
-    constexpr int kTile = D > 128 ? 32 : 64, KS = D / 16, DT = D / 32, TT = kTile / 32, PS = kTile / 16;
+    constexpr int kTile = ManyShared<D>::kTile, KS = D / 16, DT = D / 32, TT = kTile / 32, PS = kTile / 16;
     constexpr int kTileBytes = kTile * D * 2;
     constexpr int kCopies = kTileBytes / 1024 / kWaves;                // of keys, and again of values, a wave and tile
-    __shared__ Finder finder;
-    __shared__ __attribute__((aligned(16))) unsigned char buf[2][2][kTileBytes];          // [turn][keys, values]
+    auto& buf = sh.buf;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
-    const int kvh = blockIdx.x % d.kv_heads;
+    const int kvh = block % d.kv_heads;
     Unit u;
-    if (!find_unit(d, share, false, blockIdx.x / d.kv_heads, finder, u)) return;
-    const Span s = span_of(d, u.request);
+    if (!find_unit(d, share, block / d.kv_heads, block == 0, finder, u)) return;
+    const Span s = uniform_span_of(d, u.request);
     const int tiles = (int)(((int64_t)s.fresh * d.group + kManyRows - 1) / kManyRows);
     const Tile t = tile_of(d, s, tiles - 1 - u.tile, kManyRows);       // the longest ranges first
+    note_cut(share, u, kvh, s, t);
     const int limit = d.width << d.page_shift;
     const int n_first = t.pos0 / kTile, n_last = (t.pos1 + kTile - 1) / kTile;
     const int per = (max(n_last - n_first, 0) + u.splits - 1) / u.splits;
@@ -411,10 +483,10 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_many(AttnDes
 
     // the wave's rows, and what of the positions all of them see
     const int w_rows = min(32, t.rows - 32 * wave);
-    const int row = t.row0 + 32 * wave + col, token = row / d.group, head = kvh * d.group + row % d.group;
+    const int among = t.rem0 + 32 * wave + col, ahead = quotient(d, among), token = t.token0 + ahead, head = kvh * d.group + among - ahead * d.group;
     const bool real = col < w_rows;
-    const int here = s.context + token, row_low = d.window ? here - d.window : -1;
-    const int first = s.context + (t.row0 + 32 * wave) / d.group, last = s.context + (t.row0 + 32 * wave + max(w_rows, 1) - 1) / d.group;
+    const int here = s.context + token;
+    const int first = s.context + t.token0 + quotient(d, t.rem0 + 32 * wave), last = s.context + t.token0 + quotient(d, t.rem0 + 32 * wave + max(w_rows, 1) - 1);
     const int full0 = d.window ? max(last + 1 - d.window, 0) : 0, full1 = min(first + 1, limit);
     const int see0 = d.window ? max(first + 1 - d.window, 0) : 0, see1 = w_rows > 0 ? min(last + 1, limit) : 0;
 
@@ -505,13 +577,15 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_many(AttnDes
             const bool masked = base < full0 || base + kTile > full1 || ~listed != 0;
             uint32_t seen = 0xffffffffu, any = 0xffffffffu;            // bit 8 s + j: position 16 s + 8 h + j of the tile
             if (masked) {
+                const int h8 = 8 * (int)opaque_bits((uint32_t)h);
+                const int row_low = d.window ? here - d.window : -1;
                 seen = any = 0;
 #pragma unroll
                 for (int s4 = 0; s4 < PS; ++s4) {
-                    const uint32_t here8 = (uint32_t)(listed >> (16 * s4 + 8 * h)) & 0xffu;
+                    const uint32_t half_tile = s4 < 2 ? (uint32_t)listed : (uint32_t)(listed >> 32), here8 = (half_tile >> (16 * (s4 & 1) + h8)) & 0xffu;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const int pos = base + 16 * s4 + 8 * h + j;
+                        const int pos = base + 16 * s4 + h8 + j;
                         if (pos >= see0 && pos < see1) any |= 1u << (8 * s4 + j);
                         if (pos <= here && pos > row_low) seen |= 1u << (8 * s4 + j);
                     }
@@ -574,7 +648,7 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_many(AttnDes
                     if (D > 128) __builtin_amdgcn_sched_barrier(0);
                 }
             } else {
-                // as in k_attn_few: values that no row sees are 0, and what is not finite is added behind the loop
+                // as in attend_few: values that no row sees are 0, and what is not finite is added behind the loop
                 bool odd = false;
 #pragma unroll
                 for (int s4 = 0; s4 < PS; ++s4) {
@@ -599,7 +673,8 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_many(AttnDes
     }
 
     // (the lane's row again: the loop has no registers to keep it in)
-    const int h2 = (int)opaque_bits((uint32_t)h), r = 32 * wave + (int)opaque_bits((uint32_t)col), to = (t.row0 + r) / d.group, q_head = kvh * d.group + (t.row0 + r) % d.group;
+    const int h2 = (int)opaque_bits((uint32_t)h), r = 32 * wave + (int)opaque_bits((uint32_t)col);
+    const int past = quotient(d, t.rem0 + r), to = t.token0 + past, q_head = kvh * d.group + t.rem0 + r - past * d.group;
     for (int pos = odd0; pos < min(odd1, see1); ++pos) {
         const qblora_bf16* v = value_row<D>(d, table, kvh, pos);
         if (!v || r >= t.rows || pos > s.context + to || (d.window && pos <= s.context + to - d.window)) continue;
@@ -633,29 +708,42 @@ __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn_many(AttnDes
     if (h2 == 0 && d.lse) d.lse[(int64_t)(s.start + to) * d.heads + q_head] = (m + __builtin_log2f(l)) * 0.69314718055994530942f;
 }
 
-// Adds up the partial results of a split tile, weights 2^(m - max m): a workgroup takes every gridDim.y-th row, four
-// features a thread, and what threads are left over share the parts.
-template <int D, int ROWS, bool LAST_FIRST>
-__global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share share) {
-    constexpr int kQuads = D / 4, kGroups = kThreads / kQuads, kMost = kFewTarget;
+// One of the forms, or both, so that chunks and single tokens of a batch run beside each other.
+enum { FEW = 1, LOT = 2, BOTH = 3 };
+template <int D, int FORMS>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn(AttnDesc d, Share lot, Share few, int lot_blocks) {
     __shared__ Finder finder;
-    __shared__ float weight[kMost];
+    __shared__ union Shared {
+        std::conditional_t<(FORMS & LOT) != 0, ManyShared<D>, char> many;
+        std::conditional_t<(FORMS & FEW) != 0, FewShared<D>, char> few;
+    } sh;
+    if constexpr ((FORMS & LOT) != 0) {
+        if (FORMS == LOT || (int)blockIdx.x < lot_blocks) return attend_many<D>(d, lot, blockIdx.x, finder, sh.many);
+    }
+    if constexpr ((FORMS & FEW) != 0) attend_few<D>(d, few, blockIdx.x - (FORMS & LOT ? lot_blocks : 0), finder, sh.few);
+}
+
+// Adds up the parts of a cut tile, weights 2^(m - max m): a workgroup takes every gridDim.y-th row, four features a thread,
+// and what threads are left over share the parts.
+template <int D>
+__global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share lot, Share few, int lot_blocks) {
+    constexpr int kQuads = D / 4, kGroups = kThreads / kQuads;
+    __shared__ float weight[kFewTarget + 1];
     __shared__ float top_of[kWaves], sum_of[kWaves];
     __shared__ f32x4 sums[kGroups][kQuads];
+    const bool of_lot = (int)blockIdx.x < lot_blocks;
+    const Share& share = of_lot ? lot : few;
+    const int block = blockIdx.x - (of_lot ? 0 : lot_blocks), kvh = block % d.kv_heads, number = block / d.kv_heads;
+    if (number >= *share.cuts) return;
+    const CutTile t = share.cut[number];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, quad = tid % kQuads, grp = tid / kQuads;
-    const int kvh = blockIdx.x % d.kv_heads;
-    Unit u;
-    if (!find_unit(d, share, true, blockIdx.x / d.kv_heads, finder, u)) return;
-    const Span s = span_of(d, u.request);
-    const int tiles = (int)(((int64_t)s.fresh * d.group + ROWS - 1) / ROWS);
-    const Tile t = tile_of(d, s, LAST_FIRST ? tiles - 1 - u.tile : u.tile, ROWS);
-    constexpr int64_t kPart = ROWS * (D + 2);
-    const int64_t step = kPart * d.kv_heads;
-    const float* part = share.part + ((int64_t)u.slot * d.kv_heads + kvh) * kPart;
+    const int rows = share.rows, part_floats = rows * (D + 2);
+    const int64_t step = (int64_t)part_floats * d.kv_heads;
+    const float* part = share.part + ((int64_t)t.slot * d.kv_heads + kvh) * part_floats;
     for (int r = blockIdx.y; r < t.rows; r += gridDim.y) {
         float top = kNegInf;
-        for (int k = tid; k < u.splits; k += kThreads) {
-            weight[k] = part[k * step + ROWS * D + r];
+        for (int k = tid; k < t.splits; k += kThreads) {
+            weight[k] = part[k * step + rows * D + r];
             top = fmaxf(top, weight[k]);
         }
         for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
@@ -664,9 +752,9 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share share)
         top = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
         const float use = top == kNegInf ? 0.0f : top;
         float sum = 0.0f;
-        for (int k = tid; k < u.splits; k += kThreads) {
+        for (int k = tid; k < t.splits; k += kThreads) {
             weight[k] = exp2_of(weight[k] - use);
-            sum = __fmaf_rn(part[k * step + ROWS * (D + 1) + r], weight[k], sum);
+            sum = __fmaf_rn(part[k * step + rows * (D + 1) + r], weight[k], sum);
         }
         for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x);
         if (lane == 0) sum_of[wave] = sum;
@@ -674,7 +762,7 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share share)
         sum = (sum_of[0] + sum_of[1]) + (sum_of[2] + sum_of[3]);
         f32x4 v = {0, 0, 0, 0};
 #pragma unroll 4
-        for (int k = grp; k < u.splits; k += kGroups) {
+        for (int k = grp; k < t.splits; k += kGroups) {
             const float a = weight[k];
             const f32x4 x = *reinterpret_cast<const f32x4*>(part + k * step + r * D + 4 * quad);
             for (int j = 0; j < 4; ++j) v[j] = __fmaf_rn(x[j], a, v[j]);
@@ -683,7 +771,8 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share share)
         __syncthreads();
         if (grp == 0) {
             for (int g = 1; g < kGroups; ++g) v += sums[g][quad];
-            const int64_t tok = s.start + (t.row0 + r) / d.group, h = kvh * d.group + (t.row0 + r) % d.group;
+            const int ahead = quotient(d, t.rem0 + r);
+            const int64_t tok = t.token0 + ahead, h = kvh * d.group + t.rem0 + r - ahead * d.group;
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
             *reinterpret_cast<uint2*>(d.out + tok * d.ldo + h * D + 4 * quad) =
                 make_uint2(pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv));
@@ -695,36 +784,77 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share share)
 
 // `target` counts workgroups over all key / value heads
 int target_of(int target, int kv_heads) { return (target + kv_heads - 1) / kv_heads; }
-size_t part_floats(int target, int kv_heads, int rows, int head_dim) {
-    return (size_t)2 * target_of(target, kv_heads) * kv_heads * rows * (head_dim + 2);
-}
 // More rows than this in a request, if the caller knows of any, and they go through LDS.
 bool many_rows(int group, int max_new) { return (int64_t)group * max_new > kFewRows; }
+
+// The workspace: counts, the cut tiles of both forms, their parts (at most two for each unit of the target: what is cut is
+// longer than a unit).
+struct Space {
+    size_t bytes = 0;
+    char* base;
+    explicit Space(void* p) : base(static_cast<char*>(p)) {}
+    template <typename T>
+    T* take(size_t count) {
+        T* r = reinterpret_cast<T*>(base + bytes);
+        bytes += (count * sizeof(T) + 255) / 256 * 256;
+        return r;
+    }
+};
+void lay_out(Space& space, int kv_heads, int head_dim, bool many, Share& lot, Share& few) {
+    int* cuts = space.take<int>(64);
+    few.cuts = cuts;
+    lot.cuts = cuts + 1;
+    few.cut = space.take<CutTile>(few.target);
+    few.part = space.take<float>((size_t)2 * few.target * kv_heads * kFewRows * (head_dim + 2));
+    if (!many) return;
+    lot.cut = space.take<CutTile>(lot.target);
+    lot.part = space.take<float>((size_t)2 * lot.target * kv_heads * kManyRows * (head_dim + 2));
+}
+Share few_share(int kv_heads, bool many) {
+    return Share{kFewRows, target_of(kFewTarget, kv_heads), kFewLeast, 0, many ? (int64_t)kFewRows : INT64_MAX, nullptr, nullptr, nullptr};
+}
+Share lot_share(int kv_heads) {
+    return Share{kManyRows, target_of(kManyTarget, kv_heads), kManyLeast, kFewRows, INT64_MAX, nullptr, nullptr, nullptr};
+}
 
 template <int D>
 int launch(const AttnDesc& d, hipStream_t st) {
     const bool many = many_rows(d.group, d.max_new);
-    Share few{kFewRows, target_of(kFewTarget, d.kv_heads), kFewLeast, 0, many ? (int64_t)kFewRows : INT64_MAX, d.part};
-    const int64_t few_tiles = many ? d.n : (int64_t)d.T * d.group / kFewRows + d.n, few_grid = (few_tiles + few.target) * d.kv_heads;
-    Share lot{kManyRows, target_of(kManyTarget, d.kv_heads), kManyLeast, kFewRows, INT64_MAX,
-              d.part + part_floats(kFewTarget, d.kv_heads, kFewRows, D)};
-    const int64_t lot_tiles = (int64_t)d.T * d.group / kManyRows + d.n, lot_grid = (lot_tiles + lot.target) * d.kv_heads;
-    if (few_grid > INT32_MAX || lot_grid > INT32_MAX) return QBLORA_ERR_UNSUPPORTED;
-    const auto least = [&](int64_t tiles, const Share& w) { return (unsigned)((tiles < w.target ? tiles : w.target) * d.kv_heads); };
-    if (many) hipLaunchKernelGGL(k_attn_many<D>, dim3((unsigned)lot_grid), dim3(kThreads), 0, st, d, lot);
-    hipLaunchKernelGGL(k_attn_few<D>, dim3((unsigned)few_grid), dim3(kThreads), 0, st, d, few);
-    if (many) hipLaunchKernelGGL((k_attn_join<D, kManyRows, true>), dim3(least(lot_tiles, lot), 16), dim3(kThreads), 0, st, d, lot);
-    hipLaunchKernelGGL((k_attn_join<D, kFewRows, false>), dim3(least(few_tiles, few), d.group < kFewRows ? d.group : kFewRows), dim3(kThreads),
-                       0, st, d, few);
+    Share few = few_share(d.kv_heads, many), lot = lot_share(d.kv_heads);
+    Space space(d.part);
+    lay_out(space, d.kv_heads, D, many, lot, few);
+    const int64_t few_tiles = many ? d.n : (int64_t)d.T * d.group / kFewRows + d.n;
+    const int64_t lot_tiles = many ? (int64_t)d.T * d.group / kManyRows + d.n : 0;
+    const int64_t lot_blocks = many ? (lot_tiles + lot.target) * d.kv_heads : 0, blocks = lot_blocks + (few_tiles + few.target) * d.kv_heads;
+    if (blocks > INT32_MAX) return QBLORA_ERR_UNSUPPORTED;
+    const auto go = [&](auto kernel, int64_t count) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(kThreads), 0, st, d, lot, few, (int)lot_blocks);
+    };
+    if (!many) {
+        go(k_attn<D, FEW>, blocks);
+    } else if constexpr (D <= 128) {
+        go(k_attn<D, BOTH>, blocks);
+    } else {                                                           // (one kernel of both would not have the registers)
+        go(k_attn<D, LOT>, lot_blocks);
+        go(k_attn<D, FEW>, blocks - lot_blocks);
+    }
+    // no context is long enough for a cut
+    if ((int64_t)d.width << d.page_shift <= kFewLeast * kBlock) return launch_status();
+    const int64_t lot_cuts = (lot_tiles < lot.target ? lot_tiles : lot.target) * d.kv_heads;
+    const int64_t few_cuts = (few_tiles < few.target ? few_tiles : few.target) * d.kv_heads;
+    hipLaunchKernelGGL(k_attn_join<D>, dim3((unsigned)(lot_cuts + few_cuts), many || d.group > kFewRows ? kFewRows : d.group), dim3(kThreads), 0, st,
+                       d, lot, few, (int)lot_cuts);
     return launch_status();
 }
 
 }  // namespace
 
 size_t attention_part_bytes(int head_dim, int kv_heads, int group, int max_new) {
-    size_t floats = part_floats(kFewTarget, kv_heads, kFewRows, head_dim);
-    if (many_rows(group, max_new)) floats += part_floats(kManyTarget, kv_heads, kManyRows, head_dim);
-    return floats * sizeof(float);
+    const bool many = many_rows(group, max_new);
+    Share few = few_share(kv_heads, many), lot = lot_share(kv_heads);
+    Space space(nullptr);
+    lay_out(space, kv_heads, head_dim, many, lot, few);
+    return space.bytes;
 }
 
 int launch_attention(const AttnDesc& d, hipStream_t st) {

@@ -51,6 +51,7 @@ int launch_rms_norm_bwd(const NormBackDesc& d, hipStream_t st);
 
 struct AttnDesc {
     const qblora_bf16* q; int64_t ldq; int heads, kv_heads, group;          // group: query heads per key / value head
+    uint32_t group_magic;                                                    // 2^32 / group + 1
     const qblora_bf16* kc; const qblora_bf16* vc; int pages, page_shift, head_dim;
     const int32_t* table; int width;
     const int32_t* starts; const int32_t* context; int n, T;

@@ -148,7 +148,8 @@ int qblora_paged_attention(const qblora_bf16* q, int64_t ldq, int32_t heads, con
     if (n < 0 || T < 0 || width < 0 || window < 0 || max_new < 0 || heads <= 0 || heads % cache->heads != 0)
         return QBLORA_ERR_SHAPE;
     if (T > kMostPositions || (int64_t)width * cache->page > kMostPositions || window > kMostPositions ||
-        T * (heads / cache->heads) > INT32_MAX || cache->heads > 65535)
+        T * (heads / cache->heads) > INT32_MAX || cache->heads > 65535 ||
+        heads / cache->heads > 32768)
         return QBLORA_ERR_UNSUPPORTED;
     if (T == 0 || n == 0) return QBLORA_OK;
     if (!q || !out || !starts || !context || (width && !table)) return QBLORA_ERR_NULL;
@@ -158,6 +159,7 @@ int qblora_paged_attention(const qblora_bf16* q, int64_t ldq, int32_t heads, con
     if (!aligned(workspace, 16)) return QBLORA_ERR_SHAPE;
     AttnDesc d{};
     d.q = q; d.ldq = ldq; d.heads = heads; d.kv_heads = cache->heads; d.group = heads / cache->heads;
+    d.group_magic = (uint32_t)(((uint64_t)1 << 32) / (uint32_t)d.group + 1);
     d.kc = cache->k; d.vc = cache->v; d.pages = cache->pages; d.page_shift = page_shift_of(cache->page);
     d.head_dim = cache->head_dim; d.table = table; d.width = width; d.starts = starts; d.context = context;
     d.n = n; d.T = (int)T; d.scale_log2 = scale * 1.44269504088896340736f; d.window = window; d.max_new = max_new;
