@@ -29,7 +29,7 @@ namespace qblora {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
+constexpr int kThreads = 256, kMostWaves = 8;
 constexpr int kFewRows = 16;
 constexpr int kBlock = 32;                     // positions of a step
 constexpr int kManyRows = 128;
@@ -108,13 +108,13 @@ __device__ __forceinline__ Units units_of(const Cost& c, int64_t per) {
 
 // The unit number `want` of the batch; false: there are not so many.  With `first`, the number of cut tiles is left where
 // k_attn_join looks for it.  All threads call it.  Up to 64 requests every wave finds it by itself, a request a lane; more
-// are taken 256 at a time.
+// are taken a workgroup's threads at a time.
 struct Finder {
-    int64_t sums[kWaves];
-    int ends[2][kWaves], found[6];
+    int64_t sums[kMostWaves];
+    int ends[2][kMostWaves], found[6];
 };
 __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share, int want, bool first, Finder& f, Unit& u) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, threads = blockDim.x, waves = threads >> 6;
     if (d.n <= 64) {
         Cost c{0, 0};
         if (lane < d.n) c = cost_of(d, lane, share);
@@ -135,7 +135,7 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
         return true;
     }
     int64_t all = 0;
-    for (int i = tid; i < d.n; i += kThreads) {
+    for (int i = tid; i < d.n; i += threads) {
         const Cost c = cost_of(d, i, share);
         all += (int64_t)c.tiles * c.blocks;
     }
@@ -144,10 +144,10 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
     if (tid == 0) f.found[0] = -1;
     __syncthreads();
     all = 0;
-    for (int w = 0; w < kWaves; ++w) all += f.sums[w];
+    for (int w = 0; w < waves; ++w) all += f.sums[w];
     const int64_t per = blocks_per_unit(all, share);
-    int units = 0, cuts = 0;                                           // in front of these 256 requests
-    for (int base = 0; base < d.n; base += kThreads) {
+    int units = 0, cuts = 0;                                           // in front of these requests
+    for (int base = 0; base < d.n; base += threads) {
         const int i = base + tid;
         Cost c{0, 0};
         if (i < d.n) c = cost_of(d, i, share);
@@ -156,7 +156,7 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
         __syncthreads();
         if (lane == 63) { f.ends[0][wave] = a; f.ends[1][wave] = b; }
         __syncthreads();
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < waves; ++w) {
             if (w == wave) { a += units; b += cuts; }
             units += f.ends[0][w];
             cuts += f.ends[1][w];
@@ -230,14 +230,14 @@ __device__ __forceinline__ const qblora_bf16* value_row(const AttnDesc& d, const
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-template <int D>
+template <int D, int W>
 struct FewShared {
-    float o[kWaves][kFewRows][D + 4];
-    float m[kWaves][kFewRows], l[kWaves][kFewRows];
+    float o[W][kFewRows][D + 4];
+    float m[W][kFewRows], l[W][kFewRows];
 };
 
-template <int D>
-__device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share, int block, Finder& finder, FewShared<D>& sh) {
+template <int D, int W>
+__device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share, int block, Finder& finder, FewShared<D, W>& sh) {
     constexpr int KS = D / 32, DT = D / 16;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, col = lane & 15;
     const int kvh = block % d.kv_heads;
@@ -267,7 +267,7 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
     const int shift = d.page_shift, page = 1 << shift;
     const int64_t page_elems = (int64_t)d.kv_heads * D << shift, head_elems = ((int64_t)kvh * D) << shift;
     const int32_t* table = d.table + (int64_t)u.request * d.width;
-    const int steps = b0 + wave < b1 ? (b1 - b0 - wave + kWaves - 1) / kWaves : 0;
+    const int steps = b0 + wave < b1 ? (b1 - b0 - wave + W - 1) / W : 0;
 
     f32x4 o[DT];
 #pragma unroll
@@ -281,7 +281,7 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
     // pages of a step (step 64 k first)
     auto find_pages = [&](int step, int& id0, int& id1) {
         if ((step & 63) == 0) {
-            const int pos = (b0 + wave + kWaves * (step + lane)) * kBlock;
+            const int pos = (b0 + wave + W * (step + lane)) * kBlock;
             ids0 = ids1 = -1;
             if (pos < t.pos1) ids0 = table[pos >> shift];
             if (pos + 16 < t.pos1) ids1 = table[(pos + 16) >> shift];
@@ -292,7 +292,7 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
         id1 = __builtin_amdgcn_readlane(ids1, step & 63);
     };
     auto load_keys = [&](int step, int id0, int id1) {
-        const int base = (b0 + wave + kWaves * step) * kBlock;
+        const int base = (b0 + wave + W * step) * kBlock;
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
             const int at = 8 * (col >> 2) + 4 * tt + (col & 3);        // position of row `col` of this 16 x 16 tile
@@ -303,7 +303,7 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
         }
     };
     auto load_values = [&](int step, int id0, int id1) {
-        const int base = (b0 + wave + kWaves * step) * kBlock;
+        const int base = (b0 + wave + W * step) * kBlock;
         const int id = max(g < 2 ? id0 : id1, 0);
         const qblora_bf16* v = d.vc + id * page_elems + head_elems + ((((base + 8 * g) & (page - 1)) >> 3) * D + col) * 8;
 #pragma unroll
@@ -317,7 +317,7 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
         load_values(0, id0, id1);
     }
     for (int step = 0; step < steps; ++step) {
-        const int base = (b0 + wave + kWaves * step) * kBlock;
+        const int base = (b0 + wave + W * step) * kBlock;
         const bool listed0 = id0 >= 0, listed1 = id1 >= 0;
         f32x4 sc[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
 #pragma unroll
@@ -404,14 +404,14 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
         for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4*>(&sh.o[wave][col][16 * i + 4 * g]) = o[i];
     __syncthreads();
     float* part = u.splits > 1 ? share.part + ((int64_t)u.slot * d.kv_heads + kvh) * (kFewRows * (D + 2)) : nullptr;
-    for (int i = tid; i < t.rows * (D / 4); i += kThreads) {
+    for (int i = tid; i < t.rows * (D / 4); i += 64 * W) {
         const int r = i / (D / 4), f = 4 * (i % (D / 4));
         float top = kNegInf;
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh.m[w][r]);
+        for (int w = 0; w < W; ++w) top = fmaxf(top, sh.m[w][r]);
         const float use = top == kNegInf ? 0.0f : top;
         float sum = 0.0f;
         f32x4 v = {0, 0, 0, 0};
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < W; ++w) {
             const float a = exp2_of(sh.m[w][r] - use);
             sum = __fmaf_rn(sh.l[w][r], a, sum);
             const f32x4 x = *reinterpret_cast<const f32x4*>(&sh.o[w][r][f]);
@@ -441,7 +441,16 @@ __device__ __forceinline__ void gather_to_lds(const void* p, uint32_t lds_base) 
 __device__ __forceinline__ void copy_to_lds(const void* uniform_base, uint32_t lane_offset, uint32_t lds_base) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds_base), "v"(lane_offset), "s"(uniform_base) : "memory");
 }
-__device__ __forceinline__ void wait_for_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// until at most N of the wave's copies are on their way
+template <int N>
+__device__ __forceinline__ void wait_for_copies() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | 7 << 4 | 15 << 8 | (N >> 4) << 14);            // vmcnt alone
+    asm volatile("" ::: "memory");
+}
+
+// A barrier that leaves copies on their way: what the wave has read of LDS it has.
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // of both halves of the wave
 __device__ __forceinline__ float max_of_halves(float x) {
@@ -456,18 +465,19 @@ __device__ __forceinline__ float sum_of_halves(float x) {
 }
 
 template <int D>
-struct ManyShared {                                                    // [turn][keys, values]
-    static constexpr int kTile = D > 128 ? 32 : 64;
-    __attribute__((aligned(16))) unsigned char buf[2][2][kTile * D * 2];
+struct ManyShared {
+    // positions of a tile: 64, or 32 where the registers hold no more beside 256 features
+    static constexpr int kTile = D > 128 ? 32 : 64, kTileBytes = kTile * D * 2;
+    __attribute__((aligned(16))) unsigned char buf[2][2][kTileBytes];          // [keys, values][turn]
 };
 
 template <int D>
 __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& share, int block, Finder& finder, ManyShared<D>& sh) {
-    // positions of a tile: 64, or 32 where the registers hold no more beside 256 features
-    constexpr int kTile = ManyShared<D>::kTile, KS = D / 16, DT = D / 32, TT = kTile / 32, PS = kTile / 16;
-    constexpr int kTileBytes = kTile * D * 2;
-    constexpr int kCopies = kTileBytes / 1024 / kWaves;                // of keys, and again of values, a wave and tile
-    auto& buf = sh.buf;
+    constexpr int kTile = ManyShared<D>::kTile, kTileBytes = ManyShared<D>::kTileBytes;
+    constexpr int KS = D / 16, DT = D / 32, TT = kTile / 32;
+    constexpr int PS = kTile / 16, kSixteen = D * 32;                  // a tile's sixteens of positions, bytes of one
+    constexpr int kSharers = 4 / PS, kCopies = kSixteen / 1024 / kSharers;     // waves that copy a sixteen, copies of each
+    constexpr int kBatch = 64 / PS;                                    // tiles whose pages a wave looks up at once
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
     const int kvh = block % d.kv_heads;
     Unit u;
@@ -487,7 +497,7 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
     const bool real = col < w_rows;
     const int here = s.context + token;
     const int first = s.context + t.token0 + quotient(d, t.rem0 + 32 * wave), last = s.context + t.token0 + quotient(d, t.rem0 + 32 * wave + max(w_rows, 1) - 1);
-    const int full0 = d.window ? max(last + 1 - d.window, 0) : 0, full1 = min(first + 1, limit);
+    const int full0 = d.window ? max(last + 1 - d.window, 0) : 0, full1 = w_rows > 0 ? min(first + 1, limit) : 0;
     const int see0 = d.window ? max(first + 1 - d.window, 0) : 0, see1 = w_rows > 0 ? min(last + 1, limit) : 0;
 
     // rows: operand B, row = lane & 31, features 16 i + 8 h ..; a negative scale is the rows' sign, one of 0 makes them 0
@@ -502,174 +512,185 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
         qf[i] = __builtin_bit_cast(bf16x8, v);
     }
 
+    // Copies: every wave has a sixteen of a tile's positions, or half of its features, so that it needs one page.
     const int shift = d.page_shift, page = 1 << shift;
-    const int64_t page_elems = (int64_t)d.kv_heads * D << shift, head_elems = ((int64_t)kvh * D) << shift;
+    const int64_t page_bytes = (int64_t)d.kv_heads * D * 2 << shift;
+    const int mine = wave % PS, part = wave / PS;                      // the sixteen, the half
     const int32_t* table = d.table + (int64_t)u.request * d.width;
-    const uint32_t lds = lds_address(buf);
-
-    auto page_id = [&](int tile) {                                     // of the tile's position `lane` (and again behind 32)
-        const int pos = tile * kTile + lane % kTile;
-        return tile < n1 && pos < t.pos1 ? table[pos >> shift] : -1;
-    };
-    // copies of a tile with these pages; which of its positions are listed
-    auto copy = [&](int tile, int id, int turn) {
-        const bool ok = (uint32_t)id < (uint32_t)d.pages;
-        id = ok ? id : 0;
-        const int in_page = (tile * kTile + lane % kTile) & (page - 1);
-        const qblora_bf16* k = d.kc + id * page_elems + head_elems + (((lane / kTile) << shift) + in_page) * 8;
+    const unsigned char* k_head = reinterpret_cast<const unsigned char*>(d.kc) + ((int64_t)kvh * D * 2 << shift) + ((part * kCopies * 4) << shift) * 16;
+    const unsigned char* v_head = reinterpret_cast<const unsigned char*>(d.vc) + ((int64_t)kvh * D * 2 << shift) + part * kCopies * 1024;
+    const uint32_t k_lane = (((lane >> 4) << shift) + (lane & 15)) * 16, v_lane = lane * 16;
+    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(sh.buf)) + mine * kSixteen + part * kCopies * 1024;
+    int batch = 0;
+    uint64_t batch_listed = 0;
+    // copies tile j, and says which of its sixteens are listed; for j = 0, 1, ..
+    auto copy = [&](int j) {
+        const int tile = n0 + j;
+        if (j % kBatch == 0) {
+            const int pos = (tile + lane / PS) * kTile + 16 * (lane % PS);
+            batch = -1;
+            if (pos < min(t.pos1, n1 * kTile)) batch = table[pos >> shift];
+            const bool ok = (uint32_t)batch < (uint32_t)d.pages;
+            batch_listed = __ballot(ok);
+            batch = ok ? batch : 0;
+        }
+        const int id = __builtin_amdgcn_readlane(batch, j % kBatch * PS + mine), in_page = (tile * kTile + 16 * mine) & (page - 1);
+        const unsigned char* k = k_head + id * page_bytes + in_page * 16;
+        const unsigned char* v = v_head + id * page_bytes + in_page * (D * 2);
+        const uint32_t to = lds + (j & 1) * kTileBytes;
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
-            const int part = wave * kCopies + i;
-            gather_to_lds(k + (part * (64 / kTile) << shift) * 8, lds + (uint32_t)(turn * 2 * kTileBytes + part * 1024));
+            copy_to_lds(k, k_lane, to + i * 1024);
+            k += (4 << shift) * 16;
         }
 #pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
-            const int part = wave * kCopies + i, octet = part / (D / 64), f0 = part % (D / 64) * 64;
-            const int o_id = __builtin_amdgcn_readlane(id, 8 * octet);
-            const int o_page = ((tile * kTile + 8 * octet) & (page - 1)) >> 3;
-            const qblora_bf16* v = d.vc + o_id * page_elems + head_elems + (o_page * D + f0) * 8;
-            copy_to_lds(v, 16 * lane, lds + (uint32_t)(turn * 2 * kTileBytes + kTileBytes + part * 1024));
-        }
-        return __ballot(ok);
+        for (int i = 0; i < kCopies; ++i) copy_to_lds(v + i * 1024, v_lane, to + 2 * kTileBytes + i * 1024);
+        return (uint32_t)(batch_listed >> (j % kBatch * PS)) & ((1u << PS) - 1);
     };
 
     f32x16 o[DT];
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
-    float m = kNegInf, l = 0.0f;                                       // l: of this lane's positions
+        for (int k = 0; k < 16; ++k) o[i][k] = 0.0f;
+    // Exponents are c s - ref, ref near the maximum of c s; l: the sum over this lane's positions.  Where c s is so large that
+    // a product's rounding counts, ref is 0 and the maximum `m` is taken off the products first.
+    float ref = kNegInf, m = kNegInf, l = 0.0f;
+    bool large = false;
     int odd0 = INT_MAX, odd1 = 0;                                      // positions among which values are not finite
 
     // position of row `col` of a 32 x 32 tile, so that a lane's scores are of eight consecutive positions twice
     const int perm = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
-    uint64_t listed = 0, next_listed = 0;
-    int id = page_id(n0);
-    if (n0 < n1) {
-        listed = copy(n0, id, 0);
-        id = page_id(n0 + 1);
-    }
-    for (int tile = n0, turn = 0; tile < n1; ++tile, turn ^= 1) {
-        wait_for_copies();
-        __syncthreads();                                               // the tile is there, and the other one is free
-        if (tile + 1 < n1) {
-            const int now = id;
-            id = page_id(tile + 2);
-            next_listed = copy(tile + 1, now, turn ^ 1);
+    const unsigned char* const k_from = sh.buf[0][0] + (perm >> 4) * kSixteen + h * 256 + (perm & 15) * 16;
+    const unsigned char* const v_from = sh.buf[1][0] + (h * D + col) * 16;
+    auto key = [&](int j, int i, int tt) {
+        return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(k_from + (j & 1) * kTileBytes + tt * 2 * kSixteen + i * 512));
+    };
+    auto value = [&](int j, int s4, int i) { return *reinterpret_cast<const uint4*>(v_from + (j & 1) * kTileBytes + s4 * kSixteen + i * 512); };
+    auto products = [&](int j, f32x16 (&sc)[TT]) {
+#pragma unroll
+        for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) sc[tt][k] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+#pragma unroll
+            for (int tt = 0; tt < TT; ++tt) sc[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key(j, i, tt), qf[i], sc[tt], 0, 0, 0);
+            if (D > 128 && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);          // no more operands ahead than registers
         }
-        const int base = tile * kTile;
-        if (base < see1 && base + kTile > see0) {
-            const unsigned char* kb = buf[turn][0] + (h * kTile + perm) * 16;
-            const unsigned char* vb = buf[turn][1] + (h * D + col) * 16;
+    };
+    auto weights = [&](f32x16 (&sc)[TT], bf16x8 (&pf)[PS]) {
+        float top = sc[0][0];
+#pragma unroll
+        for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) top = fmaxf(top, sc[tt][k]);
+        top = max_of_halves(top);
+        if (__any(top * c > ref + kSlack || m == kNegInf || large)) {
+            const float m_new = fmaxf(m, top), m_use = m_new == kNegInf ? 0.0f : m_new;
+            const float a = m == kNegInf ? 0.0f : exp2_of(large ? (m - m_use) * c : ref - m_use * c);
+            large = large || __any(fabsf(m_use) * c > 0x1p26f);
+            m = m_new;
+            ref = large ? 0.0f : m_use * c;
+            l *= a;
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) o[i][k] *= a;
+            if (large) {
+#pragma unroll
+                for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) sc[tt][k] -= m_use;
+            }
+        }
+#pragma unroll
+        for (int s4 = 0; s4 < PS; ++s4) {
+            uint32_t pw[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float p0 = exp2_of(__fmaf_rn(sc[s4 >> 1][8 * (s4 & 1) + 2 * k], c, -ref));
+                const float p1 = exp2_of(__fmaf_rn(sc[s4 >> 1][8 * (s4 & 1) + 2 * k + 1], c, -ref));
+                l += p0 + p1;
+                pw[k] = pack_bf16(p0, p1);
+            }
+            pf[s4] = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+        }
+    };
+
+    const int turns = n1 - n0;
+    uint32_t listed = 0, next_listed = 0;
+    if (turns > 0) next_listed = copy(0);
+    auto full = [&](int j) {                                           // seen by all rows of the wave
+        const int base = (n0 + j) * kTile;
+        return base >= full0 && base + kTile <= full1 && next_listed == (1u << PS) - 1;
+    };
+    auto enter = [&](int j) {                                          // tile j is there, and the next one is copied
+        listed = next_listed;
+        wait_for_copies<0>();
+        meet();
+        if (j + 1 < turns) next_listed = copy(j + 1);
+    };
+    for (int j = 0; j < turns;) {
+        // tiles that some row sees in part, or none
+        for (; j < turns && !full(j); ++j) {
+            enter(j);
+            const int base = (n0 + j) * kTile;
+            if (base >= see1 || base + kTile <= see0) continue;
             f32x16 sc[TT];
+            products(j, sc);
+            const int row_low = d.window ? here - d.window : -1;
+            uint32_t any = 0, seen = 0;                                // by some row, by this lane's; bit 8 s4 + k: position 16 s4 + 8 h + k
 #pragma unroll
-            for (int tt = 0; tt < TT; ++tt)
+            for (int s4 = 0; s4 < PS; ++s4)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) sc[tt][j] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < KS; ++i) {
-#pragma unroll
-                for (int tt = 0; tt < TT; ++tt)
-                    sc[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(kb + 2 * i * kTile * 16 + tt * 512)), qf[i], sc[tt], 0, 0, 0);
-                if (D > 128 && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // no more operands ahead than registers
-            }
-            const bool masked = base < full0 || base + kTile > full1 || ~listed != 0;
-            uint32_t seen = 0xffffffffu, any = 0xffffffffu;            // bit 8 s + j: position 16 s + 8 h + j of the tile
-            if (masked) {
-                const int h8 = 8 * (int)opaque_bits((uint32_t)h);
-                const int row_low = d.window ? here - d.window : -1;
-                seen = any = 0;
-#pragma unroll
-                for (int s4 = 0; s4 < PS; ++s4) {
-                    const uint32_t half_tile = s4 < 2 ? (uint32_t)listed : (uint32_t)(listed >> 32), here8 = (half_tile >> (16 * (s4 & 1) + h8)) & 0xffu;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int pos = base + 16 * s4 + h8 + j;
-                        if (pos >= see0 && pos < see1) any |= 1u << (8 * s4 + j);
-                        if (pos <= here && pos > row_low) seen |= 1u << (8 * s4 + j);
-                    }
-                    any &= ~(0xffu << (8 * s4)) | here8 << (8 * s4);
+                for (int k = 0; k < 8; ++k) {
+                    const int pos = base + 16 * s4 + 8 * h + k;
+                    if (pos >= see0 && pos < see1 && (listed >> s4 & 1)) any |= 1u << (8 * s4 + k);
+                    if (pos <= here && pos > row_low) seen |= 1u << (8 * s4 + k);
                 }
-                seen &= any;
-#pragma unroll
-                for (int tt = 0; tt < TT; ++tt)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) sc[tt][j] = (seen >> (16 * tt + j)) & 1 ? sc[tt][j] : kNegInf;
-            }
-            float top = sc[0][0];
+            seen &= any;
 #pragma unroll
             for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) top = fmaxf(top, sc[tt][j]);
-            top = max_of_halves(top);                                  // m, top: maxima of the products, not scaled yet
-            if (__any(top * c > m * c + kSlack || m == kNegInf)) {
-                const float m_new = fmaxf(m, top), a = exp2_of((m - (m_new == kNegInf ? 0.0f : m_new)) * c);
-                m = m_new;
-                l *= a;
-#pragma unroll
-                for (int i = 0; i < DT; ++i)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) o[i][j] *= a;
-            }
-            // The exponents c (s - m), as c s - (c m) in one operation while the rounding of c m, 2^-24 of it, is nothing
-            const float m_use = m == kNegInf ? 0.0f : m, mc = m_use * c;
-            if (__any(fabsf(mc) > 1024.0f)) {
-#pragma unroll
-                for (int tt = 0; tt < TT; ++tt)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) sc[tt][j] = (sc[tt][j] - m_use) * c;
-            } else {
-#pragma unroll
-                for (int tt = 0; tt < TT; ++tt)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) sc[tt][j] = __fmaf_rn(sc[tt][j], c, -mc);
-            }
+                for (int k = 0; k < 16; ++k) sc[tt][k] = (seen >> (16 * tt + k)) & 1 ? sc[tt][k] : kNegInf;
             bf16x8 pf[PS];
+            weights(sc, pf);
+            // as in attend_few: values that no row sees are 0, and what is not finite is added behind the loop
+            bool odd = false;
 #pragma unroll
             for (int s4 = 0; s4 < PS; ++s4) {
-                uint32_t pw[4];
+                const uint32_t bits = any >> (8 * s4), k0 = mask_of(bits), k1 = mask_of(bits >> 2), k2 = mask_of(bits >> 4), k3 = mask_of(bits >> 6);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float p0 = exp2_of(sc[s4 >> 1][8 * (s4 & 1) + 2 * j]);
-                    const float p1 = exp2_of(sc[s4 >> 1][8 * (s4 & 1) + 2 * j + 1]);
-                    l += p0 + p1;
-                    pw[j] = pack_bf16(p0, p1);
+                for (int i = 0; i < DT; ++i) {
+                    uint4 v = value(j, s4, i);
+                    v = make_uint4(v.x & k0, v.y & k1, v.z & k2, v.w & k3);
+                    odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
+                    v = make_uint4(without_not_finite(v.x), without_not_finite(v.y), without_not_finite(v.z), without_not_finite(v.w));
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pf[s4], o[i], 0, 0, 0);
                 }
-                pf[s4] = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+                __builtin_amdgcn_sched_barrier(0);
             }
-            if (!masked) {
-#pragma unroll
-                for (int s4 = 0; s4 < PS; ++s4) {
-#pragma unroll
-                    for (int i = 0; i < DT; ++i)
-                        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(vb + (2 * s4 * D + 32 * i) * 16)), pf[s4], o[i], 0, 0, 0);
-                    if (D > 128) __builtin_amdgcn_sched_barrier(0);
-                }
-            } else {
-                // as in attend_few: values that no row sees are 0, and what is not finite is added behind the loop
-                bool odd = false;
-#pragma unroll
-                for (int s4 = 0; s4 < PS; ++s4) {
-                    const uint32_t bits = any >> (8 * s4), k0 = mask_of(bits), k1 = mask_of(bits >> 2), k2 = mask_of(bits >> 4), k3 = mask_of(bits >> 6);
-#pragma unroll
-                    for (int i = 0; i < DT; ++i) {
-                        uint4 v = *reinterpret_cast<const uint4*>(vb + (2 * s4 * D + 32 * i) * 16);
-                        v = make_uint4(v.x & k0, v.y & k1, v.z & k2, v.w & k3);
-                        odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
-                        v = make_uint4(without_not_finite(v.x), without_not_finite(v.y), without_not_finite(v.z), without_not_finite(v.w));
-                        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pf[s4], o[i], 0, 0, 0);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                if (__any(odd)) {
-                    odd0 = min(odd0, base);
-                    odd1 = base + kTile;
-                }
+            if (__any(odd)) {
+                odd0 = min(odd0, base);
+                odd1 = base + kTile;
             }
         }
-        listed = next_listed;
+        // the others, nearly all of a long context: a loop of its own, so that its registers are its own
+        for (; j < turns && full(j); ++j) {
+            enter(j);
+            f32x16 sc[TT];
+            products(j, sc);
+            bf16x8 pf[PS];
+            weights(sc, pf);
+#pragma unroll
+            for (int s4 = 0; s4 < PS; ++s4) {
+#pragma unroll
+                for (int i = 0; i < DT; ++i)
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, value(j, s4, i)), pf[s4], o[i], 0, 0, 0);
+                if (D > 128) __builtin_amdgcn_sched_barrier(0);
+            }
+        }
     }
 
     // (the lane's row again: the loop has no registers to keep it in)
@@ -681,20 +702,19 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) o[i][j] += if_not_finite(v[(32 * i + 8 * (j >> 2) + 4 * h2 + (j & 3)) * 8]);
+            for (int k = 0; k < 16; ++k) o[i][k] += if_not_finite(v[(32 * i + 8 * (k >> 2) + 4 * h2 + (k & 3)) * 8]);
     }
-
     l = sum_of_halves(l);
-    m *= c;
+    const float top = m == kNegInf ? kNegInf : large ? m * c : ref;    // what the sums are relative to
     if (r >= t.rows) return;
     if (u.splits > 1) {
-        float* part = share.part + ((int64_t)u.slot * d.kv_heads + kvh) * (kManyRows * (D + 2));
+        float* part_of = share.part + ((int64_t)u.slot * d.kv_heads + kvh) * (kManyRows * (D + 2));
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
             for (int b = 0; b < 4; ++b)
-                *reinterpret_cast<float4*>(part + r * D + 32 * i + 8 * b + 4 * h2) = make_float4(o[i][4 * b], o[i][4 * b + 1], o[i][4 * b + 2], o[i][4 * b + 3]);
-        if (h2 == 0) { part[kManyRows * D + r] = m; part[kManyRows * (D + 1) + r] = l; }
+                *reinterpret_cast<float4*>(part_of + r * D + 32 * i + 8 * b + 4 * h2) = make_float4(o[i][4 * b], o[i][4 * b + 1], o[i][4 * b + 2], o[i][4 * b + 3]);
+        if (h2 == 0) { part_of[kManyRows * D + r] = top; part_of[kManyRows * (D + 1) + r] = l; }
         return;
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -705,22 +725,25 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
         for (int b = 0; b < 4; ++b)
             *reinterpret_cast<uint2*>(out + 32 * i + 8 * b + 4 * h2) =
                 make_uint2(pack_bf16(o[i][4 * b] * inv, o[i][4 * b + 1] * inv), pack_bf16(o[i][4 * b + 2] * inv, o[i][4 * b + 3] * inv));
-    if (h2 == 0 && d.lse) d.lse[(int64_t)(s.start + to) * d.heads + q_head] = (m + __builtin_log2f(l)) * 0.69314718055994530942f;
+    if (h2 == 0 && d.lse) d.lse[(int64_t)(s.start + to) * d.heads + q_head] = (top + __builtin_log2f(l)) * 0.69314718055994530942f;
 }
 
 // One of the forms, or both, so that chunks and single tokens of a batch run beside each other.
 enum { FEW = 1, LOT = 2, BOTH = 3 };
 template <int D, int FORMS>
-__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2) void k_attn(AttnDesc d, Share lot, Share few, int lot_blocks) {
+constexpr int waves_of() { return 4; }
+template <int D, int FORMS>
+__global__ __launch_bounds__((64 * waves_of<D, FORMS>()), (D > 128 ? 1 : 2)) void k_attn(AttnDesc d, Share lot, Share few, int lot_blocks) {
+    constexpr int W = waves_of<D, FORMS>();
     __shared__ Finder finder;
     __shared__ union Shared {
         std::conditional_t<(FORMS & LOT) != 0, ManyShared<D>, char> many;
-        std::conditional_t<(FORMS & FEW) != 0, FewShared<D>, char> few;
+        std::conditional_t<(FORMS & FEW) != 0, FewShared<D, W>, char> few;
     } sh;
     if constexpr ((FORMS & LOT) != 0) {
         if (FORMS == LOT || (int)blockIdx.x < lot_blocks) return attend_many<D>(d, lot, blockIdx.x, finder, sh.many);
     }
-    if constexpr ((FORMS & FEW) != 0) attend_few<D>(d, few, blockIdx.x - (FORMS & LOT ? lot_blocks : 0), finder, sh.few);
+    if constexpr ((FORMS & FEW) != 0) attend_few<D, W>(d, few, blockIdx.x - (FORMS & LOT ? lot_blocks : 0), finder, sh.few);
 }
 
 // Adds up the parts of a cut tile, weights 2^(m - max m): a workgroup takes every gridDim.y-th row, four features a thread,
@@ -729,7 +752,7 @@ template <int D>
 __global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share lot, Share few, int lot_blocks) {
     constexpr int kQuads = D / 4, kGroups = kThreads / kQuads;
     __shared__ float weight[kFewTarget + 1];
-    __shared__ float top_of[kWaves], sum_of[kWaves];
+    __shared__ float top_of[4], sum_of[4];
     __shared__ f32x4 sums[kGroups][kQuads];
     const bool of_lot = (int)blockIdx.x < lot_blocks;
     const Share& share = of_lot ? lot : few;
@@ -827,16 +850,16 @@ int launch(const AttnDesc& d, hipStream_t st) {
     const int64_t lot_tiles = many ? (int64_t)d.T * d.group / kManyRows + d.n : 0;
     const int64_t lot_blocks = many ? (lot_tiles + lot.target) * d.kv_heads : 0, blocks = lot_blocks + (few_tiles + few.target) * d.kv_heads;
     if (blocks > INT32_MAX) return QBLORA_ERR_UNSUPPORTED;
-    const auto go = [&](auto kernel, int64_t count) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(kThreads), 0, st, d, lot, few, (int)lot_blocks);
+    const auto go = [&](auto kernel, int waves, int64_t count) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(64 * waves), 0, st, d, lot, few, (int)lot_blocks);
     };
     if (!many) {
-        go(k_attn<D, FEW>, blocks);
+        go(k_attn<D, FEW>, waves_of<D, FEW>(), blocks);
     } else if constexpr (D <= 128) {
-        go(k_attn<D, BOTH>, blocks);
+        go(k_attn<D, BOTH>, waves_of<D, BOTH>(), blocks);
     } else {                                                           // (one kernel of both would not have the registers)
-        go(k_attn<D, LOT>, lot_blocks);
-        go(k_attn<D, FEW>, blocks - lot_blocks);
+        go(k_attn<D, LOT>, waves_of<D, LOT>(), lot_blocks);
+        go(k_attn<D, FEW>, waves_of<D, FEW>(), blocks - lot_blocks);
     }
     // no context is long enough for a cut
     if ((int64_t)d.width << d.page_shift <= kFewLeast * kBlock) return launch_status();
