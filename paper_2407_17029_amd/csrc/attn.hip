@@ -8,8 +8,8 @@
 //
 // attend_few takes 16 rows, the width of the matrix instruction, and is bound by the stream of the cache: a wave takes 32
 // positions at a time straight from the pages into registers, in the operand order that the cache is stored in, with the
-// next 32 in flight behind them.  Scores are formed transposed, S^T = K Q^T, so that a lane holds eight consecutive positions
-// of one row: that is the operand of O^T = V^T P^T as it stands.  The four waves of a workgroup take turns on the positions
+// next 32 in flight behind them.  Scores are formed transposed, S^T = K Q^T, so that a lane holds eight positions of one row,
+// the operand of O^T = V^T P^T but for four exchanges between lanes.  The four waves of a workgroup take turns on the positions
 // and are joined in LDS.
 //
 // attend_many takes 128 rows, 32 a wave, and is bound by the matrix pipe and by the exponentials beside it.  64 positions at a
@@ -37,12 +37,12 @@ constexpr float kNegInf = -__builtin_inff();
 constexpr float kSlack = 8.0f;                 // a maximum may grow by 2^8 before what was summed is rescaled
 
 // Which requests a form takes, by their rows, and how their work is shared out: units of `rows` rows, about `target` of them
-// for a key / value head, at least `least` blocks each.  Tiles that are cut leave their parts in `part` and themselves in
+// for a key / value head, at least `least` blocks each; one that is not more than 1 + slack / 2 units long stays whole.  Tiles that are cut leave their parts in `part` and themselves in
 // `cut`, `cuts` counts those.
 struct CutTile { int token0, rem0, rows, splits, slot, pad[3]; };
-struct Share { int rows, target, least; int64_t over, upto; int* cuts; CutTile* cut; float* part; };
+struct Share { int rows, target, least, slack; int64_t over, upto; int* cuts; CutTile* cut; float* part; };
 constexpr int kFewTarget = 1024, kFewLeast = 8;
-constexpr int kManyTarget = 512, kManyLeast = 16;
+constexpr int kManyTarget = 384, kManyLeast = 32;
 static_assert(2 * kFewTarget < 1 << 15 && 2 * kManyTarget < 1 << 15, "parts and cut tiles are counted in halves of a word");
 
 // A workgroup's rows and range of positions; slot: its place among the parts, cut: its tile's among those that are cut
@@ -97,10 +97,10 @@ __device__ __forceinline__ int64_t blocks_per_unit(int64_t all, const Share& w) 
     return max(per, (int64_t)w.least);
 }
 struct Units { int tiles, splits, count, cuts; };                      // cuts: parts, and cut tiles in the upper half
-__device__ __forceinline__ Units units_of(const Cost& c, int64_t per) {
+__device__ __forceinline__ Units units_of(const Cost& c, int64_t per, int slack) {
     Units u;
     u.tiles = c.tiles;
-    u.splits = c.blocks > per ? (int)((uint32_t)(c.blocks - 1) / (uint32_t)per) + 1 : 1;
+    u.splits = max(1, (int)(((uint32_t)c.blocks + (uint32_t)(slack ? per / 2 : per - 1)) / (uint32_t)per));
     u.count = u.tiles * u.splits;
     u.cuts = u.splits > 1 ? u.count + (u.tiles << 16) : 0;
     return u;
@@ -118,7 +118,7 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
     if (d.n <= 64) {
         Cost c{0, 0};
         if (lane < d.n) c = cost_of(d, lane, share);
-        const Units v = units_of(c, blocks_per_unit(sum_of_wave((int64_t)c.tiles * c.blocks), share));
+        const Units v = units_of(c, blocks_per_unit(sum_of_wave((int64_t)c.tiles * c.blocks), share), share.slack);
         const int a = scan(v.count), b = scan(v.cuts);
         if (first && tid == 63) *share.cuts = b >> 16;
         const uint64_t hit = __ballot(v.count && a - v.count <= want && want < a);
@@ -151,7 +151,7 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
         const int i = base + tid;
         Cost c{0, 0};
         if (i < d.n) c = cost_of(d, i, share);
-        const Units v = units_of(c, per);
+        const Units v = units_of(c, per, share.slack);
         int a = scan(v.count), b = scan(v.cuts);
         __syncthreads();
         if (lane == 63) { f.ends[0][wave] = a; f.ends[1][wave] = b; }
@@ -228,6 +228,12 @@ __device__ __forceinline__ const qblora_bf16* value_row(const AttnDesc& d, const
     return d.vc + (((int64_t)id * d.kv_heads + kvh) * D << d.page_shift) + (in_page >> 3) * D * 8 + (in_page & 7);
 }
 
+// A part of the cache that this call reads once: no line is kept for it.  64 tokens of 40 heads, contexts of 1750: 411 us
+// without, 376 with values that way.
+__device__ __forceinline__ uint4 stream(const qblora_bf16* p) {
+    return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p)));
+}
+
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 template <int D, int W>
@@ -295,11 +301,10 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
         const int base = (b0 + wave + W * step) * kBlock;
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
-            const int at = 8 * (col >> 2) + 4 * tt + (col & 3);        // position of row `col` of this 16 x 16 tile
-            const int id = max(at < 16 ? id0 : id1, 0);
-            const qblora_bf16* k = d.kc + id * page_elems + head_elems + ((g << shift) + ((base + at) & (page - 1))) * 8;
+            const int id = max(tt == 0 ? id0 : id1, 0);
+            const qblora_bf16* k = d.kc + id * page_elems + head_elems + ((g << shift) + ((base + 16 * tt) & (page - 1)) + col) * 8;
 #pragma unroll
-            for (int i = 0; i < KS; ++i) kf[tt][i] = *reinterpret_cast<const uint4*>(k + ((4 * i) << shift) * 8);
+            for (int i = 0; i < KS; ++i) kf[tt][i] = stream(k + ((4 * i) << shift) * 8);
         }
     };
     auto load_values = [&](int step, int id0, int id1) {
@@ -307,7 +312,7 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
         const int id = max(g < 2 ? id0 : id1, 0);
         const qblora_bf16* v = d.vc + id * page_elems + head_elems + ((((base + 8 * g) & (page - 1)) >> 3) * D + col) * 8;
 #pragma unroll
-        for (int i = 0; i < DT; ++i) vf[i] = *reinterpret_cast<const uint4*>(v + 16 * i * 8);
+        for (int i = 0; i < DT; ++i) vf[i] = stream(v + 16 * i * 8);
     };
 
     int id0 = -1, id1 = -1;
@@ -333,20 +338,18 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = sc[j >> 2][j & 3] * d.scale_log2;
         const bool masked = base < t.full0 || base + kBlock > t.full1 || !listed0 || !listed1;
-        uint32_t seen = 0xff;                                          // by this lane's row, of its eight positions
-        uint32_t any = 0xff;                                           // by some row
+        uint32_t any = 0xff;                                           // of the lane's octet of values: seen by some row
         if (masked) {
-            seen = any = 0;
+            any = 0;
             const bool listed = g < 2 ? listed0 : listed1;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int pos = base + 8 * g + j;
-                if (listed && pos >= t.pos0 && pos < t.pos1) any |= 1u << j;
-                if (pos <= here && pos > row_low) seen |= 1u << j;
+                const int at = base + 8 * g + j;
+                if (listed && at >= t.pos0 && at < t.pos1) any |= 1u << j;
+                const int pos = base + 16 * (j >> 2) + 4 * g + (j & 3);
+                const bool seen = pos <= here && pos > row_low && pos < t.pos1 && (j < 4 ? listed0 : listed1);
+                x[j] = seen ? x[j] : kNegInf;
             }
-            seen &= any;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = (seen >> j) & 1 ? x[j] : kNegInf;
         }
         float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
         top = fmaxf(top, __shfl_xor(top, 16));
@@ -362,6 +365,15 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
             l += p0 + p1;
             pw[j / 2] = pack_bf16(p0, p1);
         }
+        // lanes 16 g have the weights of positions 4 g .. and 16 + 4 g ..; their values are those of 8 g ..
+        const auto to_octets = [](uint32_t& p, uint32_t& q) {
+            const auto u = __builtin_amdgcn_permlane32_swap(p, q, false, false);
+            const auto w = __builtin_amdgcn_permlane16_swap(u[0], u[1], false, false);
+            p = w[0];
+            q = w[1];
+        };
+        to_octets(pw[0], pw[2]);
+        to_octets(pw[1], pw[3]);
         const bf16x8 pf = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
 #pragma unroll
         for (int i = 0; i < DT; ++i)
@@ -746,8 +758,9 @@ __global__ __launch_bounds__((64 * waves_of<D, FORMS>()), (D > 128 ? 1 : 2)) voi
     if constexpr ((FORMS & FEW) != 0) attend_few<D, W>(d, few, blockIdx.x - (FORMS & LOT ? lot_blocks : 0), finder, sh.few);
 }
 
-// Adds up the parts of a cut tile, weights 2^(m - max m): a workgroup takes every gridDim.y-th row, four features a thread,
-// and what threads are left over share the parts.
+// Adds up the parts of a cut tile, weights 2^(m - max m), four features a thread.  Few parts: a thread has them all in flight,
+// and the threads that are left over take other rows; many: they share the parts, of every gridDim.y-th row.
+constexpr int kFewParts = 4;
 template <int D>
 __global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share lot, Share few, int lot_blocks) {
     constexpr int kQuads = D / 4, kGroups = kThreads / kQuads;
@@ -763,6 +776,38 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share lot, S
     const int rows = share.rows, part_floats = rows * (D + 2);
     const int64_t step = (int64_t)part_floats * d.kv_heads;
     const float* part = share.part + ((int64_t)t.slot * d.kv_heads + kvh) * part_floats;
+    const auto store = [&](int r, float top, float sum, const f32x4& v) {
+        const int ahead = quotient(d, t.rem0 + r);
+        const int64_t tok = t.token0 + ahead, h = kvh * d.group + t.rem0 + r - ahead * d.group;
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        *reinterpret_cast<uint2*>(d.out + tok * d.ldo + h * D + 4 * quad) =
+            make_uint2(pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv));
+        if (quad == 0 && d.lse) d.lse[tok * d.heads + h] = (top + __builtin_log2f(sum)) * 0.69314718055994530942f;
+    };
+    if (t.splits <= kFewParts) {                                       // a row for each group of threads
+        for (int r = blockIdx.y * kGroups + grp; r < t.rows; r += gridDim.y * kGroups) {
+            float tops[kFewParts], sums_of[kFewParts], top = kNegInf, sum = 0.0f;
+            f32x4 x[kFewParts], v = {0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < kFewParts; ++k) {
+                const float* p = part + min(k, t.splits - 1) * step;
+                tops[k] = p[rows * D + r];
+                sums_of[k] = p[rows * (D + 1) + r];
+                x[k] = *reinterpret_cast<const f32x4*>(p + r * D + 4 * quad);
+                top = fmaxf(top, tops[k]);
+            }
+            const float use = top == kNegInf ? 0.0f : top;
+#pragma unroll
+            for (int k = 0; k < kFewParts; ++k) {
+                if (k >= t.splits) break;
+                const float a = exp2_of(tops[k] - use);
+                sum = __fmaf_rn(sums_of[k], a, sum);
+                for (int j = 0; j < 4; ++j) v[j] = __fmaf_rn(x[k][j], a, v[j]);
+            }
+            store(r, top, sum, v);
+        }
+        return;
+    }
     for (int r = blockIdx.y; r < t.rows; r += gridDim.y) {
         float top = kNegInf;
         for (int k = tid; k < t.splits; k += kThreads) {
@@ -794,12 +839,7 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share lot, S
         __syncthreads();
         if (grp == 0) {
             for (int g = 1; g < kGroups; ++g) v += sums[g][quad];
-            const int ahead = quotient(d, t.rem0 + r);
-            const int64_t tok = t.token0 + ahead, h = kvh * d.group + t.rem0 + r - ahead * d.group;
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-            *reinterpret_cast<uint2*>(d.out + tok * d.ldo + h * D + 4 * quad) =
-                make_uint2(pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv));
-            if (quad == 0 && d.lse) d.lse[tok * d.heads + h] = (top + __builtin_log2f(sum)) * 0.69314718055994530942f;
+            store(r, top, sum, v);
         }
         __syncthreads();
     }
@@ -834,10 +874,10 @@ void lay_out(Space& space, int kv_heads, int head_dim, bool many, Share& lot, Sh
     lot.part = space.take<float>((size_t)2 * lot.target * kv_heads * kManyRows * (head_dim + 2));
 }
 Share few_share(int kv_heads, bool many) {
-    return Share{kFewRows, target_of(kFewTarget, kv_heads), kFewLeast, 0, many ? (int64_t)kFewRows : INT64_MAX, nullptr, nullptr, nullptr};
+    return Share{kFewRows, target_of(kFewTarget, kv_heads), kFewLeast, 0, 0, many ? (int64_t)kFewRows : INT64_MAX, nullptr, nullptr, nullptr};
 }
 Share lot_share(int kv_heads) {
-    return Share{kManyRows, target_of(kManyTarget, kv_heads), kManyLeast, kFewRows, INT64_MAX, nullptr, nullptr, nullptr};
+    return Share{kManyRows, target_of(kManyTarget, kv_heads), kManyLeast, 1, kFewRows, INT64_MAX, nullptr, nullptr, nullptr};
 }
 
 template <int D>
