@@ -596,10 +596,14 @@ def qblora_linear_decode(qw: QWeight, X: torch.Tensor, Y: torch.Tensor = None, w
 _BF16, _F32, _I32, _I64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
 
 
-def _address(t, dtype, *shape) -> int:
+def _address(t, dtype, shape) -> int:
     """Of a contiguous device array of this type and shape."""
-    assert t.dtype is dtype and t.is_cuda and t.is_contiguous() and t.shape == shape
+    assert t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous()
     return t.data_ptr()
+
+
+def _current_stream():
+    return _stream() if _raw_stream is None else _raw_stream(torch._C._cuda_getDevice())
 
 
 def _heads(t, T, heads, dim) -> int:
@@ -617,8 +621,8 @@ def _cache(k_cache, v_cache) -> bytes:
     head_dim, 8]."""
     pages, heads, octets, page, eight = k_cache.shape
     assert eight == 8
-    return _KV_CACHE.pack(pages, page, heads, octets * 8, _address(k_cache, _BF16, pages, heads, octets, page, 8),
-                          _address(v_cache, _BF16, pages, heads, page // 8, octets * 8, 8))
+    return _KV_CACHE.pack(pages, page, heads, octets * 8, _address(k_cache, _BF16, (pages, heads, octets, page, 8)),
+                          _address(v_cache, _BF16, (pages, heads, page // 8, octets * 8, 8)))
 
 
 def qblora_page_tables(context: torch.Tensor, fresh: torch.Tensor, page: int, free_pages: torch.Tensor, table: torch.Tensor,
@@ -637,13 +641,13 @@ def qblora_page_tables(context: torch.Tensor, fresh: torch.Tensor, page: int, fr
         starts = torch.empty(n + 1, dtype=_I32, device=dev) if starts is None else starts
         positions = torch.empty(tokens, dtype=_I32, device=dev) if positions is None else positions
         taken = torch.empty(1, dtype=_I32, device=dev) if taken is None else taken
-        p_starts, p_positions, p_taken = (_address(starts, _I32, n + 1), _address(positions, _I32, tokens),
-                                          _address(taken, _I32, 1))
+        p_starts, p_positions, p_taken = (_address(starts, _I32, (n + 1,)), _address(positions, _I32, (tokens,)),
+                                          _address(taken, _I32, (1,)))
     if slots is None:
         slots = torch.empty(tokens, dtype=_I64, device=dev)
-    rc = lib().qblora_page_tables(_address(context, _I32, n), _address(fresh, _I32, n), n, page,
-                                  _address(free_pages, _I32, n_free), n_free, _address(table, _I32, n, width), width, tokens,
-                                  p_starts, p_positions, _address(slots, _I64, tokens), p_taken, _stream())
+    rc = lib().qblora_page_tables(_address(context, _I32, (n,)), _address(fresh, _I32, (n,)), n, page,
+                                  _address(free_pages, _I32, (n_free,)), n_free, _address(table, _I32, (n, width)), width, tokens,
+                                  p_starts, p_positions, _address(slots, _I64, (tokens,)), p_taken, _current_stream())
     if rc:
         _check(rc, "qblora_page_tables")
     return starts, positions, slots, taken
@@ -662,7 +666,7 @@ def qblora_rope_frequencies(rot: int, base: float = 10000.0, kind: int = ROPE_PL
 
 def _rope(freq, interleaved, scale) -> bytes:
     half, = freq.shape
-    return _ROPE.pack(2 * half, interleaved, scale, _address(freq, _F32, half))
+    return _ROPE.pack(2 * half, interleaved, scale, _address(freq, _F32, (half,)))
 
 
 def _rope_call(name, q, k, positions, freq, interleaved, scale, q_out, k_out):
@@ -684,7 +688,7 @@ def _rope_call(name, q, k, positions, freq, interleaved, scale, q_out, k_out):
             ldk_out = _heads(k_out, T, kv_heads, dim)
         p_k, p_k_out = k.data_ptr(), k_out.data_ptr()
     rc = getattr(lib(), name)(_rope(freq, interleaved, scale), q.data_ptr(), ldq, heads, p_k, ldk, kv_heads, dim,
-                              _address(positions, _I32, T), T, q_out.data_ptr(), ld_out, p_k_out, ldk_out, _stream())
+                              _address(positions, _I32, (T,)), T, q_out.data_ptr(), ld_out, p_k_out, ldk_out, _current_stream())
     if rc:
         _check(rc, name)
     return q_out, k_out
@@ -716,8 +720,8 @@ def qblora_rope_cache(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positio
         ld_out = _heads(q_out, T, heads, dim)
     rc = lib().qblora_rope_cache(_rope(freq, interleaved, scale), q.data_ptr(), ldq, heads, k.data_ptr(),
                                  _heads(k, T, kv_heads, dim), v.data_ptr(), _heads(v, T, kv_heads, dim),
-                                 _address(positions, _I32, T), _address(slots, _I64, T), T, q_out.data_ptr(), ld_out,
-                                 _cache(k_cache, v_cache), _stream())
+                                 _address(positions, _I32, (T,)), _address(slots, _I64, (T,)), T, q_out.data_ptr(), ld_out,
+                                 _cache(k_cache, v_cache), _current_stream())
     if rc:
         _check(rc, "qblora_rope_cache")
     return q_out
@@ -750,10 +754,10 @@ def qblora_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torc
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     else:
         nbytes = workspace.numel() * workspace.element_size()
-    rc = L.qblora_paged_attention(q.data_ptr(), ldq, heads, cache, _address(table, _I32, n, width), width,
-                                  _address(starts, _I32, n + 1), _address(context, _I32, n), n, T, scale, window, max_new,
-                                  out.data_ptr(), ld_out, None if lse is None else _address(lse, _F32, T, heads),
-                                  workspace.data_ptr(), nbytes, _stream())
+    rc = L.qblora_paged_attention(q.data_ptr(), ldq, heads, cache, _address(table, _I32, (n, width)), width,
+                                  _address(starts, _I32, (n + 1,)), _address(context, _I32, (n,)), n, T, scale, window, max_new,
+                                  out.data_ptr(), ld_out, None if lse is None else _address(lse, _F32, (T, heads)),
+                                  workspace.data_ptr(), nbytes, _current_stream())
     if rc:
         _check(rc, "qblora_paged_attention")
     return out
@@ -764,17 +768,17 @@ def qblora_rms_norm_fwd(x: torch.Tensor, w: torch.Tensor, eps: float, residual: 
     """(y, total, rstd): the norm of total = x + residual (x itself without one); rstd, for the backward pass, is None unless
     `keep` is set or a tensor is given."""
     T, d = x.shape
-    p_x, p_residual = _address(x, _BF16, T, d), None
+    p_x, p_residual = _address(x, _BF16, (T, d)), None
     y = torch.empty_like(x) if y is None else y
     if residual is None:
         total = x
     else:
-        p_residual = _address(residual, _BF16, T, d)
+        p_residual = _address(residual, _BF16, (T, d))
         total = torch.empty_like(x) if total is None else total
     if keep and rstd is None:
         rstd = torch.empty(T, dtype=_F32, device=x.device)
-    rc = lib().qblora_rms_norm_fwd(p_x, p_residual, _address(w, _BF16, d), T, d, eps, _address(total, _BF16, T, d),
-                                   _address(y, _BF16, T, d), None if rstd is None else _address(rstd, _F32, T), _stream())
+    rc = lib().qblora_rms_norm_fwd(p_x, p_residual, _address(w, _BF16, (d,)), T, d, eps, _address(total, _BF16, (T, d)),
+                                   _address(y, _BF16, (T, d)), None if rstd is None else _address(rstd, _F32, (T,)), _current_stream())
     if rc:
         _check(rc, "qblora_rms_norm_fwd")
     return y, total, rstd
@@ -790,17 +794,17 @@ def qblora_rms_norm_bwd(total: torch.Tensor, w: torch.Tensor, rstd: torch.Tensor
     """(dx, dw): the gradients of the sum (x and residual alike) and of the weight."""
     T, d = total.shape
     dev = total.device
-    p_total = _address(total, _BF16, T, d)
+    p_total = _address(total, _BF16, (T, d))
     dx = torch.empty((T, d), dtype=_BF16, device=dev) if dx is None else dx
     p_dw = ws = None
     nbytes = 0
     if need_dw:
         dw = torch.empty(d, dtype=_F32, device=dev) if dw is None else dw
-        p_dw = _address(dw, _F32, d)
+        p_dw = _address(dw, _F32, (d,))
         ws = _workspace(lambda: lib().qblora_rms_norm_bwd_workspace_bytes(T, d), dev, workspace)
         nbytes = ws.numel() * ws.element_size()
-    rc = lib().qblora_rms_norm_bwd(p_total, _address(w, _BF16, d), _address(rstd, _F32, T), _address(dy, _BF16, T, d),
-                                   None if dtotal is None else _address(dtotal, _BF16, T, d), T, d, _address(dx, _BF16, T, d),
-                                   p_dw, _ptr(ws), nbytes, _stream())
+    rc = lib().qblora_rms_norm_bwd(p_total, _address(w, _BF16, (d,)), _address(rstd, _F32, (T,)), _address(dy, _BF16, (T, d)),
+                                   None if dtotal is None else _address(dtotal, _BF16, (T, d)), T, d, _address(dx, _BF16, (T, d)),
+                                   p_dw, _ptr(ws), nbytes, _current_stream())
     _check(rc, "qblora_rms_norm_bwd")
     return dx, (dw if need_dw else None)

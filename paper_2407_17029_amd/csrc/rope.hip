@@ -82,6 +82,23 @@ __global__ __launch_bounds__(kThreads) void k_rope_any(RopeDesc d) {
 
 constexpr int kHeads = 4;                      // in flight
 
+// Whether a token begins a run: its slot does not follow that of the token before, or begins an octet.
+__device__ __forceinline__ bool begins(const RopeDesc& d, int64_t t) {
+    if (t == 0 || t >= d.T) return true;
+    const int64_t slot = d.slots[t];
+    return (slot & 7) == 0 || d.slots[t - 1] != slot - 1;
+}
+// The runs that begin among the eight tokens from t0 on: what a workgroup owns, so that an octet of a page has one writer.
+// They end within seven more tokens.
+__device__ __forceinline__ void owned_tokens(const RopeDesc& d, int64_t t0, int64_t& from, int64_t& to) {
+    const int lane = threadIdx.x & 63;
+    const uint32_t at = (uint32_t)__ballot(lane < 16 && begins(d, t0 + lane));
+    from = t0 + (at & 0xff ? __builtin_ctz(at) : 8);
+    to = t0 + 8 + (at >> 8 ? __builtin_ctz(at >> 8) : 8);
+    if (to > d.T) to = d.T;
+    if (!(at & 0xff)) from = to;
+}
+
 struct RopeGrid { int qk_blocks, v_blocks; };  // of blockIdx.y
 
 template <int TB, bool PAIRS>
@@ -89,76 +106,85 @@ __global__ __launch_bounds__(kThreads) void k_rope(RopeDesc d, RopeGrid grid) {
     const int tid = threadIdx.x;
     const int64_t t0 = (int64_t)blockIdx.x * TB;
     if ((int)blockIdx.y < grid.qk_blocks) {
-        const int units = d.head_dim >> 4, turning = d.rot >> 4, lanes = kThreads / (TB * units);
+        // A thread's unit is two chunks of eight features, neighbouring lanes' chunks side by side: with half pairs chunk u of
+        // the first and of the second members (or two of the chunks behind them), else chunks u and u + units.
+        const int units = d.head_dim >> 4, chunks = d.rot >> 3, turning = d.rot >> 4, lanes = kThreads / (TB * units);
         const int tb = tid % TB, u = tid / TB % units, hl = tid / (TB * units);
-        const int64_t t = t0 + tb;
-        if (hl >= lanes || t >= d.T) return;
-        const bool turns = u < turning;
-        // the unit's two chunks of eight features
-        const int c0 = !PAIRS && turns ? u : 2 * u, c1 = !PAIRS && turns ? u + turning : 2 * u + 1;
-        float cs[8], sn[8];
-        if (turns) {
-            const int32_t p = d.positions[t];
+        const int c0 = PAIRS || u < turning ? u : turning + u, c1 = PAIRS ? u + units : u < turning ? u + turning : u + units;
+        const bool turns0 = c0 < chunks, turns1 = c1 < chunks;         // (half pairs: both or none)
+        int64_t from = t0, to = t0 + TB < d.T ? t0 + TB : d.T;
+        if (TB > 1) owned_tokens(d, t0, from, to);
+        if (hl >= lanes) return;
+        for (int64_t t = from + tb; t < to; t += TB) {
+            float cs[8], sn[8];
+            if (turns0) {
+                const int32_t p = d.positions[t];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                turn(p, d.freq[8 * u + j], d.scale, cs[j], sn[j]);
-                sn[j] *= d.sign;
+                for (int j = 0; j < 8; ++j) {
+                    const int pair = !PAIRS ? 8 * u + j : j < 4 ? 4 * c0 + j : 4 * c1 + j - 4;
+                    if (PAIRS && j >= 4 && !turns1) break;
+                    turn(p, d.freq[pair], d.scale, cs[j], sn[j]);
+                    sn[j] *= d.sign;
+                }
             }
-        }
-        const int64_t slot = d.kc ? d.slots[t] : -1;
-        const int all = d.heads + d.kv_heads;
-        for (int h0 = hl + (int)blockIdx.y * lanes * kHeads; h0 < all; h0 += grid.qk_blocks * lanes * kHeads) {
-            bf16x8_any x[kHeads][2];
+            const int64_t slot = d.kc ? d.slots[t] : -1;
+            const int all = d.heads + d.kv_heads;
+            for (int h0 = hl + (int)blockIdx.y * lanes * kHeads; h0 < all; h0 += grid.qk_blocks * lanes * kHeads) {
+                bf16x8_any x[kHeads][2];
 #pragma unroll
-            for (int i = 0; i < kHeads; ++i) {
-                const int h = h0 + i * lanes;
-                if (h >= all) continue;
-                const qblora_bf16* in = h < d.heads ? d.q + t * d.ldq + h * d.head_dim : d.k + t * d.ldk + (h - d.heads) * d.head_dim;
-                x[i][0] = *reinterpret_cast<const bf16x8_any*>(in + 8 * c0);
-                x[i][1] = *reinterpret_cast<const bf16x8_any*>(in + 8 * c1);
-            }
+                for (int i = 0; i < kHeads; ++i) {
+                    const int h = h0 + i * lanes;
+                    if (h >= all) continue;
+                    const qblora_bf16* in = h < d.heads ? d.q + t * d.ldq + h * d.head_dim : d.k + t * d.ldk + (h - d.heads) * d.head_dim;
+                    x[i][0] = *reinterpret_cast<const bf16x8_any*>(in + 8 * c0);
+                    x[i][1] = *reinterpret_cast<const bf16x8_any*>(in + 8 * c1);
+                }
 #pragma unroll
-            for (int i = 0; i < kHeads; ++i) {
-                const int h = h0 + i * lanes;
-                if (h >= all) continue;
-                bf16x8_any y[2] = {x[i][0], x[i][1]};
-                if (turns) {
+                for (int i = 0; i < kHeads; ++i) {
+                    const int h = h0 + i * lanes;
+                    if (h >= all) continue;
+                    bf16x8_any y[2] = {x[i][0], x[i][1]};
+                    if (turns0) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (PAIRS) {                                   // a dword is a pair
+                        for (int j = 0; j < 4; ++j) {
+                            if (PAIRS) {                                   // a dword is a pair
 #pragma unroll
-                            for (int c = 0; c < 2; ++c) {
-                                const float a = bf16_lo(x[i][c][j]), b = bf16_hi(x[i][c][j]);
-                                y[c][j] = pack_bf16(__fmaf_rn(a, cs[4 * c + j], -(b * sn[4 * c + j])), __fmaf_rn(b, cs[4 * c + j], a * sn[4 * c + j]));
+                                for (int c = 0; c < 2; ++c) {
+                                    if (c == 1 && !turns1) break;
+                                    const float a = bf16_lo(x[i][c][j]), b = bf16_hi(x[i][c][j]);
+                                    y[c][j] = pack_bf16(__fmaf_rn(a, cs[4 * c + j], -(b * sn[4 * c + j])), __fmaf_rn(b, cs[4 * c + j], a * sn[4 * c + j]));
+                                }
+                            } else {                                       // the two chunks are eight pairs
+                                const float a0 = bf16_lo(x[i][0][j]), a1 = bf16_hi(x[i][0][j]), b0 = bf16_lo(x[i][1][j]), b1 = bf16_hi(x[i][1][j]);
+                                const float k0 = cs[2 * j], k1 = cs[2 * j + 1], s0 = sn[2 * j], s1 = sn[2 * j + 1];
+                                y[0][j] = pack_bf16(__fmaf_rn(a0, k0, -(b0 * s0)), __fmaf_rn(a1, k1, -(b1 * s1)));
+                                y[1][j] = pack_bf16(__fmaf_rn(b0, k0, a0 * s0), __fmaf_rn(b1, k1, a1 * s1));
                             }
-                        } else {                                       // the two chunks are eight pairs
-                            const float a0 = bf16_lo(x[i][0][j]), a1 = bf16_hi(x[i][0][j]), b0 = bf16_lo(x[i][1][j]), b1 = bf16_hi(x[i][1][j]);
-                            const float k0 = cs[2 * j], k1 = cs[2 * j + 1], s0 = sn[2 * j], s1 = sn[2 * j + 1];
-                            y[0][j] = pack_bf16(__fmaf_rn(a0, k0, -(b0 * s0)), __fmaf_rn(a1, k1, -(b1 * s1)));
-                            y[1][j] = pack_bf16(__fmaf_rn(b0, k0, a0 * s0), __fmaf_rn(b1, k1, a1 * s1));
                         }
                     }
+                    qblora_bf16 *o0, *o1;
+                    if (h >= d.heads && d.kc) {
+                        if (!in_cache(d, slot)) continue;
+                        int place;
+                        qblora_bf16* out = d.kc + page_of(d, slot, h - d.heads, place);
+                        o0 = out + key_at(d, place, 8 * c0);
+                        o1 = out + key_at(d, place, 8 * c1);
+                    } else {
+                        qblora_bf16* out = h < d.heads ? d.q_out + t * d.ldq_out + h * d.head_dim : d.k_out + t * d.ldk_out + (h - d.heads) * d.head_dim;
+                        o0 = out + 8 * c0;
+                        o1 = out + 8 * c1;
+                    }
+                    *reinterpret_cast<bf16x8_any*>(o0) = y[0];
+                    *reinterpret_cast<bf16x8_any*>(o1) = y[1];
                 }
-                qblora_bf16 *o0, *o1;
-                if (h >= d.heads && d.kc) {
-                    if (!in_cache(d, slot)) continue;
-                    int place;
-                    qblora_bf16* out = d.kc + page_of(d, slot, h - d.heads, place);
-                    o0 = out + key_at(d, place, 8 * c0);
-                    o1 = out + key_at(d, place, 8 * c1);
-                } else {
-                    qblora_bf16* out = h < d.heads ? d.q_out + t * d.ldq_out + h * d.head_dim : d.k_out + t * d.ldk_out + (h - d.heads) * d.head_dim;
-                    o0 = out + 8 * c0;
-                    o1 = out + 8 * c1;
-                }
-                *reinterpret_cast<bf16x8_any*>(o0) = y[0];
-                *reinterpret_cast<bf16x8_any*>(o1) = y[1];
             }
         }
         return;
     }
 
-    // values: four features a thread, and the run of tokens whose slots follow each other up to the end of an octet
+    // Values: four features a thread, and the run of tokens whose slots follow each other up to the end of an octet.  A whole
+    // octet goes through LDS, so that a store is 64 features side by side rather than every fourth.
+    __shared__ uint4 turned[kThreads / 64][TB > 1 ? 256 : 1];
     const int first = ((int)blockIdx.y - grid.qk_blocks) * kThreads + tid, step = grid.v_blocks * kThreads;
     const int quads = d.kv_heads * d.head_dim / 4;
     for (int b = 0; b < TB && t0 + b < d.T; ++b) {
@@ -169,32 +195,55 @@ __global__ __launch_bounds__(kThreads) void k_rope(RopeDesc d, RopeGrid grid) {
             if (t > 0 && (slot & 7) && d.slots[t - 1] == slot - 1) continue;             // in another token's run
             while (((slot + run) & 7) && t + run < d.T && d.slots[t + run] == slot + run) ++run;
         }
-        for (int i = first; i < quads; i += step) {
-            const int f = 4 * i % d.head_dim, h = 4 * i / d.head_dim;
-            int place;
-            qblora_bf16* out = d.vc + page_of(d, slot, h, place);
-            out += value_at(d, place, f);
-            const qblora_bf16* in = d.v + t * d.ldv + 4 * i;
-            if (run == 8) {
-                bf16x4_any x[8];
+        int place;
+        (void)page_of(d, slot, 0, place);
+        if (TB > 1 && run == 8) {
+            const int lane = tid & 63;
+            uint4* mine = turned[tid >> 6];
+            for (int i = first; i - lane < quads; i += step) {
+                if (i < quads) {
+                    const qblora_bf16* in = d.v + t * d.ldv + 4 * i;
+                    bf16x4_any x[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = *reinterpret_cast<const bf16x4_any*>(in + k * d.ldv);
+                    for (int k = 0; k < 8; ++k) x[k] = *reinterpret_cast<const bf16x4_any*>(in + k * d.ldv);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t y[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t lo = x[2 * k][j >> 1], hi = x[2 * k + 1][j >> 1];
+                            y[k] = j & 1 ? (lo >> 16) | (hi & 0xffff0000u) : (lo & 0xffffu) | (hi << 16);
+                        }
+                        // feature 4 lane + j, its low bits turned by the lane: 16 lanes to every bank
+                        mine[(4 * lane + j) ^ ((lane >> 1) & 3)] = make_uint4(y[0], y[1], y[2], y[3]);
+                    }
+                }
+                __builtin_amdgcn_wave_barrier();
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    bf16x8_any y;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t lo = x[2 * k][j >> 1], hi = x[2 * k + 1][j >> 1];
-                        y[k] = j & 1 ? (lo >> 16) | (hi & 0xffff0000u) : (lo & 0xffffu) | (hi << 16);
+                    const int at = 64 * j + lane, f = 4 * (i - lane) + at;               // feature of all heads'
+                    if (f < 4 * quads) {
+                        const int h = f / d.head_dim;
+                        int same;
+                        qblora_bf16* out = d.vc + page_of(d, slot, h, same) + value_at(d, place, f - h * d.head_dim);
+                        const uint4 y = mine[at ^ ((at >> 3) & 3)];
+                        bf16x8_any o = {y.x, y.y, y.z, y.w};
+                        *reinterpret_cast<bf16x8_any*>(out) = o;
                     }
-                    *reinterpret_cast<bf16x8_any*>(out + 8 * j) = y;
                 }
-            } else {
-                for (int k = 0; k < run; ++k) {
-                    const bf16x4_any x = *reinterpret_cast<const bf16x4_any*>(in + k * d.ldv);
+                __builtin_amdgcn_wave_barrier();
+            }
+            continue;
+        }
+        for (int i = first; i < quads; i += step) {
+            const int h = 4 * i / d.head_dim, f = 4 * i - h * d.head_dim;
+            int same;
+            qblora_bf16* out = d.vc + page_of(d, slot, h, same) + value_at(d, place, f);
+            const qblora_bf16* in = d.v + t * d.ldv + 4 * i;
+            for (int k = 0; k < run; ++k) {
+                const bf16x4_any x = *reinterpret_cast<const bf16x4_any*>(in + k * d.ldv);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) out[8 * j + k] = (qblora_bf16)(j & 1 ? x[j >> 1] >> 16 : x[j >> 1]);
-                }
+                for (int j = 0; j < 4; ++j) out[8 * j + k] = (qblora_bf16)(j & 1 ? x[j >> 1] >> 16 : x[j >> 1]);
             }
         }
     }
