@@ -20,6 +20,7 @@
 // of all requests, which gives the number of positions that a workgroup takes if there are to be `target` of them, and finds
 // its own (request, rows, range of positions) from the prefix sums.  A context that is cut this way leaves partial results
 // in the workspace, which k_attn_join adds up.
+#include <algorithm>
 #include <climits>
 #include <type_traits>
 
@@ -888,7 +889,13 @@ int launch(const AttnDesc& d, hipStream_t st) {
     lay_out(space, d.kv_heads, D, many, lot, few);
     const int64_t few_tiles = many ? d.n : (int64_t)d.T * d.group / kFewRows + d.n;
     const int64_t lot_tiles = many ? (int64_t)d.T * d.group / kManyRows + d.n : 0;
-    const int64_t lot_blocks = many ? (lot_tiles + lot.target) * d.kv_heads : 0, blocks = lot_blocks + (few_tiles + few.target) * d.kv_heads;
+    // No more units than the tiles and the target, nor than the longest row of the table allows.
+    const int64_t blocks_of_row = (((int64_t)d.width << d.page_shift) + kBlock - 1) / kBlock + 1;
+    const auto units = [&](int64_t tiles, const Share& w) {
+        const int64_t most = tiles * ((blocks_of_row + w.least - 1) / w.least);
+        return std::max<int64_t>(std::min(most, tiles + 2 * w.target), 1) * d.kv_heads;
+    };
+    const int64_t lot_blocks = many ? units(lot_tiles, lot) : 0, blocks = lot_blocks + units(few_tiles, few);
     if (blocks > INT32_MAX) return QBLORA_ERR_UNSUPPORTED;
     const auto go = [&](auto kernel, int waves, int64_t count) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(64 * waves), 0, st, d, lot, few, (int)lot_blocks);

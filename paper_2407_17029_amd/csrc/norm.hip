@@ -12,26 +12,30 @@ namespace qblora {
 
 namespace {
 
-// chunk c of a row of d: eight bf16 as four dwords, 0 behind the end
-__device__ __forceinline__ uint4 load_chunk(const qblora_bf16* row, int c, int d) {
-    if (8 * c + 8 <= d) {
-        const bf16x8_any v = *reinterpret_cast<const bf16x8_any*>(row + 8 * c);
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// The eight features from e on of a row of d, as four dwords, 0 behind the end
+__device__ __forceinline__ uint4 load_chunk(const qblora_bf16* row, int e, int d) {
+    if (e + 8 <= d) {
+        const bf16x8_any v = *reinterpret_cast<const bf16x8_any*>(row + e);
         return make_uint4(v[0], v[1], v[2], v[3]);
     }
     uint32_t w[4] = {0, 0, 0, 0};
     for (int j = 0; j < 8; ++j)
-        if (8 * c + j < d) w[j / 2] |= (uint32_t)row[8 * c + j] << (16 * (j & 1));
+        if (e + j < d) w[j / 2] |= (uint32_t)row[e + j] << (16 * (j & 1));
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void store_chunk(qblora_bf16* row, int c, int d, uint4 v) {
-    if (8 * c + 8 <= d) {
-        bf16x8_any o = {v.x, v.y, v.z, v.w};
-        *reinterpret_cast<bf16x8_any*>(row + 8 * c) = o;
+template <bool PAST>
+__device__ __forceinline__ void store_chunk(qblora_bf16* row, int e, int d, uint4 v) {
+    if (e + 8 <= d) {
+        const bf16x8_any o = {v.x, v.y, v.z, v.w};
+        if (PAST) __builtin_nontemporal_store(o, reinterpret_cast<bf16x8_any*>(row + e));
+        else *reinterpret_cast<bf16x8_any*>(row + e) = o;
         return;
     }
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
     for (int j = 0; j < 8; ++j)
-        if (8 * c + j < d) row[8 * c + j] = (qblora_bf16)(w[j / 2] >> (16 * (j & 1)));
+        if (e + j < d) row[e + j] = (qblora_bf16)(w[j / 2] >> (16 * (j & 1)));
 }
 __device__ __forceinline__ uint32_t word(const uint4& v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
 __device__ __forceinline__ void set_word(uint4& v, int j, uint32_t x) {
@@ -50,18 +54,18 @@ __device__ __forceinline__ float block_sum(float v, float* slots) {
     return v;
 }
 
-template <int NC>
+template <int NC, bool PAST>                  // PAST: stores go past the caches
 __global__ __launch_bounds__(1024) void k_rms_norm(NormDesc a) {
     __shared__ float slots[16];
     const int64_t row = blockIdx.x;
-    const int d = a.d, chunks = (d + 7) >> 3;
+    const int d = a.d;
     const qblora_bf16* x = a.x + row * d;
     uint4 v[NC], w[NC];
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-        const int c = threadIdx.x + i * blockDim.x;
+        const int c = 8 * (threadIdx.x + i * blockDim.x);
         v[i] = w[i] = make_uint4(0, 0, 0, 0);
-        if (c < chunks) {
+        if (c < d) {
             v[i] = load_chunk(x, c, d);
             w[i] = load_chunk(a.w, c, d);
         }
@@ -70,15 +74,15 @@ __global__ __launch_bounds__(1024) void k_rms_norm(NormDesc a) {
         const qblora_bf16* res = a.residual + row * d;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            const int c = threadIdx.x + i * blockDim.x;
-            if (c >= chunks) continue;
+            const int c = 8 * (threadIdx.x + i * blockDim.x);
+            if (c >= d) continue;
             const uint4 r = load_chunk(res, c, d);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const uint32_t p = word(v[i], j), q = word(r, j);
                 set_word(v[i], j, pack_bf16(bf16_lo(p) + bf16_lo(q), bf16_hi(p) + bf16_hi(q)));
             }
-            store_chunk(a.total + row * d, c, d, v[i]);
+            store_chunk<PAST>(a.total + row * d, c, d, v[i]);
         }
     }
     float sum = 0.0f;
@@ -95,28 +99,28 @@ __global__ __launch_bounds__(1024) void k_rms_norm(NormDesc a) {
     if (a.rstd && threadIdx.x == 0) a.rstd[row] = r;
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-        const int c = threadIdx.x + i * blockDim.x;
-        if (c >= chunks) continue;
+        const int c = 8 * (threadIdx.x + i * blockDim.x);
+        if (c >= d) continue;
         uint4 o;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint32_t p = word(v[i], j), q = word(w[i], j);
             set_word(o, j, pack_bf16(bf16_lo(p) * r * bf16_lo(q), bf16_hi(p) * r * bf16_hi(q)));
         }
-        store_chunk(a.y + row * d, c, d, o);
+        store_chunk<PAST>(a.y + row * d, c, d, o);
     }
 }
 
-template <int NC>
+template <int NC, bool PAST>                  // PAST: stores go past the caches
 __global__ __launch_bounds__(1024) void k_rms_norm_bwd(NormBackDesc a) {
     __shared__ float slots[2][16];
-    const int d = a.d, chunks = (d + 7) >> 3;
+    const int d = a.d;
     uint4 w[NC];
     float dw[NC][8];
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-        const int c = threadIdx.x + i * blockDim.x;
-        w[i] = c < chunks ? load_chunk(a.w, c, d) : make_uint4(0, 0, 0, 0);
+        const int c = 8 * (threadIdx.x + i * blockDim.x);
+        w[i] = c < d ? load_chunk(a.w, c, d) : make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int j = 0; j < 8; ++j) dw[i][j] = 0.0f;
     }
@@ -126,9 +130,9 @@ __global__ __launch_bounds__(1024) void k_rms_norm_bwd(NormBackDesc a) {
         uint4 t[NC], y[NC], e[NC];
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            const int c = threadIdx.x + i * blockDim.x;
+            const int c = 8 * (threadIdx.x + i * blockDim.x);
             t[i] = y[i] = e[i] = make_uint4(0, 0, 0, 0);
-            if (c < chunks) {
+            if (c < d) {
                 t[i] = load_chunk(a.total + row * d, c, d);
                 y[i] = load_chunk(a.dy + row * d, c, d);
                 if (a.dtotal) e[i] = load_chunk(a.dtotal + row * d, c, d);
@@ -147,8 +151,8 @@ __global__ __launch_bounds__(1024) void k_rms_norm_bwd(NormBackDesc a) {
         const float mean = block_sum(sum / (float)d, slots[turn]);
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            const int c = threadIdx.x + i * blockDim.x;
-            if (c >= chunks) continue;
+            const int c = 8 * (threadIdx.x + i * blockDim.x);
+            if (c >= d) continue;
             uint4 o;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -157,64 +161,82 @@ __global__ __launch_bounds__(1024) void k_rms_norm_bwd(NormBackDesc a) {
                 const float hi = __fmaf_rn(-bf16_hi(tp) * r, mean, bf16_hi(yp) * bf16_hi(wp));
                 set_word(o, j, pack_bf16(__fmaf_rn(r, lo, bf16_lo(ep)), __fmaf_rn(r, hi, bf16_hi(ep))));
             }
-            store_chunk(a.dx + row * d, c, d, o);
+            store_chunk<PAST>(a.dx + row * d, c, d, o);
         }
     }
     if (!a.part) return;
+    float* part = a.part + (int64_t)blockIdx.x * d;
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-        const int c = threadIdx.x + i * blockDim.x;
+        const int c = 8 * (threadIdx.x + i * blockDim.x);
+        if (c + 8 <= d) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (8 * c + j < d) a.part[(int64_t)blockIdx.x * d + 8 * c + j] = dw[i][j];
+            for (int j = 0; j < 8; j += 4) {
+                const f32x4_any v = {dw[i][j], dw[i][j + 1], dw[i][j + 2], dw[i][j + 3]};
+                *reinterpret_cast<f32x4_any*>(part + c + j) = v;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c + j < d) part[c + j] = dw[i][j];
+        }
     }
 }
 
-// dw[c] = sum over the rows of `part`, 16 columns and 16 rows at a time
-__global__ __launch_bounds__(256) void k_rms_norm_dw(const float* __restrict__ part, int rows, int d, float* __restrict__ dw) {
-    __shared__ float sums[16][17];
+// dw[c] = sum over the rows of `part`, 16 columns and 64 rows at a time
+__global__ __launch_bounds__(1024) void k_rms_norm_dw(const float* __restrict__ part, int rows, int d, float* __restrict__ dw) {
+    __shared__ float sums[64][17];
     const int c = blockIdx.x * 16 + (threadIdx.x & 15), r0 = threadIdx.x >> 4;
     float s = 0.0f;
     if (c < d)
-        for (int r = r0; r < rows; r += 16) s += part[(int64_t)r * d + c];
+#pragma unroll 4
+        for (int r = r0; r < rows; r += 64) s += part[(int64_t)r * d + c];
     sums[r0][threadIdx.x & 15] = s;
     __syncthreads();
     if (r0 == 0 && c < d) {
         s = 0.0f;
-        for (int i = 0; i < 16; ++i) s += sums[i][threadIdx.x & 15];
+        for (int i = 0; i < 64; ++i) s += sums[i][threadIdx.x & 15];
         dw[c] = s;
     }
 }
 
-int threads_of(int d) {
+struct Plan { int threads, chunks; };          // threads of a row, chunks of a thread
+Plan plan_of(int d) {
     const int chunks = (d + 7) / 8, t = (chunks + 63) / 64 * 64;
-    return t < 1024 ? t : 1024;
+    return {t < 1024 ? t : 1024, t <= 1024 ? 1 : 2};
 }
+// From so many bytes an array on, no L2 holds the outputs when they are read: 8192 rows of 8192 both ways 199 us through the
+// caches, 190 past them; 2001 rows of 4096 31 and 28.
+constexpr int64_t kPastBytes = 8 << 20;
+bool past_caches(int64_t T, int d) { return T * d * 2 >= kPastBytes; }
 
 }  // namespace
 
 int launch_rms_norm(const NormDesc& a, hipStream_t st) {
-    const int threads = threads_of(a.d), nc = ((a.d + 7) / 8 + threads - 1) / threads;
-    const dim3 grid((unsigned)a.T);
-    if (nc == 1) hipLaunchKernelGGL(k_rms_norm<1>, grid, dim3(threads), 0, st, a);
-    else hipLaunchKernelGGL(k_rms_norm<2>, grid, dim3(threads), 0, st, a);
+    const Plan p = plan_of(a.d);
+    const bool past = past_caches(a.T, a.d);
+    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)a.T), dim3(p.threads), 0, st, a); };
+    if (p.chunks == 1) go(past ? k_rms_norm<1, true> : k_rms_norm<1, false>);
+    else go(past ? k_rms_norm<2, true> : k_rms_norm<2, false>);
     return launch_status();
 }
 
 int64_t rms_norm_bwd_parts(int64_t T, int d) {
-    const int64_t full = 256 * 1024 / threads_of(d), some = (T + 7) / 8;
+    const int64_t full = 256 * 1024 / plan_of(d).threads;                // what the chip holds at once
+    const int64_t some = (T + 3) / 4;                                    // four rows at least: 8001 x 600 25 us, with one 28.7
     return some < full ? some : full;
 }
 
 int launch_rms_norm_bwd(const NormBackDesc& a, hipStream_t st) {
-    const int threads = threads_of(a.d), nc = ((a.d + 7) / 8 + threads - 1) / threads;
+    const Plan p = plan_of(a.d);
+    const bool past = past_caches(a.T, a.d);
     const int rows = (int)rms_norm_bwd_parts(a.T, a.d);
+    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(rows), dim3(p.threads), 0, st, a); };
     if (rows) {
-        const dim3 grid(rows);
-        if (nc == 1) hipLaunchKernelGGL(k_rms_norm_bwd<1>, grid, dim3(threads), 0, st, a);
-        else hipLaunchKernelGGL(k_rms_norm_bwd<2>, grid, dim3(threads), 0, st, a);
+        if (p.chunks == 1) go(past ? k_rms_norm_bwd<1, true> : k_rms_norm_bwd<1, false>);
+        else go(past ? k_rms_norm_bwd<2, true> : k_rms_norm_bwd<2, false>);
     }
-    if (a.dw) hipLaunchKernelGGL(k_rms_norm_dw, dim3((a.d + 15) / 16), dim3(256), 0, st, a.part, rows, a.d, a.dw);
+    if (a.dw) hipLaunchKernelGGL(k_rms_norm_dw, dim3((a.d + 15) / 16), dim3(1024), 0, st, a.part, rows, a.d, a.dw);
     return launch_status();
 }
 
