@@ -30,7 +30,7 @@ namespace qblora {
 
 namespace {
 
-constexpr int kThreads = 256, kMostWaves = 8;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kFewRows = 16;
 constexpr int kBlock = 32;                     // positions of a step
 constexpr int kManyRows = 128;
@@ -111,11 +111,11 @@ __device__ __forceinline__ Units units_of(const Cost& c, int64_t per, int slack)
 // k_attn_join looks for it.  All threads call it.  Up to 64 requests every wave finds it by itself, a request a lane; more
 // are taken a workgroup's threads at a time.
 struct Finder {
-    int64_t sums[kMostWaves];
-    int ends[2][kMostWaves], found[6];
+    int64_t sums[kWaves];
+    int ends[2][kWaves], found[6];
 };
 __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share, int want, bool first, Finder& f, Unit& u) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, threads = blockDim.x, waves = threads >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (d.n <= 64) {
         Cost c{0, 0};
         if (lane < d.n) c = cost_of(d, lane, share);
@@ -136,7 +136,7 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
         return true;
     }
     int64_t all = 0;
-    for (int i = tid; i < d.n; i += threads) {
+    for (int i = tid; i < d.n; i += kThreads) {
         const Cost c = cost_of(d, i, share);
         all += (int64_t)c.tiles * c.blocks;
     }
@@ -145,10 +145,10 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
     if (tid == 0) f.found[0] = -1;
     __syncthreads();
     all = 0;
-    for (int w = 0; w < waves; ++w) all += f.sums[w];
+    for (int w = 0; w < kWaves; ++w) all += f.sums[w];
     const int64_t per = blocks_per_unit(all, share);
     int units = 0, cuts = 0;                                           // in front of these requests
-    for (int base = 0; base < d.n; base += threads) {
+    for (int base = 0; base < d.n; base += kThreads) {
         const int i = base + tid;
         Cost c{0, 0};
         if (i < d.n) c = cost_of(d, i, share);
@@ -157,7 +157,7 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
         __syncthreads();
         if (lane == 63) { f.ends[0][wave] = a; f.ends[1][wave] = b; }
         __syncthreads();
-        for (int w = 0; w < waves; ++w) {
+        for (int w = 0; w < kWaves; ++w) {
             if (w == wave) { a += units; b += cuts; }
             units += f.ends[0][w];
             cuts += f.ends[1][w];
@@ -237,14 +237,14 @@ __device__ __forceinline__ uint4 stream(const qblora_bf16* p) {
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-template <int D, int W>
+template <int D>
 struct FewShared {
-    float o[W][kFewRows][D + 4];
-    float m[W][kFewRows], l[W][kFewRows];
+    float o[kWaves][kFewRows][D + 4];
+    float m[kWaves][kFewRows], l[kWaves][kFewRows];
 };
 
-template <int D, int W>
-__device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share, int block, Finder& finder, FewShared<D, W>& sh) {
+template <int D>
+__device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share, int block, Finder& finder, FewShared<D>& sh) {
     constexpr int KS = D / 32, DT = D / 16;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, col = lane & 15;
     const int kvh = block % d.kv_heads;
@@ -274,7 +274,7 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
     const int shift = d.page_shift, page = 1 << shift;
     const int64_t page_elems = (int64_t)d.kv_heads * D << shift, head_elems = ((int64_t)kvh * D) << shift;
     const int32_t* table = d.table + (int64_t)u.request * d.width;
-    const int steps = b0 + wave < b1 ? (b1 - b0 - wave + W - 1) / W : 0;
+    const int steps = b0 + wave < b1 ? (b1 - b0 - wave + kWaves - 1) / kWaves : 0;
 
     f32x4 o[DT];
 #pragma unroll
@@ -288,7 +288,7 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
     // pages of a step (step 64 k first)
     auto find_pages = [&](int step, int& id0, int& id1) {
         if ((step & 63) == 0) {
-            const int pos = (b0 + wave + W * (step + lane)) * kBlock;
+            const int pos = (b0 + wave + kWaves * (step + lane)) * kBlock;
             ids0 = ids1 = -1;
             if (pos < t.pos1) ids0 = table[pos >> shift];
             if (pos + 16 < t.pos1) ids1 = table[(pos + 16) >> shift];
@@ -299,7 +299,7 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
         id1 = __builtin_amdgcn_readlane(ids1, step & 63);
     };
     auto load_keys = [&](int step, int id0, int id1) {
-        const int base = (b0 + wave + W * step) * kBlock;
+        const int base = (b0 + wave + kWaves * step) * kBlock;
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
             const int id = max(tt == 0 ? id0 : id1, 0);
@@ -309,7 +309,7 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
         }
     };
     auto load_values = [&](int step, int id0, int id1) {
-        const int base = (b0 + wave + W * step) * kBlock;
+        const int base = (b0 + wave + kWaves * step) * kBlock;
         const int id = max(g < 2 ? id0 : id1, 0);
         const qblora_bf16* v = d.vc + id * page_elems + head_elems + ((((base + 8 * g) & (page - 1)) >> 3) * D + col) * 8;
 #pragma unroll
@@ -323,7 +323,7 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
         load_values(0, id0, id1);
     }
     for (int step = 0; step < steps; ++step) {
-        const int base = (b0 + wave + W * step) * kBlock;
+        const int base = (b0 + wave + kWaves * step) * kBlock;
         const bool listed0 = id0 >= 0, listed1 = id1 >= 0;
         f32x4 sc[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
 #pragma unroll
@@ -417,14 +417,14 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
         for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4*>(&sh.o[wave][col][16 * i + 4 * g]) = o[i];
     __syncthreads();
     float* part = u.splits > 1 ? share.part + ((int64_t)u.slot * d.kv_heads + kvh) * (kFewRows * (D + 2)) : nullptr;
-    for (int i = tid; i < t.rows * (D / 4); i += 64 * W) {
+    for (int i = tid; i < t.rows * (D / 4); i += kThreads) {
         const int r = i / (D / 4), f = 4 * (i % (D / 4));
         float top = kNegInf;
-        for (int w = 0; w < W; ++w) top = fmaxf(top, sh.m[w][r]);
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sh.m[w][r]);
         const float use = top == kNegInf ? 0.0f : top;
         float sum = 0.0f;
         f32x4 v = {0, 0, 0, 0};
-        for (int w = 0; w < W; ++w) {
+        for (int w = 0; w < kWaves; ++w) {
             const float a = exp2_of(sh.m[w][r] - use);
             sum = __fmaf_rn(sh.l[w][r], a, sum);
             const f32x4 x = *reinterpret_cast<const f32x4*>(&sh.o[w][r][f]);
@@ -489,7 +489,7 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
     constexpr int kTile = ManyShared<D>::kTile, kTileBytes = ManyShared<D>::kTileBytes;
     constexpr int KS = D / 16, DT = D / 32, TT = kTile / 32;
     constexpr int PS = kTile / 16, kSixteen = D * 32;                  // a tile's sixteens of positions, bytes of one
-    constexpr int kSharers = 4 / PS, kCopies = kSixteen / 1024 / kSharers;     // waves that copy a sixteen, copies of each
+    constexpr int kSharers = kWaves / PS, kCopies = kSixteen / 1024 / kSharers;     // waves that copy a sixteen, copies of each
     constexpr int kBatch = 64 / PS;                                    // tiles whose pages a wave looks up at once
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
     const int kvh = block % d.kv_heads;
@@ -744,24 +744,21 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
 // One of the forms, or both, so that chunks and single tokens of a batch run beside each other.
 enum { FEW = 1, LOT = 2, BOTH = 3 };
 template <int D, int FORMS>
-constexpr int waves_of() { return 4; }
-template <int D, int FORMS>
-__global__ __launch_bounds__((64 * waves_of<D, FORMS>()), (D > 128 ? 1 : 2)) void k_attn(AttnDesc d, Share lot, Share few, int lot_blocks) {
-    constexpr int W = waves_of<D, FORMS>();
+__global__ __launch_bounds__(kThreads, (D > 128 ? 1 : 2)) void k_attn(AttnDesc d, Share lot, Share few, int lot_blocks) {
     __shared__ Finder finder;
     __shared__ union Shared {
         std::conditional_t<(FORMS & LOT) != 0, ManyShared<D>, char> many;
-        std::conditional_t<(FORMS & FEW) != 0, FewShared<D, W>, char> few;
+        std::conditional_t<(FORMS & FEW) != 0, FewShared<D>, char> few;
     } sh;
     if constexpr ((FORMS & LOT) != 0) {
         if (FORMS == LOT || (int)blockIdx.x < lot_blocks) return attend_many<D>(d, lot, blockIdx.x, finder, sh.many);
     }
-    if constexpr ((FORMS & FEW) != 0) attend_few<D, W>(d, few, blockIdx.x - (FORMS & LOT ? lot_blocks : 0), finder, sh.few);
+    if constexpr ((FORMS & FEW) != 0) attend_few<D>(d, few, blockIdx.x - (FORMS & LOT ? lot_blocks : 0), finder, sh.few);
 }
 
 // Adds up the parts of a cut tile, weights 2^(m - max m), four features a thread.  Few parts: a thread has them all in flight,
 // and the threads that are left over take other rows; many: they share the parts, of every gridDim.y-th row.
-constexpr int kFewParts = 4;
+constexpr int kFewParts = 4, kPartsAhead = 4;
 template <int D>
 __global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share lot, Share few, int lot_blocks) {
     constexpr int kQuads = D / 4, kGroups = kThreads / kQuads;
@@ -771,8 +768,9 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share lot, S
     const bool of_lot = (int)blockIdx.x < lot_blocks;
     const Share& share = of_lot ? lot : few;
     const int block = blockIdx.x - (of_lot ? 0 : lot_blocks), kvh = block % d.kv_heads, number = block / d.kv_heads;
-    if (number >= *share.cuts) return;
+    const int cuts = *share.cuts;                                      // (both loads in flight: the grid fits the list)
     const CutTile t = share.cut[number];
+    if (number >= cuts) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, quad = tid % kQuads, grp = tid / kQuads;
     const int rows = share.rows, part_floats = rows * (D + 2);
     const int64_t step = (int64_t)part_floats * d.kv_heads;
@@ -810,6 +808,10 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share lot, S
         return;
     }
     for (int r = blockIdx.y; r < t.rows; r += gridDim.y) {
+        f32x4 ahead[kPartsAhead];                                      // in flight while the weights are made
+#pragma unroll
+        for (int i = 0; i < kPartsAhead; ++i)
+            ahead[i] = *reinterpret_cast<const f32x4*>(part + min(grp + i * kGroups, t.splits - 1) * step + r * D + 4 * quad);
         float top = kNegInf;
         for (int k = tid; k < t.splits; k += kThreads) {
             weight[k] = part[k * step + rows * D + r];
@@ -830,8 +832,14 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share lot, S
         __syncthreads();
         sum = (sum_of[0] + sum_of[1]) + (sum_of[2] + sum_of[3]);
         f32x4 v = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < kPartsAhead; ++i) {
+            if (grp + i * kGroups >= t.splits) break;
+            const float a = weight[grp + i * kGroups];
+            for (int j = 0; j < 4; ++j) v[j] = __fmaf_rn(ahead[i][j], a, v[j]);
+        }
 #pragma unroll 4
-        for (int k = grp; k < t.splits; k += kGroups) {
+        for (int k = grp + kPartsAhead * kGroups; k < t.splits; k += kGroups) {
             const float a = weight[k];
             const f32x4 x = *reinterpret_cast<const f32x4*>(part + k * step + r * D + 4 * quad);
             for (int j = 0; j < 4; ++j) v[j] = __fmaf_rn(x[j], a, v[j]);
@@ -897,16 +905,16 @@ int launch(const AttnDesc& d, hipStream_t st) {
     };
     const int64_t lot_blocks = many ? units(lot_tiles, lot) : 0, blocks = lot_blocks + units(few_tiles, few);
     if (blocks > INT32_MAX) return QBLORA_ERR_UNSUPPORTED;
-    const auto go = [&](auto kernel, int waves, int64_t count) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(64 * waves), 0, st, d, lot, few, (int)lot_blocks);
+    const auto go = [&](auto kernel, int64_t count) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(kThreads), 0, st, d, lot, few, (int)lot_blocks);
     };
     if (!many) {
-        go(k_attn<D, FEW>, waves_of<D, FEW>(), blocks);
+        go(k_attn<D, FEW>, blocks);
     } else if constexpr (D <= 128) {
-        go(k_attn<D, BOTH>, waves_of<D, BOTH>(), blocks);
+        go(k_attn<D, BOTH>, blocks);
     } else {                                                           // (one kernel of both would not have the registers)
-        go(k_attn<D, LOT>, waves_of<D, LOT>(), lot_blocks);
-        go(k_attn<D, FEW>, waves_of<D, FEW>(), blocks - lot_blocks);
+        go(k_attn<D, LOT>, lot_blocks);
+        go(k_attn<D, FEW>, blocks - lot_blocks);
     }
     // no context is long enough for a cut
     if ((int64_t)d.width << d.page_shift <= kFewLeast * kBlock) return launch_status();
