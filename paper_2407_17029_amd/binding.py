@@ -645,9 +645,12 @@ def qblora_page_tables(context: torch.Tensor, fresh: torch.Tensor, page: int, fr
                                           _address(taken, _I32, (1,)))
     if slots is None:
         slots = torch.empty(tokens, dtype=_I64, device=dev)
+        p_slots = slots.data_ptr()
+    else:
+        p_slots = _address(slots, _I64, (tokens,))
     rc = lib().qblora_page_tables(_address(context, _I32, (n,)), _address(fresh, _I32, (n,)), n, page,
                                   _address(free_pages, _I32, (n_free,)), n_free, _address(table, _I32, (n, width)), width, tokens,
-                                  p_starts, p_positions, _address(slots, _I64, (tokens,)), p_taken, _current_stream())
+                                  p_starts, p_positions, p_slots, p_taken, _current_stream())
     if rc:
         _check(rc, "qblora_page_tables")
     return starts, positions, slots, taken
@@ -669,11 +672,17 @@ def _rope(freq, interleaved, scale) -> bytes:
     return _ROPE.pack(2 * half, interleaved, scale, _address(freq, _F32, (half,)))
 
 
+def _like(q, ld):
+    """A contiguous array for the results of q, whose tokens are ld elements apart."""
+    T, heads, dim = q.shape
+    return torch.empty_like(q) if ld == heads * dim else torch.empty((T, heads, dim), dtype=_BF16, device=q.device)
+
+
 def _rope_call(name, q, k, positions, freq, interleaved, scale, q_out, k_out):
     T, heads, dim = q.shape
     ldq, ld_out = _heads(q, T, heads, dim), heads * dim
     if q_out is None:
-        q_out = torch.empty((T, heads, dim), dtype=_BF16, device=q.device)
+        q_out = _like(q, ldq)
     else:
         ld_out = _heads(q_out, T, heads, dim)
     if k is None:
@@ -683,7 +692,7 @@ def _rope_call(name, q, k, positions, freq, interleaved, scale, q_out, k_out):
         kv_heads = k.shape[1]
         ldk, ldk_out = _heads(k, T, kv_heads, dim), kv_heads * dim
         if k_out is None:
-            k_out = torch.empty((T, kv_heads, dim), dtype=_BF16, device=q.device)
+            k_out = _like(k, ldk)
         else:
             ldk_out = _heads(k_out, T, kv_heads, dim)
         p_k, p_k_out = k.data_ptr(), k_out.data_ptr()
@@ -715,7 +724,7 @@ def qblora_rope_cache(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positio
     assert dim == 8 * k_cache.shape[2]
     ldq, ld_out = _heads(q, T, heads, dim), heads * dim
     if q_out is None:
-        q_out = torch.empty((T, heads, dim), dtype=_BF16, device=q.device)
+        q_out = _like(q, ldq)
     else:
         ld_out = _heads(q_out, T, heads, dim)
     rc = lib().qblora_rope_cache(_rope(freq, interleaved, scale), q.data_ptr(), ldq, heads, k.data_ptr(),
@@ -745,7 +754,7 @@ def qblora_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torc
         max_new = T
     dev = q.device
     if out is None:
-        out = torch.empty((T, heads, dim), dtype=_BF16, device=dev)
+        out = _like(q, ldq)
     else:
         ld_out = _heads(out, T, heads, dim)
     L = lib()
@@ -769,16 +778,24 @@ def qblora_rms_norm_fwd(x: torch.Tensor, w: torch.Tensor, eps: float, residual: 
     `keep` is set or a tensor is given."""
     T, d = x.shape
     p_x, p_residual = _address(x, _BF16, (T, d)), None
-    y = torch.empty_like(x) if y is None else y
+    if y is None:
+        y = torch.empty_like(x)
+        p_y = y.data_ptr()
+    else:
+        p_y = _address(y, _BF16, (T, d))
     if residual is None:
-        total = x
+        total, p_total = x, p_x
     else:
         p_residual = _address(residual, _BF16, (T, d))
-        total = torch.empty_like(x) if total is None else total
+        if total is None:
+            total = torch.empty_like(x)
+            p_total = total.data_ptr()
+        else:
+            p_total = _address(total, _BF16, (T, d))
     if keep and rstd is None:
         rstd = torch.empty(T, dtype=_F32, device=x.device)
-    rc = lib().qblora_rms_norm_fwd(p_x, p_residual, _address(w, _BF16, (d,)), T, d, eps, _address(total, _BF16, (T, d)),
-                                   _address(y, _BF16, (T, d)), None if rstd is None else _address(rstd, _F32, (T,)), _current_stream())
+    rc = lib().qblora_rms_norm_fwd(p_x, p_residual, _address(w, _BF16, (d,)), T, d, eps, p_total, p_y,
+                                   None if rstd is None else _address(rstd, _F32, (T,)), _current_stream())
     if rc:
         _check(rc, "qblora_rms_norm_fwd")
     return y, total, rstd
