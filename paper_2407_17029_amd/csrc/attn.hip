@@ -43,7 +43,7 @@ constexpr float kSlack = 8.0f;                 // a maximum may grow by 2^8 befo
 struct CutTile { int token0, rem0, rows, splits, slot, pad[3]; };
 struct Share { int rows, target, least, slack; int64_t over, upto; int* cuts; CutTile* cut; float* part; };
 constexpr int kFewTarget = 1024, kFewLeast = 8;
-constexpr int kManyTarget = 384, kManyLeast = 32;
+constexpr int kManyTarget = 384, kManyLeast = 16;
 static_assert(2 * kFewTarget < 1 << 15 && 2 * kManyTarget < 1 << 15, "parts and cut tiles are counted in halves of a word");
 
 // A workgroup's rows and range of positions; slot: its place among the parts, cut: its tile's among those that are cut
