@@ -812,16 +812,28 @@ def qblora_rms_norm_bwd(total: torch.Tensor, w: torch.Tensor, rstd: torch.Tensor
     T, d = total.shape
     dev = total.device
     p_total = _address(total, _BF16, (T, d))
-    dx = torch.empty((T, d), dtype=_BF16, device=dev) if dx is None else dx
-    p_dw = ws = None
+    if dx is None:
+        dx = torch.empty_like(total)
+        p_dx = dx.data_ptr()
+    else:
+        p_dx = _address(dx, _BF16, (T, d))
+    p_dw = p_ws = None
     nbytes = 0
     if need_dw:
-        dw = torch.empty(d, dtype=_F32, device=dev) if dw is None else dw
-        p_dw = _address(dw, _F32, (d,))
-        ws = _workspace(lambda: lib().qblora_rms_norm_bwd_workspace_bytes(T, d), dev, workspace)
-        nbytes = ws.numel() * ws.element_size()
+        if dw is None:
+            dw = torch.empty(d, dtype=_F32, device=dev)
+            p_dw = dw.data_ptr()
+        else:
+            p_dw = _address(dw, _F32, (d,))
+        if workspace is None:
+            nbytes = lib().qblora_rms_norm_bwd_workspace_bytes(T, d)
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        else:
+            nbytes = workspace.numel() * workspace.element_size()
+        p_ws = workspace.data_ptr()
     rc = lib().qblora_rms_norm_bwd(p_total, _address(w, _BF16, (d,)), _address(rstd, _F32, (T,)), _address(dy, _BF16, (T, d)),
-                                   None if dtotal is None else _address(dtotal, _BF16, (T, d)), T, d, _address(dx, _BF16, (T, d)),
-                                   p_dw, _ptr(ws), nbytes, _current_stream())
-    _check(rc, "qblora_rms_norm_bwd")
+                                   None if dtotal is None else _address(dtotal, _BF16, (T, d)), T, d, p_dx,
+                                   p_dw, p_ws, nbytes, _current_stream())
+    if rc:
+        _check(rc, "qblora_rms_norm_bwd")
     return dx, (dw if need_dw else None)

@@ -45,6 +45,7 @@ struct NormBackDesc {
     const qblora_bf16* total; const qblora_bf16* w; const float* rstd; const qblora_bf16* dy; const qblora_bf16* dtotal;
     int64_t T; int d;
     qblora_bf16* dx; float* dw; float* part;
+    int rows;                                      // workgroups that take rows
 };
 int64_t rms_norm_bwd_parts(int64_t T, int d);      // rows of [d] partial sums of dw
 int launch_rms_norm_bwd(const NormBackDesc& d, hipStream_t st);

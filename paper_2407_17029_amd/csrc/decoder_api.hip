@@ -193,7 +193,7 @@ int qblora_rms_norm_bwd(const qblora_bf16* total, const qblora_bf16* w, const fl
         if (!aligned(workspace, 16)) return QBLORA_ERR_SHAPE;
     }
     if (T == 0 && !dw) return QBLORA_OK;
-    NormBackDesc a{total, w, rstd, dy, dtotal, T, d, dx, dw, dw ? static_cast<float*>(workspace) : nullptr};
+    NormBackDesc a{total, w, rstd, dy, dtotal, T, d, dx, dw, dw ? static_cast<float*>(workspace) : nullptr, 0};
     return launch_rms_norm_bwd(a, as_stream(stream));
 }
 

@@ -6,6 +6,8 @@
 // Bound by HBM: one pass over each array.  A workgroup holds a row in registers, 8 features a thread and chunk, so the mean
 // is known before anything is written; the only other traffic is dw.  Rows of any length and alignment: a 16-byte access
 // takes any address in one instruction, and the features behind the last whole chunk go one by one.
+#include <algorithm>
+
 #include "decoder.h"
 
 namespace qblora {
@@ -111,9 +113,37 @@ __global__ __launch_bounds__(1024) void k_rms_norm(NormDesc a) {
     }
 }
 
+constexpr int kSumStride = 65;
+// dw of 64 columns: every eighth thread takes the same eight, rows threads / 8 apart, which are added up in a fixed order.
+__device__ __forceinline__ void column_sums(const NormBackDesc& a, int block, float* sums) {
+    const int c = 64 * block + 8 * (threadIdx.x & 7), groups = blockDim.x >> 3, g = threadIdx.x >> 3;
+    float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (c < a.d)
+#pragma unroll 4
+        for (int64_t row = g; row < a.T; row += groups) {
+            const uint4 t = load_chunk(a.total + row * a.d, c, a.d), y = load_chunk(a.dy + row * a.d, c, a.d);
+            const float r = a.rstd[row];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                s[2 * j] = __fmaf_rn(bf16_lo(word(y, j)), bf16_lo(word(t, j)) * r, s[2 * j]);
+                s[2 * j + 1] = __fmaf_rn(bf16_hi(word(y, j)), bf16_hi(word(t, j)) * r, s[2 * j + 1]);
+            }
+        }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[g * kSumStride + 8 * (threadIdx.x & 7) + j] = s[j];
+    __syncthreads();
+    if (threadIdx.x >= 64 || 64 * block + (int)threadIdx.x >= a.d) return;
+    float sum = 0.0f;
+    for (int i = 0; i < groups; ++i) sum += sums[i * kSumStride + threadIdx.x];
+    a.dw[64 * block + threadIdx.x] = sum;
+}
+
+// The first a.rows workgroups take rows, the others, if any, 64 columns of dw each.
 template <int NC, bool PAST>                  // PAST: stores go past the caches
 __global__ __launch_bounds__(1024) void k_rms_norm_bwd(NormBackDesc a) {
     __shared__ float slots[2][16];
+    extern __shared__ float sums[];                                      // of the workgroups with columns
+    if ((int)blockIdx.x >= a.rows) return column_sums(a, blockIdx.x - a.rows, sums);
     const int d = a.d;
     uint4 w[NC];
     float dw[NC][8];
@@ -125,7 +155,7 @@ __global__ __launch_bounds__(1024) void k_rms_norm_bwd(NormBackDesc a) {
         for (int j = 0; j < 8; ++j) dw[i][j] = 0.0f;
     }
     int turn = 0;
-    for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x, turn ^= 1) {
+    for (int64_t row = blockIdx.x; row < a.T; row += a.rows, turn ^= 1) {
         const float r = a.rstd[row];
         uint4 t[NC], y[NC], e[NC];
 #pragma unroll
@@ -210,6 +240,12 @@ Plan plan_of(int d) {
 constexpr int64_t kPastBytes = 8 << 20;
 bool past_caches(int64_t T, int d) { return T * d * 2 >= kPastBytes; }
 
+// Up to so many rows whose arrays stay in the caches, dw is summed by columns in the same launch, which reads total and dy a
+// second time: 1000 rows of 4096 both ways 22.1 us and 23.5 with the second launch, 64 rows 21.4 and 23.8; but 1000 rows of 8192
+// 33.3 and 31.6, 2001 of 600 26.4 and 25.4.  The columns take as many threads at least, which share out the rows.
+constexpr int64_t kColumnRows = 1024;
+constexpr int kColumnThreads = 512;
+
 }  // namespace
 
 int launch_rms_norm(const NormDesc& a, hipStream_t st) {
@@ -227,16 +263,25 @@ int64_t rms_norm_bwd_parts(int64_t T, int d) {
     return some < full ? some : full;
 }
 
-int launch_rms_norm_bwd(const NormBackDesc& a, hipStream_t st) {
+int launch_rms_norm_bwd(const NormBackDesc& desc, hipStream_t st) {
+    NormBackDesc a = desc;
     const Plan p = plan_of(a.d);
     const bool past = past_caches(a.T, a.d);
-    const int rows = (int)rms_norm_bwd_parts(a.T, a.d);
-    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(rows), dim3(p.threads), 0, st, a); };
-    if (rows) {
+    const auto launch = [&](int threads, int columns) {
+        const size_t lds = columns ? threads / 8 * kSumStride * sizeof(float) : 0;
+        const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a.rows + columns), dim3(threads), lds, st, a); };
         if (p.chunks == 1) go(past ? k_rms_norm_bwd<1, true> : k_rms_norm_bwd<1, false>);
         else go(past ? k_rms_norm_bwd<2, true> : k_rms_norm_bwd<2, false>);
+    };
+    if (a.dw && a.T && a.T <= kColumnRows && !past && a.dx != a.dy) {    // (dy is read by both)
+        a.rows = (int)a.T;
+        a.part = nullptr;
+        launch(std::max(p.threads, kColumnThreads), (a.d + 63) / 64);
+        return launch_status();
     }
-    if (a.dw) hipLaunchKernelGGL(k_rms_norm_dw, dim3((a.d + 15) / 16), dim3(1024), 0, st, a.part, rows, a.d, a.dw);
+    a.rows = (int)rms_norm_bwd_parts(a.T, a.d);
+    if (a.rows) launch(p.threads, 0);
+    if (a.dw) hipLaunchKernelGGL(k_rms_norm_dw, dim3((a.d + 15) / 16), dim3(1024), 0, st, a.part, a.rows, a.d, a.dw);
     return launch_status();
 }
 
