@@ -10,11 +10,17 @@
 // positions at a time straight from the pages into registers, in the operand order that the cache is stored in, with the
 // next 32 in flight behind them.  Scores are formed transposed, S^T = K Q^T, so that a lane holds eight positions of one row,
 // the operand of O^T = V^T P^T but for four exchanges between lanes.  The four waves of a workgroup take turns on the positions
-// and are joined in LDS.
+// and are joined in LDS.  64 single tokens of 40 heads over 100 to 8000 positions (2.3 GB): 368 us, 6.2 TB/s of what a kernel
+// that only reads gets 6.3 of; four of 64 heads, 8 of them with keys, over 30000 to 131000 (0.8 GB): 131 us, 6.2 TB/s; one of
+// 4095 (67 MB): 12.3 us and 4 of the join.
 //
 // attend_many takes 128 rows, 32 a wave, and is bound by the matrix pipe and by the exponentials beside it.  64 positions at a
 // time go through LDS, in the order of the pages (copies of 1 KB that need no registers, two tiles in turn, one barrier a
 // tile); scores are transposed here too, so that a row's maximum and sum are a lane's own but for one exchange of halves.
+// 4096 tokens over 12288, 32 heads (962 GFLOP): 915 us, 1050 TFLOP/s, 0.78 of what the library's large product reaches on the
+// chip; two workgroups a CU, the matrix pipe busy for 0.58 to 0.63 of the cycles at a power-limited 1.8 GHz.  A tile takes
+// 1.45 us of a workgroup alone on its CU and 2.2 of each of two, its start 3 to 5 us, the store of a part 1.7: what small
+// chunks are bound by.
 //
 // Work: requests differ by orders of magnitude, and only the device knows their lengths.  Every workgroup adds up the work
 // of all requests, which gives the number of positions that a workgroup takes if there are to be `target` of them, and finds
@@ -35,21 +41,33 @@ constexpr int kFewRows = 16;
 constexpr int kBlock = 32;                     // positions of a step
 constexpr int kManyRows = 128;
 constexpr float kNegInf = -__builtin_inff();
-constexpr float kSlack = 8.0f;                 // a maximum may grow by 2^8 before what was summed is rescaled
+// A maximum may grow by 2^8 before what was summed is rescaled: the weights stay below 2^8 and most steps do without the 64
+// products.  4096 tokens over 12288 take 974 us with every growth followed, 927 so.
+constexpr float kSlack = 8.0f;
 
-// Which requests a form takes, by their rows, and how their work is shared out: units of `rows` rows, about `target` of them
-// for a key / value head, at least `least` blocks each; one that is not more than 1 + slack / 2 units long stays whole.  Tiles that are cut leave their parts in `part` and themselves in
-// `cut`, `cuts` counts those.
+// Which requests a form takes, and how their work is shared out: units of `rows` rows, about `target` of them for a key /
+// value head, at least `least` blocks each.  A tile that is longer than a unit is cut into parts no longer than one, or, with
+// `slack`, into as many as come nearest.  Cut tiles leave their parts in `part` and themselves in `cut`; `cuts` counts them.
 struct CutTile { int token0, rem0, rows, splits, slot, pad[3]; };
-struct Share { int rows, target, least, slack; int64_t over, upto; int* cuts; CutTile* cut; float* part; };
+enum { FEW = 1, LOT = 2, ALL = 3 };            // the requests of few rows, those of more, or all
+struct Share { int rows, target, least, slack, form; int* cuts; CutTile* cut; float* part; };
+// Few rows: with 512 units 4 contexts of 30000 to 131000 take 148 us, with 1024 131, with 2048 138; single tokens of 16 x 1000 to
+// 8000 positions 55.6, 50.7 and 55.6.  With 4 blocks at least, one of 4095 takes 20.3, with 8 17.1, with 16 17.2.
 constexpr int kFewTarget = 1024, kFewLeast = 8;
+// More rows: every part costs 66 KB of writes and as many of reads, so there are fewer units than places.  Three chunks among
+// single tokens: 59 us with 384, 66 with 512; 128 tokens over 2000: 28 with 16 blocks at least, 38 with 32, 36 with 8.  Without
+// the slack 175 tokens over 3985 take 54 us, with it 46; 1000 without a context 43.6 and 35.5.
 constexpr int kManyTarget = 384, kManyLeast = 16;
+// Requests of up to kSomeRows rows go to attend_few, 16 rows at a time, if they do not make more than kSomeBlocks blocks in all:
+// what the chip takes at once in units of kFewLeast.  Four tokens of 8 heads a key head over 4000: 14.1 us that way, 20.8 in one
+// tile of 128 rows; 16 of those requests, above the limit, 48.9 and 43.7.
+constexpr int kSomeRows = 64, kSomeBlocks = 512 * kFewLeast;
 static_assert(2 * kFewTarget < 1 << 15 && 2 * kManyTarget < 1 << 15, "parts and cut tiles are counted in halves of a word");
 
-// A workgroup's rows and range of positions; slot: its place among the parts, cut: its tile's among those that are cut
 // x / group for x < 128 + group: the magic number is 2^32 / group + 1, whose excess is less than x * group / 2^32 < 1
 __device__ __forceinline__ int quotient(const AttnDesc& d, int x) { return d.group == 1 ? x : (int)__umulhi((uint32_t)x, d.group_magic); }
 
+// A workgroup's rows and range of positions; slot: its place among the parts, cut: its tile's among those that are cut
 struct Unit { int request, tile, split, splits, slot, cut; };
 
 struct Span { int start, fresh, context; };
@@ -62,17 +80,6 @@ __device__ __forceinline__ Span span_of(const AttnDesc& d, int i) {
 __device__ __forceinline__ Span uniform_span_of(const AttnDesc& d, int i) {
     const Span s = span_of(d, i);
     return {__builtin_amdgcn_readfirstlane(s.start), __builtin_amdgcn_readfirstlane(s.fresh), __builtin_amdgcn_readfirstlane(s.context)};
-}
-
-struct Cost { int tiles, blocks; };
-__device__ __forceinline__ Cost cost_of(const AttnDesc& d, int i, const Share& w) {
-    const Span s = span_of(d, i);
-    const int64_t rows = (int64_t)s.fresh * d.group;
-    if (rows <= w.over || rows > w.upto) return {0, 0};
-    const int limit = d.width << d.page_shift;
-    const int hi = min(s.context + s.fresh, limit), lo = d.window ? max(s.context + 1 - d.window, 0) : 0;
-    const int blocks = hi > lo ? (hi + kBlock - 1) / kBlock - lo / kBlock : 1;
-    return {(int)((rows + w.rows - 1) / w.rows), blocks};
 }
 
 // sum over the lanes up to this one
@@ -89,6 +96,19 @@ __device__ __forceinline__ int64_t sum_of_wave(int64_t x) {
     if (__all((uint64_t)x < 1u << 25)) return __builtin_amdgcn_readlane(scan((int)x), 63);
     for (int s = 32; s; s >>= 1) x += __shfl_xor(x, s);
     return x;
+}
+
+struct Cost { int tiles, blocks; };
+__device__ __forceinline__ int blocks_of(const AttnDesc& d, const Span& s) {
+    const int limit = d.width << d.page_shift;
+    const int hi = min(s.context + s.fresh, limit), lo = d.window ? max(s.context + 1 - d.window, 0) : 0;
+    return hi > lo ? (hi + kBlock - 1) / kBlock - lo / kBlock : 1;
+}
+// `some`: the rows up to which requests go to attend_few in this call, where both forms are there
+__device__ __forceinline__ Cost cost_of(const AttnDesc& d, const Span& s, const Share& w, int some) {
+    const int64_t rows = (int64_t)s.fresh * d.group;
+    if (rows == 0 || (w.form == FEW && rows > some) || (w.form == LOT && rows <= some)) return {0, 0};
+    return {(int)((rows + w.rows - 1) / w.rows), blocks_of(d, s)};
 }
 
 // Blocks of a unit, from the blocks of all tiles
@@ -117,8 +137,18 @@ struct Finder {
 __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share, int want, bool first, Finder& f, Unit& u) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (d.n <= 64) {
-        Cost c{0, 0};
-        if (lane < d.n) c = cost_of(d, lane, share);
+        Span s{0, 0, 0};
+        if (lane < d.n) s = span_of(d, lane);
+        int some = kFewRows;
+        if (share.form != ALL) {
+            const int64_t rows = (int64_t)s.fresh * d.group;
+            const bool between = rows > kFewRows && rows <= kSomeRows;
+            if (__any(between)) {
+                const int64_t blocks = between ? (rows + kFewRows - 1) / kFewRows * blocks_of(d, s) : 0;
+                if (sum_of_wave(blocks) * d.kv_heads <= kSomeBlocks) some = kSomeRows;
+            }
+        }
+        const Cost c = cost_of(d, s, share, some);
         const Units v = units_of(c, blocks_per_unit(sum_of_wave((int64_t)c.tiles * c.blocks), share), share.slack);
         const int a = scan(v.count), b = scan(v.cuts);
         if (first && tid == 63) *share.cuts = b >> 16;
@@ -137,7 +167,7 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
     }
     int64_t all = 0;
     for (int i = tid; i < d.n; i += kThreads) {
-        const Cost c = cost_of(d, i, share);
+        const Cost c = cost_of(d, span_of(d, i), share, kFewRows);
         all += (int64_t)c.tiles * c.blocks;
     }
     all = sum_of_wave(all);
@@ -151,7 +181,7 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
     for (int base = 0; base < d.n; base += kThreads) {
         const int i = base + tid;
         Cost c{0, 0};
-        if (i < d.n) c = cost_of(d, i, share);
+        if (i < d.n) c = cost_of(d, span_of(d, i), share, kFewRows);
         const Units v = units_of(c, per, share.slack);
         int a = scan(v.count), b = scan(v.cuts);
         __syncthreads();
@@ -229,8 +259,8 @@ __device__ __forceinline__ const qblora_bf16* value_row(const AttnDesc& d, const
     return d.vc + (((int64_t)id * d.kv_heads + kvh) * D << d.page_shift) + (in_page >> 3) * D * 8 + (in_page & 7);
 }
 
-// A part of the cache that this call reads once: no line is kept for it.  64 tokens of 40 heads, contexts of 1750: 411 us
-// without, 376 with values that way.
+// A part of the cache that this call reads once: no line is kept for it.  64 tokens of 40 heads over 100 to 8000: 411 us without,
+// 376 with values that way, 368 with both.
 __device__ __forceinline__ uint4 stream(const qblora_bf16* p) {
     return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p)));
 }
@@ -741,8 +771,7 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
     if (h2 == 0 && d.lse) d.lse[(int64_t)(s.start + to) * d.heads + q_head] = (top + __builtin_log2f(l)) * 0.69314718055994530942f;
 }
 
-// One of the forms, or both, so that chunks and single tokens of a batch run beside each other.
-enum { FEW = 1, LOT = 2, BOTH = 3 };
+// One of the forms, or both (ALL), so that chunks and single tokens of a batch run beside each other.
 template <int D, int FORMS>
 __global__ __launch_bounds__(kThreads, (D > 128 ? 1 : 2)) void k_attn(AttnDesc d, Share lot, Share few, int lot_blocks) {
     __shared__ Finder finder;
@@ -757,7 +786,8 @@ __global__ __launch_bounds__(kThreads, (D > 128 ? 1 : 2)) void k_attn(AttnDesc d
 }
 
 // Adds up the parts of a cut tile, weights 2^(m - max m), four features a thread.  Few parts: a thread has them all in flight,
-// and the threads that are left over take other rows; many: they share the parts, of every gridDim.y-th row.
+// and the threads that are left over take other rows; many: they share the parts, of every gridDim.y-th row, the first of
+// them in flight while the weights are made.  512 tokens over 2000, three parts a tile: 46 us, 67 if all go the second way.
 constexpr int kFewParts = 4, kPartsAhead = 4;
 template <int D>
 __global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share lot, Share few, int lot_blocks) {
@@ -883,10 +913,10 @@ void lay_out(Space& space, int kv_heads, int head_dim, bool many, Share& lot, Sh
     lot.part = space.take<float>((size_t)2 * lot.target * kv_heads * kManyRows * (head_dim + 2));
 }
 Share few_share(int kv_heads, bool many) {
-    return Share{kFewRows, target_of(kFewTarget, kv_heads), kFewLeast, 0, 0, many ? (int64_t)kFewRows : INT64_MAX, nullptr, nullptr, nullptr};
+    return Share{kFewRows, target_of(kFewTarget, kv_heads), kFewLeast, 0, many ? FEW : ALL, nullptr, nullptr, nullptr};
 }
 Share lot_share(int kv_heads) {
-    return Share{kManyRows, target_of(kManyTarget, kv_heads), kManyLeast, 1, kFewRows, INT64_MAX, nullptr, nullptr, nullptr};
+    return Share{kManyRows, target_of(kManyTarget, kv_heads), kManyLeast, 1, LOT, nullptr, nullptr, nullptr};
 }
 
 template <int D>
@@ -895,13 +925,16 @@ int launch(const AttnDesc& d, hipStream_t st) {
     Share few = few_share(d.kv_heads, many), lot = lot_share(d.kv_heads);
     Space space(d.part);
     lay_out(space, d.kv_heads, D, many, lot, few);
-    const int64_t few_tiles = many ? d.n : (int64_t)d.T * d.group / kFewRows + d.n;
-    const int64_t lot_tiles = many ? (int64_t)d.T * d.group / kManyRows + d.n : 0;
-    // No more units than the tiles and the target, nor than the longest row of the table allows.
+    // rows of m requests make at most (rows + m (size - 1)) / size tiles
+    const int64_t rows = (int64_t)d.T * d.group, requests = std::min<int64_t>(d.n, d.T);
+    const auto tiles_of = [&](int size) { return (rows + requests * (size - 1)) / size; };
+    const int64_t lot_tiles = many ? tiles_of(kManyRows) : 0;
+    const int64_t few_tiles = many ? std::min(tiles_of(kFewRows), requests * (d.n > 64 ? 1 : kSomeRows / kFewRows)) : tiles_of(kFewRows);
+    // A unit more than what the target makes for every tile, and no more than the longest row of the table allows.
     const int64_t blocks_of_row = (((int64_t)d.width << d.page_shift) + kBlock - 1) / kBlock + 1;
     const auto units = [&](int64_t tiles, const Share& w) {
         const int64_t most = tiles * ((blocks_of_row + w.least - 1) / w.least);
-        return std::max<int64_t>(std::min(most, tiles + 2 * w.target), 1) * d.kv_heads;
+        return std::max<int64_t>(std::min(most, tiles + w.target), 1) * d.kv_heads;
     };
     const int64_t lot_blocks = many ? units(lot_tiles, lot) : 0, blocks = lot_blocks + units(few_tiles, few);
     if (blocks > INT32_MAX) return QBLORA_ERR_UNSUPPORTED;
@@ -911,7 +944,7 @@ int launch(const AttnDesc& d, hipStream_t st) {
     if (!many) {
         go(k_attn<D, FEW>, blocks);
     } else if constexpr (D <= 128) {
-        go(k_attn<D, BOTH>, blocks);
+        go(k_attn<D, ALL>, blocks);
     } else {                                                           // (one kernel of both would not have the registers)
         go(k_attn<D, LOT>, lot_blocks);
         go(k_attn<D, FEW>, blocks - lot_blocks);

@@ -153,3 +153,16 @@ def test_norm_gradients_where_dy_is_replaced(T, d):
     assert dx2.data_ptr() == dy.data_ptr() and torch.equal(dx, dx2)
     for g in (dw, dw2):
         assert ((g.double() - terms.sum(0)).abs() <= 8e-6 * terms.abs().sum(0)).all()
+
+
+@pytest.mark.parametrize("n,ctx,new", [(1, 900, 5), (3, 400, 8), (8, 120, 2), (20, 2100, 4), (64, 40, 3), (65, 40, 3), (70, 300, 8)])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(8, 1, 128), (16, 2, 64), (4, 1, 256)])
+def test_a_few_tokens_of_several_requests(n, ctx, new, heads, kv_heads, dim):
+    """17 to 64 rows of a request and fewer, in small batches and large ones, among single tokens and one chunk."""
+    r = np.random.Generator(np.random.Philox(key=[n, new]))
+    context = [int(x) for x in r.integers(0, ctx + 1, n)]
+    fresh = [int(x) for x in r.integers(1, new + 1, n)]
+    fresh[0] = new
+    if n in (8, 65):
+        fresh[n // 2] = 40
+    _check(_batch(n + ctx, context, fresh, 16, heads, kv_heads, dim), window=100 if n == 3 else 0)
