@@ -8,7 +8,9 @@
 // access.  Tokens of a prompt that go to the cache come eight to a workgroup, neighbouring lanes one behind the other, so that
 // eight keys' 16-byte octets are one 128-byte line of their page and eight values of a feature one 16-byte store; single
 // tokens come one to a workgroup, which is four times as many of them.  k_rope_any: parts of a head that are no multiple of
-// 16 features.
+// 16 features.  6693 tokens of 64 + 64 heads of 128 to the cache (658 MB): 146 us, 4.5 TB/s of the 4.9 that a large copy
+// reaches; 1337 of 40 + 40 heads there and back (110 MB): 21.1 us, 5.2 TB/s; 64 single tokens of 32 + 32: 7 us, of which 3.5 are
+// an empty launch.
 #include "decoder.h"
 
 namespace qblora {
@@ -16,7 +18,9 @@ namespace qblora {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kManyTokens = 256;               // from here on, tokens that go to the cache are taken for prompts
+// From here on, tokens that go to the cache are taken for prompts.  A chunk of 300: 10.3 us that way, 11.2 a token at a time, of
+// 512: 10.4 and 19.9; but 256 single tokens (which no argument tells from a chunk) 12.4 and 10.7, 512 of them 21.6 and 23.7.
+constexpr int kManyTokens = 256;
 
 // cos and sin of p * freq: in 64 bits down to one turn, then by the hardware's functions of turns
 __device__ __forceinline__ void turn(int32_t p, float freq, float scale, float& c, float& s) {
@@ -196,6 +200,30 @@ __global__ __launch_bounds__(kThreads) void k_rope(RopeDesc d, RopeGrid grid) {
     __shared__ uint4 turned[kThreads / 64][TB > 1 ? 256 : 1];
     const int first = ((int)blockIdx.y - grid.qk_blocks) * kThreads + tid, step = grid.v_blocks * kThreads;
     const int quads = d.kv_heads * d.head_dim / 4;
+    if (TB > 1 && (__ballot((tid & 63) < 9 && begins(d, t0 + (tid & 63))) & 0x1ff) == 0x1ff) {
+        // no slot follows another (single tokens): the eight tokens' values in flight together
+        const int lane = tid & 63;
+        const int64_t slots = lane < 8 && t0 + lane < d.T ? d.slots[t0 + lane] : -1;
+        const uint32_t cached = (uint32_t)__ballot(lane < 8 && in_cache(d, slots));
+        for (int i = first; i - lane < quads; i += step) {
+            const int h = 4 * i / d.head_dim, f = 4 * i - h * d.head_dim;
+            bf16x4_any x[8];
+#pragma unroll
+            for (int b = 0; b < 8; ++b)
+                if (i < quads && (cached >> b & 1)) x[b] = *reinterpret_cast<const bf16x4_any*>(d.v + (t0 + b) * d.ldv + 4 * i);
+#pragma unroll
+            for (int b = 0; b < 8; ++b) {
+                const int64_t slot = __shfl(slots, b);
+                if (i >= quads || !(cached >> b & 1)) continue;
+                int place;
+                qblora_bf16* out = d.vc + page_of(d, slot, h, place);
+                out += value_at(d, place, f);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) out[8 * j] = (qblora_bf16)(j & 1 ? x[b][j >> 1] >> 16 : x[b][j >> 1]);
+            }
+        }
+        return;
+    }
     for (int b = 0; b < TB && t0 + b < d.T; ++b) {
         const int64_t t = t0 + b, slot = d.slots[t];
         if (!in_cache(d, slot)) continue;
@@ -268,7 +296,7 @@ int launch_rope(const RopeDesc& d, hipStream_t st) {
     }
     const bool prompts = d.kc && d.T >= kManyTokens;
     const int tb = prompts ? 8 : 1, lanes = kThreads / (tb * units);
-    // workgroups of a token (or eight): one pass over the heads each, few tokens; two passes, many
+    // workgroups of a token (or eight): one pass over the heads each
     const int groups = (all + lanes * kHeads - 1) / (lanes * kHeads);
     RopeGrid g{groups, 0};
     const bool past = d.T * all * d.head_dim * 2 >= kPastBytes;
