@@ -8,8 +8,7 @@
 // access.  Tokens of a prompt that go to the cache come eight to a workgroup, neighbouring lanes one behind the other, so that
 // eight keys' 16-byte octets are one 128-byte line of their page and eight values of a feature one 16-byte store; single
 // tokens come one to a workgroup, which is four times as many of them.  k_rope_any: parts of a head that are no multiple of
-// 16 features.  6693 tokens of 64 + 64 heads of 128 to the cache (658 MB): 146 us, 4.5 TB/s of the 4.9 that a large copy
-// reaches; 1337 of 40 + 40 heads there and back (110 MB): 21.1 us, 5.2 TB/s; 64 single tokens of 32 + 32: 7 us, of which 3.5 are
+// 16 features.  6693 tokens of 64 + 64 heads of 128 to the cache (658 MB): 131 us, 5.0 TB/s, where a large copy reaches 4.9; 1337 of 40 + 40 heads there and back (110 MB): 21.1 us, 5.2 TB/s; 64 single tokens of 32 + 32: 7 us, of which 3.5 are
 // an empty launch.
 #include "decoder.h"
 
@@ -86,7 +85,7 @@ __global__ __launch_bounds__(kThreads) void k_rope_any(RopeDesc d) {
 
 constexpr int kHeads = 4;                      // in flight
 // From so many bytes of q and k on, nothing of the outputs is in an L2 when they are read: 1337 tokens of 40 + 40 heads (27 MB)
-// both ways 23.7 us through the caches, 21.0 past them; 6693 tokens of 64 + 64 heads to the cache 155 and 147.
+// both ways 23.7 us through the caches, 21.0 past them; 6693 tokens of 64 + 64 heads to the cache 155 and 147 (131 by now).
 constexpr int64_t kPastBytes = 8 << 20;
 
 template <bool PAST>
@@ -200,11 +199,19 @@ __global__ __launch_bounds__(kThreads) void k_rope(RopeDesc d, RopeGrid grid) {
     __shared__ uint4 turned[kThreads / 64][TB > 1 ? 256 : 1];
     const int first = ((int)blockIdx.y - grid.qk_blocks) * kThreads + tid, step = grid.v_blocks * kThreads;
     const int quads = d.kv_heads * d.head_dim / 4;
-    if (TB > 1 && (__ballot((tid & 63) < 9 && begins(d, t0 + (tid & 63))) & 0x1ff) == 0x1ff) {
+    const int lane = tid & 63;
+    int64_t slots = -1;                                                // of token t0 + lane
+    uint32_t begin = 0x1ffff;                                          // which tokens begin a run; one ends within seven more
+    if (TB > 1) {
+        const int64_t t = t0 + lane;
+        int64_t before = -1;
+        if (lane < 16 && t < d.T) slots = d.slots[t];
+        if (lane < 16 && t < d.T && t > 0) before = d.slots[t - 1];
+        begin = (uint32_t)__ballot(lane >= 16 || t >= d.T || t == 0 || (slots & 7) == 0 || before != slots - 1) & 0x1ffff;
+    }
+    if (TB > 1 && (begin & 0x1ff) == 0x1ff) {
         // no slot follows another (single tokens): the eight tokens' values in flight together
-        const int lane = tid & 63;
-        const int64_t slots = lane < 8 && t0 + lane < d.T ? d.slots[t0 + lane] : -1;
-        const uint32_t cached = (uint32_t)__ballot(lane < 8 && in_cache(d, slots));
+        const uint32_t cached = (uint32_t)__ballot(lane < 8 && t0 + lane < d.T && in_cache(d, slots));
         for (int i = first; i - lane < quads; i += step) {
             const int h = 4 * i / d.head_dim, f = 4 * i - h * d.head_dim;
             bf16x4_any x[8];
@@ -225,17 +232,13 @@ __global__ __launch_bounds__(kThreads) void k_rope(RopeDesc d, RopeGrid grid) {
         return;
     }
     for (int b = 0; b < TB && t0 + b < d.T; ++b) {
-        const int64_t t = t0 + b, slot = d.slots[t];
+        if (!(begin >> b & 1)) continue;                               // in another token's run
+        const int64_t t = t0 + b, slot = TB > 1 ? __shfl(slots, b) : d.slots[t];
         if (!in_cache(d, slot)) continue;
-        int run = 1;
-        if (TB > 1) {
-            if (t > 0 && (slot & 7) && d.slots[t - 1] == slot - 1) continue;             // in another token's run
-            while (((slot + run) & 7) && t + run < d.T && d.slots[t + run] == slot + run) ++run;
-        }
+        const int run = TB > 1 ? __builtin_ctz(begin >> (b + 1)) + 1 : 1;
         int place;
         (void)page_of(d, slot, 0, place);
         if (TB > 1 && run == 8) {
-            const int lane = tid & 63;
             uint4* mine = turned[tid >> 6];
             for (int i = first; i - lane < quads; i += step) {
                 if (i < quads) {
