@@ -242,6 +242,10 @@ __device__ __forceinline__ void note_cut(const Share& share, const Unit& u, int 
 
 __device__ __forceinline__ bool not_finite(uint32_t pair) { return (((pair & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0; }
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2 exponents(uint32_t pair) { return __builtin_bit_cast(u16x2, pair & 0x7f807f80u); }
+__device__ __forceinline__ u16x2 larger(u16x2 a, u16x2 b) { return __builtin_elementwise_max(a, b); }
+
 // all bits of an element or none
 __device__ __forceinline__ uint32_t mask_of(uint32_t bits) { return (bits & 1u) * 0xffffu | (bits >> 1 & 1u) * 0xffff0000u; }
 __device__ __forceinline__ uint32_t without_not_finite(uint32_t pair) {
@@ -682,41 +686,68 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
             if (base >= see1 || base + kTile <= see0) continue;
             f32x16 sc[TT];
             products(j, sc);
-            const int row_low = d.window ? here - d.window : -1;
-            uint32_t any = 0, seen = 0;                                // by some row, by this lane's; bit 8 s4 + k: position 16 s4 + 8 h + k
-#pragma unroll
-            for (int s4 = 0; s4 < PS; ++s4)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const int pos = base + 16 * s4 + 8 * h + k;
-                    if (pos >= see0 && pos < see1 && (listed >> s4 & 1)) any |= 1u << (8 * s4 + k);
-                    if (pos <= here && pos > row_low) seen |= 1u << (8 * s4 + k);
-                }
-            seen &= any;
-#pragma unroll
-            for (int tt = 0; tt < TT; ++tt)
-#pragma unroll
-                for (int k = 0; k < 16; ++k) sc[tt][k] = (seen >> (16 * tt + k)) & 1 ? sc[tt][k] : kNegInf;
-            bf16x8 pf[PS];
-            weights(sc, pf);
-            // as in attend_few: values that no row sees are 0, and what is not finite is added behind the loop
-            bool odd = false;
+            // of a sixteen's positions 8 h + k this lane's row sees from low to high - 1, and the wave's rows see some of those of
+            // `some` (what they all see is no matter of a mask)
+            uint32_t some = 0, all = 0;                                // bit s4
 #pragma unroll
             for (int s4 = 0; s4 < PS; ++s4) {
-                const uint32_t bits = any >> (8 * s4), k0 = mask_of(bits), k1 = mask_of(bits >> 2), k2 = mask_of(bits >> 4), k3 = mask_of(bits >> 6);
+                const int at = base + 16 * s4;
+                const bool there = listed >> s4 & 1;
+                if (there && at < see1 && at + 16 > see0) some |= 1u << s4;
+                if (there && at >= full0 && at + 16 <= full1) all |= 1u << s4;
+                const int high = there ? min(here + 1, limit) - at - 8 * h : 0, low = d.window ? here + 1 - d.window - at - 8 * h : 0;
 #pragma unroll
-                for (int i = 0; i < DT; ++i) {
-                    uint4 v = value(j, s4, i);
-                    v = make_uint4(v.x & k0, v.y & k1, v.z & k2, v.w & k3);
-                    odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
-                    v = make_uint4(without_not_finite(v.x), without_not_finite(v.y), without_not_finite(v.z), without_not_finite(v.w));
-                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pf[s4], o[i], 0, 0, 0);
+                for (int k = 0; k < 8; ++k) {
+                    const int at8 = 8 * (s4 & 1) + k;
+                    sc[s4 >> 1][at8] = k < high ? sc[s4 >> 1][at8] : kNegInf;
                 }
-                __builtin_amdgcn_sched_barrier(0);
+                if (d.window)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int at8 = 8 * (s4 & 1) + k;
+                        sc[s4 >> 1][at8] = k >= low ? sc[s4 >> 1][at8] : kNegInf;
+                    }
             }
-            if (__any(odd)) {
-                odd0 = min(odd0, base);
-                odd1 = base + kTile;
+            bf16x8 pf[PS];
+            weights(sc, pf);
+            // As in attend_few: values that no row sees are 0, and what is not finite is added behind the loop.  Sixteens that no row
+            // sees are left out; in the others all is finite most of the time, and a weight of 0 leaves nothing of it.
+#pragma unroll
+            for (int s4 = 0; s4 < PS; ++s4) {
+                if (!(some >> s4 & 1)) continue;
+                uint4 v[DT];
+#pragma unroll
+                for (int i = 0; i < DT; ++i) v[i] = value(j, s4, i);
+                if (!(all >> s4 & 1)) {
+                    u16x2 most = {0, 0};
+#pragma unroll
+                    for (int i = 0; i < DT; ++i)
+                        most = larger(larger(larger(most, exponents(v[i].x)), larger(exponents(v[i].y), exponents(v[i].z))), exponents(v[i].w));
+                    if (__any(most[0] == 0x7f80 || most[1] == 0x7f80)) {
+                        uint32_t bits = 0;                             // of the lane's eight positions, those that some row sees
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const int pos = base + 16 * s4 + 8 * h + k;
+                            if (pos >= see0 && pos < see1) bits |= 1u << k;
+                        }
+                        const uint32_t k0 = mask_of(bits), k1 = mask_of(bits >> 2), k2 = mask_of(bits >> 4), k3 = mask_of(bits >> 6);
+                        bool odd = false;
+#pragma unroll
+                        for (int i = 0; i < DT; ++i) {
+                            v[i] = make_uint4(v[i].x & k0, v[i].y & k1, v[i].z & k2, v[i].w & k3);
+                            odd |= not_finite(v[i].x) || not_finite(v[i].y) || not_finite(v[i].z) || not_finite(v[i].w);
+                            v[i] = make_uint4(without_not_finite(v[i].x), without_not_finite(v[i].y), without_not_finite(v[i].z), without_not_finite(v[i].w));
+                        }
+                        if (__any(odd)) {
+                            odd0 = min(odd0, base);
+                            odd1 = base + kTile;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < DT; ++i)
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[i]), pf[s4], o[i], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         // the others, nearly all of a long context: a loop of its own, so that its registers are its own
