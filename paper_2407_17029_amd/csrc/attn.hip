@@ -570,7 +570,14 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
     const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(sh.buf)) + mine * kSixteen + part * kCopies * 1024;
     int batch = 0;
     uint64_t batch_listed = 0;
-    // copies tile j, and says which of its sixteens are listed; for j = 0, 1, ..
+    // A tile's values are copied later than its keys: all waves' copies at once would hold them up.
+    const unsigned char* v_late = nullptr;
+    uint32_t to_late = 0;
+    auto copy_values = [&] {
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) copy_to_lds(v_late + i * 1024, v_lane, to_late + i * 1024);
+    };
+    // copies tile j's keys, and says which of its sixteens are listed; for j = 0, 1, ..
     auto copy = [&](int j) {
         const int tile = n0 + j;
         if (j % kBatch == 0) {
@@ -590,8 +597,8 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
             copy_to_lds(k, k_lane, to + i * 1024);
             k += (4 << shift) * 16;
         }
-#pragma unroll
-        for (int i = 0; i < kCopies; ++i) copy_to_lds(v + i * 1024, v_lane, to + 2 * kTileBytes + i * 1024);
+        v_late = v;
+        to_late = to + 2 * kTileBytes;
         return (uint32_t)(batch_listed >> (j % kBatch * PS)) & ((1u << PS) - 1);
     };
 
@@ -600,9 +607,11 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
     for (int i = 0; i < DT; ++i)
 #pragma unroll
         for (int k = 0; k < 16; ++k) o[i][k] = 0.0f;
-    // Exponents are c s - ref, ref near the maximum of c s; l: the sum over this lane's positions.  Where c s is so large that
-    // a product's rounding counts, ref is 0 and the maximum `m` is taken off the products first.
-    float ref = kNegInf, m = kNegInf, l = 0.0f;
+    // Exponents are c s - ref, ref near the maximum of c s; l: the sum over this lane's positions; bound: the product up to
+    // which ref serves as it is (NaN: none).  Where c s is so large that a product's rounding counts, ref is 0 and the maximum
+    // `m` is taken off the products first.
+    const float none = __builtin_nanf("");
+    float ref = kNegInf, m = kNegInf, l = 0.0f, bound = none;
     bool large = false;
     int odd0 = INT_MAX, odd1 = 0;                                      // positions among which values are not finite
 
@@ -619,11 +628,20 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
         for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
             for (int k = 0; k < 16; ++k) sc[tt][k] = 0.0f;
+        constexpr int kAhead = 6;                                      // keys in flight
+        bf16x8 ahead[kAhead];
+        if constexpr (D >= 128) {
 #pragma unroll
-        for (int i = 0; i < KS; ++i) {
+            for (int n = 0; n < kAhead; ++n) ahead[n] = key(j, n / TT, n % TT);
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
-            for (int tt = 0; tt < TT; ++tt) sc[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key(j, i, tt), qf[i], sc[tt], 0, 0, 0);
-            if (D > 128 && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);          // no more operands ahead than registers
+        for (int n = 0; n < KS * TT; ++n) {
+            sc[n % TT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(D >= 128 ? ahead[n % kAhead] : key(j, n / TT, n % TT), qf[n / TT], sc[n % TT], 0, 0, 0);
+            if constexpr (D >= 128) {
+                if (n + kAhead < KS * TT) ahead[n % kAhead] = key(j, (n + kAhead) / TT, (n + kAhead) % TT);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     };
     auto weights = [&](f32x16 (&sc)[TT], bf16x8 (&pf)[PS]) {
@@ -632,13 +650,14 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
         for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
             for (int k = 0; k < 16; ++k) top = fmaxf(top, sc[tt][k]);
-        top = max_of_halves(top);
-        if (__any(top * c > ref + kSlack || m == kNegInf || large)) {
+        if (__any(!(top <= bound))) {
+            top = max_of_halves(top);
             const float m_new = fmaxf(m, top), m_use = m_new == kNegInf ? 0.0f : m_new;
             const float a = m == kNegInf ? 0.0f : exp2_of(large ? (m - m_use) * c : ref - m_use * c);
             large = large || __any(fabsf(m_use) * c > 0x1p26f);
             m = m_new;
             ref = large ? 0.0f : m_use * c;
+            bound = large || m_new == kNegInf ? none : m_use + kSlack / c;
             l *= a;
 #pragma unroll
             for (int i = 0; i < DT; ++i)
@@ -667,7 +686,10 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
 
     const int turns = n1 - n0;
     uint32_t listed = 0, next_listed = 0;
-    if (turns > 0) next_listed = copy(0);
+    if (turns > 0) {
+        next_listed = copy(0);
+        copy_values();
+    }
     auto full = [&](int j) {                                           // seen by all rows of the wave
         const int base = (n0 + j) * kTile;
         return base >= full0 && base + kTile <= full1 && next_listed == (1u << PS) - 1;
@@ -683,6 +705,7 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
         for (; j < turns && !full(j); ++j) {
             enter(j);
             const int base = (n0 + j) * kTile;
+            if (j + 1 < turns) copy_values();
             if (base >= see1 || base + kTile <= see0) continue;
             f32x16 sc[TT];
             products(j, sc);
@@ -755,6 +778,7 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
             enter(j);
             f32x16 sc[TT];
             products(j, sc);
+            if (j + 1 < turns) copy_values();
             bf16x8 pf[PS];
             weights(sc, pf);
 #pragma unroll
