@@ -17,10 +17,10 @@
 // attend_many takes 128 rows, 32 a wave, and is bound by the matrix pipe and by the exponentials beside it.  64 positions at a
 // time go through LDS, in the order of the pages (copies of 1 KB that need no registers, two tiles in turn, one barrier a
 // tile); scores are transposed here too, so that a row's maximum and sum are a lane's own but for one exchange of halves.
-// 4096 tokens over 12288, 32 heads (962 GFLOP): 915 us, 1050 TFLOP/s, 0.78 of what the library's large product reaches on the
-// chip; two workgroups a CU, the matrix pipe busy for 0.58 to 0.63 of the cycles at a power-limited 1.8 GHz.  A tile takes
-// 1.45 us of a workgroup alone on its CU and 2.2 of each of two, its start 3 to 5 us, the store of a part 1.7: what small
-// chunks are bound by.
+// 4096 tokens over 12288, 32 heads (962 GFLOP): 853 us, 1130 TFLOP/s, 0.84 of what the library's large product reaches on the
+// chip; two workgroups a CU, the matrix pipe busy for 0.59 of the cycles and the vector ALU for 0.48, at a power-limited 1.7
+// GHz.  In small calls a tile takes 1.1 us of a workgroup alone on its CU and 1.9 of each of two, its start 3 to 5 us, the
+// store of a part up to 1.7.
 //
 // Work: requests differ by orders of magnitude, and only the device knows their lengths.  Every workgroup adds up the work
 // of all requests, which gives the number of positions that a workgroup takes if there are to be `target` of them, and finds
@@ -42,7 +42,7 @@ constexpr int kBlock = 32;                     // positions of a step
 constexpr int kManyRows = 128;
 constexpr float kNegInf = -__builtin_inff();
 // A maximum may grow by 2^8 before what was summed is rescaled: the weights stay below 2^8 and most steps do without the 64
-// products.  4096 tokens over 12288 take 974 us with every growth followed, 927 so.
+// products.  4096 tokens over 12288 took 974 us with every growth followed, 927 so.
 constexpr float kSlack = 8.0f;
 
 // Which requests a form takes, and how their work is shared out: units of `rows` rows, about `target` of them for a key /
@@ -54,9 +54,9 @@ struct Share { int rows, target, least, slack, form; int* cuts; CutTile* cut; fl
 // Few rows: with 512 units 4 contexts of 30000 to 131000 take 148 us, with 1024 131, with 2048 138; single tokens of 16 x 1000 to
 // 8000 positions 55.6, 50.7 and 55.6.  With 4 blocks at least, one of 4095 takes 20.3, with 8 17.1, with 16 17.2.
 constexpr int kFewTarget = 1024, kFewLeast = 8;
-// More rows: every part costs 66 KB of writes and as many of reads, so there are fewer units than places.  Three chunks among
-// single tokens: 59 us with 384, 66 with 512; 128 tokens over 2000: 28 with 16 blocks at least, 38 with 32, 36 with 8.  Without
-// the slack 175 tokens over 3985 take 54 us, with it 46; 1000 without a context 43.6 and 35.5.
+// More rows: every part costs 66 KB of writes and as many of reads, so there are fewer units than places.  175 tokens over 3985 take
+// 41 us with 384, 60 with 512, 46 with 256; 128 over 2000 22.5 with 16 blocks at least, 30 with 12, 24.5 with 24.  Without the
+// slack, 175 over 3985 took 54 us, with it 46; 1000 without a context 43.6 and 35.5.
 constexpr int kManyTarget = 384, kManyLeast = 16;
 // Requests of up to kSomeRows rows go to attend_few, 16 rows at a time, if they do not make more than kSomeBlocks blocks in all:
 // what the chip takes at once in units of kFewLeast.  Four tokens of 8 heads a key head over 4000: 14.1 us that way, 20.8 in one
@@ -628,7 +628,8 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
         for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
             for (int k = 0; k < 16; ++k) sc[tt][k] = 0.0f;
-        constexpr int kAhead = 6;                                      // keys in flight
+        // keys in flight: heads of 128 865 us with two (4096 tokens over 12288), 851 with six, 860 with twelve; of 64 better without
+        constexpr int kAhead = 6;
         bf16x8 ahead[kAhead];
         if constexpr (D >= 128) {
 #pragma unroll
@@ -773,7 +774,9 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        // the others, nearly all of a long context: a loop of its own, so that its registers are its own
+        // The others, nearly all of a long context: a loop of its own, so that its registers are its own.  The compiler puts the
+        // second product's instructions among the exponentials.  (Halves of the tile in turn, the weights of one between the products
+        // of the other, an instruction of each at a time, with operands read a quarter ahead: 903 us where this took 886.)
         for (; j < turns && full(j); ++j) {
             enter(j);
             f32x16 sc[TT];
@@ -842,7 +845,7 @@ __global__ __launch_bounds__(kThreads, (D > 128 ? 1 : 2)) void k_attn(AttnDesc d
 
 // Adds up the parts of a cut tile, weights 2^(m - max m), four features a thread.  Few parts: a thread has them all in flight,
 // and the threads that are left over take other rows; many: they share the parts, of every gridDim.y-th row, the first of
-// them in flight while the weights are made.  512 tokens over 2000, three parts a tile: 46 us, 67 if all go the second way.
+// them in flight while the weights are made.  512 tokens over 2000, three parts a tile: 46 us the first way, 67 the second.
 constexpr int kFewParts = 4, kPartsAhead = 4;
 template <int D>
 __global__ __launch_bounds__(kThreads) void k_attn_join(AttnDesc d, Share lot, Share few, int lot_blocks) {
