@@ -7,7 +7,7 @@
 // is known before anything is written; the only other traffic is dw.  Rows of any length and alignment: a 16-byte access
 // takes any address in one instruction, and the features behind the last whole chunk go one by one.  8192 rows of 8192 both ways
 // (1.07 GB): 192 us, 5.6 TB/s, where a large copy reaches 4.9 (93 forward, 97 backward, 4 the sum of dw); 4001 rows of 4097, an odd
-// length, 85 us; 64 rows of 4096: 4 us, of which 3.5 are an empty launch.
+// length, 84 us (30 forward, 45 backward); 64 rows of 4096: 4 us, of which 3.5 are an empty launch.
 #include <algorithm>
 
 #include "decoder.h"
@@ -23,6 +23,15 @@ __device__ __forceinline__ uint4 load_chunk(const qblora_bf16* row, int e, int d
     if (e + 8 <= d) {
         const bf16x8_any v = *reinterpret_cast<const bf16x8_any*>(row + e);
         return make_uint4(v[0], v[1], v[2], v[3]);
+    }
+    if (d >= 8) {                                                      // the row's last eight, those of this chunk to the front
+        const bf16x8_any v = *reinterpret_cast<const bf16x8_any*>(row + d - 8);
+        uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+        const int bits = 16 * (e + 8 - d);                             // 16 to 112
+        if (bits >= 64) { lo = hi; hi = 0; }
+        const int left = bits & 63;
+        if (left) { lo = lo >> left | hi << (64 - left); hi >>= left; }
+        return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
     }
     uint32_t w[4] = {0, 0, 0, 0};
     for (int j = 0; j < 8; ++j)
