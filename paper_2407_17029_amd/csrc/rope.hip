@@ -8,7 +8,7 @@
 // access.  Tokens of a prompt that go to the cache come eight to a workgroup, neighbouring lanes one behind the other, so that
 // eight keys' 16-byte octets are one 128-byte line of their page and eight values of a feature one 16-byte store; single
 // tokens come one to a workgroup, which is four times as many of them.  k_rope_any: parts of a head that are no multiple of
-// 16 features.  6693 tokens of 64 + 64 heads of 128 to the cache (658 MB): 131 us, 5.0 TB/s, where a large copy reaches 4.9; 1337 of 40 + 40 heads there and back (110 MB): 21.1 us, 5.2 TB/s; 64 single tokens of 32 + 32: 7 us, of which 3.5 are
+// 16 features.  6693 tokens of 64 + 64 heads of 128 to the cache (658 MB): 130 us, 5.1 TB/s, where a large copy reaches 4.9; 1337 of 40 + 40 heads there and back (110 MB): 21.1 us, 5.2 TB/s; 64 single tokens of 32 + 32: 7 us, of which 3.5 are
 // an empty launch.
 #include "decoder.h"
 
@@ -18,7 +18,7 @@ namespace {
 
 constexpr int kThreads = 256;
 // From here on, tokens that go to the cache are taken for prompts.  A chunk of 300: 10.3 us that way, 11.2 a token at a time, of
-// 512: 10.4 and 19.9; but 256 single tokens (which no argument tells from a chunk) 12.4 and 10.7, 512 of them 21.6 and 23.7.
+// 512: 10.4 and 19.9; but 256 single tokens (which no argument tells from a chunk) 12.4 and 10.7, 512 of them 25.6 and 23.7.
 constexpr int kManyTokens = 256;
 
 // cos and sin of p * freq: in 64 bits down to one turn, then by the hardware's functions of turns
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(kThreads) void k_rope_any(RopeDesc d) {
 
 constexpr int kHeads = 4;                      // in flight
 // From so many bytes of q and k on, nothing of the outputs is in an L2 when they are read: 1337 tokens of 40 + 40 heads (27 MB)
-// both ways 23.7 us through the caches, 21.0 past them; 6693 tokens of 64 + 64 heads to the cache 155 and 147 (131 by now).
+// both ways 23.7 us through the caches, 21.0 past them; 6693 tokens of 64 + 64 heads to the cache 155 and 147 (130 by now).
 constexpr int64_t kPastBytes = 8 << 20;
 
 template <bool PAST>
@@ -128,6 +128,24 @@ __global__ __launch_bounds__(kThreads) void k_rope(RopeDesc d, RopeGrid grid) {
         if (TB > 1) owned_tokens(d, t0, from, to);
         if (hl >= lanes) return;
         for (int64_t t = from + tb; t < to; t += TB) {
+            const int all = d.heads + d.kv_heads;
+            bf16x8_any x[kHeads][2];
+            auto load = [&](int h0) {
+#pragma unroll
+                for (int i = 0; i < kHeads; ++i) {
+                    const int h = h0 + i * lanes;
+                    if (h >= all) continue;
+                    const qblora_bf16* in = h < d.heads ? d.q + t * d.ldq + h * d.head_dim : d.k + t * d.ldk + (h - d.heads) * d.head_dim;
+                    x[i][0] = *reinterpret_cast<const bf16x8_any*>(in + 8 * c0);
+                    x[i][1] = *reinterpret_cast<const bf16x8_any*>(in + 8 * c1);
+                }
+            };
+            const int begin = hl + (int)blockIdx.y * lanes * kHeads, step = grid.qk_blocks * lanes * kHeads;
+            const int64_t slot = d.kc ? d.slots[t] : -1;
+            // The first heads are on their way while the turns are made: 2000 tokens of 64 + 8 heads to the cache 17.3 us without, 16.0
+            // with (512 single tokens, which pay for the registers: 22.1 and 25.6).  Not where many small workgroups do that for each
+            // other: 8001 of 32 + 8 both ways 61 us without, 65 with.
+            if (TB > 1) load(begin);
             float cs[8], sn[8];
             if (turns0) {
                 const int32_t p = d.positions[t];
@@ -139,18 +157,8 @@ __global__ __launch_bounds__(kThreads) void k_rope(RopeDesc d, RopeGrid grid) {
                     sn[j] *= d.sign;
                 }
             }
-            const int64_t slot = d.kc ? d.slots[t] : -1;
-            const int all = d.heads + d.kv_heads;
-            for (int h0 = hl + (int)blockIdx.y * lanes * kHeads; h0 < all; h0 += grid.qk_blocks * lanes * kHeads) {
-                bf16x8_any x[kHeads][2];
-#pragma unroll
-                for (int i = 0; i < kHeads; ++i) {
-                    const int h = h0 + i * lanes;
-                    if (h >= all) continue;
-                    const qblora_bf16* in = h < d.heads ? d.q + t * d.ldq + h * d.head_dim : d.k + t * d.ldk + (h - d.heads) * d.head_dim;
-                    x[i][0] = *reinterpret_cast<const bf16x8_any*>(in + 8 * c0);
-                    x[i][1] = *reinterpret_cast<const bf16x8_any*>(in + 8 * c1);
-                }
+            for (int h0 = begin; h0 < all; h0 += step) {
+                if (TB == 1 || h0 != begin) load(h0);
 #pragma unroll
                 for (int i = 0; i < kHeads; ++i) {
                     const int h = h0 + i * lanes;
