@@ -373,14 +373,9 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = sc[j >> 2][j & 3] * d.scale_log2;
         const bool masked = base < t.full0 || base + kBlock > t.full1 || !listed0 || !listed1;
-        uint32_t any = 0xff;                                           // of the lane's octet of values: seen by some row
         if (masked) {
-            any = 0;
-            const bool listed = g < 2 ? listed0 : listed1;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int at = base + 8 * g + j;
-                if (listed && at >= t.pos0 && at < t.pos1) any |= 1u << j;
                 const int pos = base + 16 * (j >> 2) + 4 * g + (j & 3);
                 const bool seen = pos <= here && pos > row_low && pos < t.pos1 && (j < 4 ? listed0 : listed1);
                 x[j] = seen ? x[j] : kNegInf;
@@ -415,18 +410,30 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[i][j] *= a;
         if (masked) {
-            // Values that no row sees count as 0 whatever they are: 0 * NaN would spread.  So do those of the other
-            // positions that are not finite, which some rows may see and others not; they are added behind the loop.
-            bool odd = false;
+            // A weight of 0 leaves nothing of a finite value.  If there are others: those that no row sees count as 0, 0 * NaN would
+            // spread.  So do those of the other positions, which some rows may see and others not; they are added behind the loop.
+            u16x2 most = {0, 0};
 #pragma unroll
-            for (int i = 0; i < DT; ++i) {
-                const uint4 v = make_uint4(vf[i].x & mask_of(any), vf[i].y & mask_of(any >> 2), vf[i].z & mask_of(any >> 4), vf[i].w & mask_of(any >> 6));
-                odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
-                vf[i] = make_uint4(without_not_finite(v.x), without_not_finite(v.y), without_not_finite(v.z), without_not_finite(v.w));
-            }
-            if (__any(odd)) {
-                odd0 = min(odd0, base);
-                odd1 = base + kBlock;
+            for (int i = 0; i < DT; ++i)
+                most = larger(larger(larger(most, exponents(vf[i].x)), larger(exponents(vf[i].y), exponents(vf[i].z))), exponents(vf[i].w));
+            if (__any(most[0] == 0x7f80 || most[1] == 0x7f80)) {
+                uint32_t any = 0;                                      // of the lane's octet of values: seen by some row
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int at = base + 8 * g + j;
+                    if ((g < 2 ? listed0 : listed1) && at >= t.pos0 && at < t.pos1) any |= 1u << j;
+                }
+                bool odd = false;
+#pragma unroll
+                for (int i = 0; i < DT; ++i) {
+                    const uint4 v = make_uint4(vf[i].x & mask_of(any), vf[i].y & mask_of(any >> 2), vf[i].z & mask_of(any >> 4), vf[i].w & mask_of(any >> 6));
+                    odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
+                    vf[i] = make_uint4(without_not_finite(v.x), without_not_finite(v.y), without_not_finite(v.z), without_not_finite(v.w));
+                }
+                if (__any(odd)) {
+                    odd0 = min(odd0, base);
+                    odd1 = base + kBlock;
+                }
             }
         }
 #pragma unroll
