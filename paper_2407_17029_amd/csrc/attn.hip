@@ -20,7 +20,8 @@
 // 4096 tokens over 12288, 32 heads (962 GFLOP): 853 us, 1130 TFLOP/s, 0.84 of what the library's large product reaches on the
 // chip; two workgroups a CU, the matrix pipe busy for 0.59 of the cycles and the vector ALU for 0.48, at a power-limited 1.7
 // GHz.  In small calls a tile takes 1.1 us of a workgroup alone on its CU and 1.9 of each of two, its start 3 to 5 us, the
-// store of a part up to 1.7.
+// store of a part up to 1.7.  Heads of 64 are bound by the exponentials (4096 tokens over 4000, 32 heads, 203 GFLOP: 241 us, 845
+// TFLOP/s), heads of 256 by one wave a SIMD (2000 over 2000, 16 heads, 98 GFLOP: 179 us, 550 TFLOP/s).
 //
 // Work: requests differ by orders of magnitude, and only the device knows their lengths.  Every workgroup adds up the work
 // of all requests, which gives the number of positions that a workgroup takes if there are to be `target` of them, and finds
