@@ -54,11 +54,14 @@ enum { FEW = 1, LOT = 2, ALL = 3 };            // the requests of few rows, thos
 struct Share { int rows, target, least, slack, form; int* cuts; CutTile* cut; float* part; };
 // Few rows: with 512 units 4 contexts of 30000 to 131000 take 148 us, with 1024 131, with 2048 138; single tokens of 16 x 1000 to
 // 8000 positions 55.6, 50.7 and 55.6.  With 4 blocks at least, one of 4095 takes 20.3, with 8 17.1, with 16 17.2.
-constexpr int kFewTarget = 1024, kFewLeast = 8;
+// Heads of 256 leave one workgroup a CU: 4 of 16 / 4 heads over 10000 to 60000 119 us with 1024, 111 with 512, 144 with 256 (64 of
+// 16 over 500 to 3000 241, 247 and 247).
+constexpr int kFewTarget = 1024, kFewWideTarget = 512, kFewLeast = 8;
 // More rows: every part costs 66 KB of writes and as many of reads, so there are fewer units than places.  175 tokens over 3985 take
 // 41 us with 384, 60 with 512, 46 with 256; 128 over 2000 22.5 with 16 blocks at least, 30 with 12, 24.5 with 24.  Without the
 // slack, 175 over 3985 took 54 us, with it 46; 1000 without a context 43.6 and 35.5.
-constexpr int kManyTarget = 384, kManyLeast = 16;
+// Heads of 256: 512 tokens of 16 heads over 2000 79 us with 384, which is one round and a half, and 51 with 256.
+constexpr int kManyTarget = 384, kManyWideTarget = 256, kManyLeast = 16;
 // Requests of up to kSomeRows rows go to attend_few, 16 rows at a time, if they do not make more than kSomeBlocks blocks in all:
 // what the chip takes at once in units of kFewLeast.  Four tokens of 8 heads a key head over 4000: 14.1 us that way, 20.8 in one
 // tile of 128 rows; 16 of those requests, above the limit, 48.9 and 43.7.
@@ -978,17 +981,17 @@ void lay_out(Space& space, int kv_heads, int head_dim, bool many, Share& lot, Sh
     lot.cut = space.take<CutTile>(lot.target);
     lot.part = space.take<float>((size_t)2 * lot.target * kv_heads * kManyRows * (head_dim + 2));
 }
-Share few_share(int kv_heads, bool many) {
-    return Share{kFewRows, target_of(kFewTarget, kv_heads), kFewLeast, 0, many ? FEW : ALL, nullptr, nullptr, nullptr};
+Share few_share(int kv_heads, int head_dim, bool many) {
+    return Share{kFewRows, target_of(head_dim > 128 ? kFewWideTarget : kFewTarget, kv_heads), kFewLeast, 0, many ? FEW : ALL, nullptr, nullptr, nullptr};
 }
-Share lot_share(int kv_heads) {
-    return Share{kManyRows, target_of(kManyTarget, kv_heads), kManyLeast, 1, LOT, nullptr, nullptr, nullptr};
+Share lot_share(int kv_heads, int head_dim) {
+    return Share{kManyRows, target_of(head_dim > 128 ? kManyWideTarget : kManyTarget, kv_heads), kManyLeast, 1, LOT, nullptr, nullptr, nullptr};
 }
 
 template <int D>
 int launch(const AttnDesc& d, hipStream_t st) {
     const bool many = many_rows(d.group, d.max_new);
-    Share few = few_share(d.kv_heads, many), lot = lot_share(d.kv_heads);
+    Share few = few_share(d.kv_heads, D, many), lot = lot_share(d.kv_heads, D);
     Space space(d.part);
     lay_out(space, d.kv_heads, D, many, lot, few);
     // rows of m requests make at most (rows + m (size - 1)) / size tiles
@@ -1028,7 +1031,7 @@ int launch(const AttnDesc& d, hipStream_t st) {
 
 size_t attention_part_bytes(int head_dim, int kv_heads, int group, int max_new) {
     const bool many = many_rows(group, max_new);
-    Share few = few_share(kv_heads, many), lot = lot_share(kv_heads);
+    Share few = few_share(kv_heads, head_dim, many), lot = lot_share(kv_heads, head_dim);
     Space space(nullptr);
     lay_out(space, kv_heads, head_dim, many, lot, few);
     return space.bytes;
