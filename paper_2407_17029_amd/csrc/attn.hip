@@ -3,6 +3,10 @@
 //   out = sum_j e_j v_j / sum_j e_j,  e_j = exp(scale q.k_j - m),  over the positions j a row sees, in one pass: m is the
 //   maximum so far, and what was summed under a smaller one is multiplied by 2^(old - new) (the exponents are in base 2).
 //
+// Scores, maxima, sums and parts are fp32.  The weights e_j are rounded to bf16, as the matrix instruction takes the second
+// product's operands: 2^-9 of each, which many positions average out (0.002 of the result's size where an output's own rounding is
+// 0.0017); the sum below the line is of the unrounded ones.
+//
 // A row is a query head of a new token; the rows of one request that share a key / value head go together, token by token
 // (row r: token r / group, head r % group of the group), so that the cache is read once for all of them.
 //
@@ -491,19 +495,14 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
-// 64 lanes x 16 bytes from anywhere to lds_base + 16 * lane
-__device__ __forceinline__ void gather_to_lds(const void* p, uint32_t lds_base) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_base), "v"(p) : "memory");
-}
-// the same from uniform_base + lane_offset
+// 64 lanes x 16 bytes from uniform_base + lane_offset to lds_base + 16 * lane
 __device__ __forceinline__ void copy_to_lds(const void* uniform_base, uint32_t lane_offset, uint32_t lds_base) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds_base), "v"(lane_offset), "s"(uniform_base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds_base), "v"(lane_offset), "s"(uniform_base) : "memory", "m0");
 }
-// until at most N of the wave's copies are on their way
-template <int N>
+// until none of the wave's copies is on its way
 __device__ __forceinline__ void wait_for_copies() {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt((N & 15) | 7 << 4 | 15 << 8 | (N >> 4) << 14);            // vmcnt alone
+    __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);                      // vmcnt alone, 0
     asm volatile("" ::: "memory");
 }
 
@@ -708,7 +707,7 @@ __device__ __forceinline__ void attend_many(const AttnDesc& d, const Share& shar
     };
     auto enter = [&](int j) {                                          // tile j is there, and the next one is copied
         listed = next_listed;
-        wait_for_copies<0>();
+        wait_for_copies();
         meet();
         if (j + 1 < turns) next_listed = copy(j + 1);
     };

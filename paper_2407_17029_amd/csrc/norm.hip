@@ -3,6 +3,9 @@
 //   total = bf16(x + residual),  r = 1 / sqrt(mean(total^2) + eps),  y = total * r * w
 //   dx = r (g - h mean(g h)) + dtotal,  dw = sum_t dy h,  with h = total * r, g = dy * w
 //
+// Everything between the bf16 arrays is fp32; the sum is rounded before it is normed, as it is what the next layer and the
+// backward pass get.
+//
 // Bound by HBM: one pass over each array.  A workgroup holds a row in registers, 8 features a thread and chunk, so the mean
 // is known before anything is written; the only other traffic is dw.  Rows of any length and alignment: a 16-byte access
 // takes any address in one instruction, and the features behind the last whole chunk go one by one.  8192 rows of 8192 both ways
