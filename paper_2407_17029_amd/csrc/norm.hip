@@ -8,9 +8,10 @@
 //
 // Bound by HBM: one pass over each array.  A workgroup holds a row in registers, 8 features a thread and chunk, so the mean
 // is known before anything is written; the only other traffic is dw.  Rows of any length and alignment: a 16-byte access
-// takes any address in one instruction, and the features behind the last whole chunk go one by one.  8192 rows of 8192 both ways
-// (1.07 GB): 192 us, 5.6 TB/s, where a large copy reaches 4.9 (93 forward, 97 backward, 4 the sum of dw); 4001 rows of 4097, an odd
-// length, 84 us (30 forward, 45 backward); 64 rows of 4096: 4 us, of which 3.5 are an empty launch.
+// takes any address in one instruction; the features behind the last whole chunk are read with the row's last eight and written
+// one by one.  8192 rows of 8192 both ways (1.07 GB): 192 us, 5.6 TB/s, where a large copy reaches 4.9 (93 forward, 97 backward, 4
+// the sum of dw); 4001 rows of 4097, an odd length, 84 us (30 forward, 45 backward); 64 rows of 4096: 4 us, of which 3.5 are an
+// empty launch.
 #include <algorithm>
 
 #include "decoder.h"
