@@ -166,3 +166,57 @@ def test_a_few_tokens_of_several_requests(n, ctx, new, heads, kv_heads, dim):
     if n in (8, 65):
         fresh[n // 2] = 40
     _check(_batch(n + ctx, context, fresh, 16, heads, kv_heads, dim), window=100 if n == 3 else 0)
+
+
+@pytest.mark.parametrize("T", [256, 300, 513])
+@pytest.mark.parametrize("lengths", [[1], [1, 1, 1, 1, 9], [2, 3], [40, 1, 1]])
+@pytest.mark.parametrize("page", [16, 64])
+def test_many_tokens_of_short_runs_to_the_cache(T, lengths, page):
+    """Slots that follow each other for so many tokens, then begin somewhere else; every seventeenth lies outside the cache.  The
+    tolerance is that of test_gpu_rope.py."""
+    import decoder_util as du
+    from test_gpu_rope import _delta, _freq
+    from paper_2407_17029_amd import binding as qb
+    heads, kv_heads, dim = 3, 2, 64
+    r = np.random.Generator(np.random.Philox(key=[T, len(lengths) + page]))
+    pages = T // page * 2 + 8
+    starts, slots, at = r.permutation(pages * page // 40) * 40, [], 0       # (a run is at most 40 long)
+    while len(slots) < T:
+        n = lengths[at % len(lengths)]
+        slots += list(starts[at % len(starts)] + np.arange(n)) if at < len(starts) else [-1]
+        at += 1
+    slots = np.array(slots[:T], np.int64)
+    slots[::17] = np.where(np.arange(len(slots[::17])) % 2, -3, pages * page + 5)
+    q, k, v = (du.bf16(r.standard_normal((T, h, dim))) for h in (heads, kv_heads, kv_heads))
+    p, f = r.integers(0, 100000, T).astype(np.int32), _freq(dim)
+    kc0, vc0 = (du.bf16(r.standard_normal((pages, page, kv_heads, dim))) for _ in range(2))
+    kc, vc = du.dev_bf16(du.key_pages(kc0)), du.dev_bf16(du.value_pages(vc0))
+    got = qb.qblora_rope_cache(du.dev_bf16(q), du.dev_bf16(k), du.dev_bf16(v), du.dev_i32(p), torch.from_numpy(slots).to(du.DEV),
+                               torch.from_numpy(f).to(du.DEV), kc, vc)
+    torch.cuda.synchronize()
+    du.assert_bf16(got, du.rope(q, p, f, False, 1.0), _delta(q, dim, False, 1.0), "q")
+    inside = (slots >= 0) & (slots < pages * page)
+    s = slots[inside]
+    assert len(set(s.tolist())) == len(s)
+    want_k, delta_k, want_v = kc0.copy(), np.zeros_like(kc0), vc0.copy()
+    want_k[s // page, s % page] = du.rope(k, p, f, False, 1.0)[inside]
+    delta_k[s // page, s % page] = _delta(k, dim, False, 1.0)[inside]
+    want_v[s // page, s % page] = v[inside]
+    du.assert_bf16(kc, du.key_pages(want_k), du.key_pages(delta_k), "keys")
+    assert np.array_equal(du.host(vc), du.value_pages(want_v)), "values"
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_mixed_batches(seed):
+    """Chunks, single tokens and idle requests of one batch, windows, pages that are not listed, a wrong max_new."""
+    r = np.random.Generator(np.random.Philox(key=[seed, 77]))
+    heads, kv_heads = [(4, 4), (8, 1), (6, 2), (16, 1), (20, 2), (8, 2)][seed % 6]
+    dim, page = [64, 128, 256][seed % 3], [16, 32, 64, 256][seed % 4]
+    n = [2, 5, 12, 66][seed // 6]
+    context = [int(x) for x in r.integers(0, 400, n)]
+    fresh = [int(x) for x in r.choice([0, 1, 1, 1, 4, 9] + [90] * (n < 20), n)]
+    fresh[0] = 7
+    b = _batch(seed, context, fresh, page, heads, kv_heads, dim)
+    if seed % 5 == 0:
+        b.table[r.random(b.table.shape) < 0.2] = [-1, 10 ** 6][seed % 2]
+    _check(b, window=[0, 0, 33, 200][seed % 4], max_new=[None, max(fresh), 1][seed % 3])
