@@ -35,6 +35,7 @@
 #include <climits>
 #include <type_traits>
 
+#include "attn_units.h"
 #include "decoder.h"
 
 namespace qblora {
@@ -55,7 +56,7 @@ constexpr float kSlack = 8.0f;
 // `slack`, into as many as come nearest.  Cut tiles leave their parts in `part` and themselves in `cut`; `cuts` counts them.
 struct CutTile { int token0, rem0, rows, splits, slot, pad[3]; };
 enum { FEW = 1, LOT = 2, ALL = 3 };            // the requests of few rows, those of more, or all
-struct Share { int rows, target, least, slack, form; int* cuts; CutTile* cut; float* part; };
+struct Share { int rows, target, least, slack, form, grid_units; int* cuts; CutTile* cut; float* part; };   // grid_units: a key / value head
 // Few rows: with 512 units 4 contexts of 30000 to 131000 take 148 us, with 1024 131, with 2048 138; single tokens of 16 x 1000 to
 // 8000 positions 55.6, 50.7 and 55.6.  With 4 blocks at least, one of 4095 takes 20.3, with 8 17.1, with 16 17.2.
 // Heads of 256 leave one workgroup a CU: 4 of 16 / 4 heads over 10000 to 60000 119 us with 1024, 111 with 512, 144 with 256 (64 of
@@ -106,7 +107,6 @@ __device__ __forceinline__ int64_t sum_of_wave(int64_t x) {
     return x;
 }
 
-struct Cost { int tiles, blocks; };
 __device__ __forceinline__ int blocks_of(const AttnDesc& d, const Span& s) {
     const int limit = d.width << d.page_shift;
     const int hi = min(s.context + s.fresh, limit), lo = d.window ? max(s.context + 1 - d.window, 0) : 0;
@@ -119,24 +119,8 @@ __device__ __forceinline__ Cost cost_of(const AttnDesc& d, const Span& s, const 
     return {(int)((rows + w.rows - 1) / w.rows), blocks_of(d, s)};
 }
 
-// Blocks of a unit, from the blocks of all tiles
-__device__ __forceinline__ int64_t blocks_per_unit(int64_t all, const Share& w) {
-    const int64_t per = all >> 32 ? (all + w.target - 1) / w.target : (int64_t)(((uint32_t)all + (uint64_t)w.target - 1) >> 32 ? (all + w.target - 1) / w.target
-                                                                                  : ((uint32_t)all + w.target - 1) / (uint32_t)w.target);
-    return max(per, (int64_t)w.least);
-}
-struct Units { int tiles, splits, count, cuts; };                      // cuts: parts, and cut tiles in the upper half
-__device__ __forceinline__ Units units_of(const Cost& c, int64_t per, int slack) {
-    Units u;
-    u.tiles = c.tiles;
-    u.splits = max(1, (int)(((uint32_t)c.blocks + (uint32_t)(slack ? per / 2 : per - 1)) / (uint32_t)per));
-    u.count = u.tiles * u.splits;
-    u.cuts = u.splits > 1 ? u.count + (u.tiles << 16) : 0;
-    return u;
-}
-
 // The unit number `want` of the batch; false: there are not so many.  With `first`, the number of cut tiles is left where
-// k_attn_join looks for it.  All threads call it.  Up to 64 requests every wave finds it by itself, a request a lane; more
+// k_attn_join looks for it: 0 if there are more units than the grid runs, as an entry that no workgroup writes is not to be read.  All threads call it.  Up to 64 requests every wave finds it by itself, a request a lane; more
 // are taken a workgroup's threads at a time.
 struct Finder {
     int64_t sums[kWaves];
@@ -157,13 +141,14 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
             }
         }
         const Cost c = cost_of(d, s, share, some);
-        const Units v = units_of(c, blocks_per_unit(sum_of_wave((int64_t)c.tiles * c.blocks), share), share.slack);
-        const int a = scan(v.count), b = scan(v.cuts);
-        if (first && tid == 63) *share.cuts = b >> 16;
-        const uint64_t hit = __ballot(v.count && a - v.count <= want && want < a);
+        const Units v = units_of(c, blocks_per_unit(sum_of_wave((int64_t)c.tiles * c.blocks), share.target, share.least), share.slack);
+        const int mine = units_within(v.count, share.grid_units);
+        const int a = scan(mine), b = scan(v.cuts);
+        if (first && tid == 63) *share.cuts = cut_tiles(b, a, share.grid_units);
+        const uint64_t hit = __ballot(mine && a - mine <= want && want < a);
         if (!hit) return false;
         const int at = __builtin_ctzll(hit);
-        const int count = __builtin_amdgcn_readlane(v.count, at), number = want - (__builtin_amdgcn_readlane(a, at) - count);
+        const int number = want - __builtin_amdgcn_readlane(a - mine, at);
         const int before = __builtin_amdgcn_readlane(b - v.cuts, at);
         u.request = at;
         u.splits = __builtin_amdgcn_readlane(v.splits, at);
@@ -184,24 +169,25 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
     __syncthreads();
     all = 0;
     for (int w = 0; w < kWaves; ++w) all += f.sums[w];
-    const int64_t per = blocks_per_unit(all, share);
+    const int64_t per = blocks_per_unit(all, share.target, share.least);
     int units = 0, cuts = 0;                                           // in front of these requests
     for (int base = 0; base < d.n; base += kThreads) {
         const int i = base + tid;
         Cost c{0, 0};
         if (i < d.n) c = cost_of(d, span_of(d, i), share, kFewRows);
         const Units v = units_of(c, per, share.slack);
-        int a = scan(v.count), b = scan(v.cuts);
+        const int mine = units_within(v.count, share.grid_units);
+        int a = scan(mine), b = scan(v.cuts);
         __syncthreads();
         if (lane == 63) { f.ends[0][wave] = a; f.ends[1][wave] = b; }
         __syncthreads();
         for (int w = 0; w < kWaves; ++w) {
             if (w == wave) { a += units; b += cuts; }
-            units += f.ends[0][w];
+            units = add_units(units, f.ends[0][w]);
             cuts += f.ends[1][w];
         }
-        if (v.count && a - v.count <= want && want < a) {
-            const int number = want - (a - v.count), before = b - v.cuts;
+        if (mine && a - mine <= want && want < a) {
+            const int number = want - (a - mine), before = b - v.cuts;
             f.found[0] = i;
             f.found[1] = number / v.splits;
             f.found[2] = number % v.splits;
@@ -212,7 +198,7 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
         __syncthreads();
         if (f.found[0] >= 0 && !first) break;
     }
-    if (first && tid == 0) *share.cuts = cuts >> 16;
+    if (first && tid == 0) *share.cuts = cut_tiles(cuts, units, share.grid_units);
     u.request = __builtin_amdgcn_readfirstlane(f.found[0]);
     if (u.request < 0) return false;
     u.tile = __builtin_amdgcn_readfirstlane(f.found[1]);
@@ -981,10 +967,10 @@ void lay_out(Space& space, int kv_heads, int head_dim, bool many, Share& lot, Sh
     lot.part = space.take<float>((size_t)2 * lot.target * kv_heads * kManyRows * (head_dim + 2));
 }
 Share few_share(int kv_heads, int head_dim, bool many) {
-    return Share{kFewRows, target_of(head_dim > 128 ? kFewWideTarget : kFewTarget, kv_heads), kFewLeast, 0, many ? FEW : ALL, nullptr, nullptr, nullptr};
+    return Share{kFewRows, target_of(head_dim > 128 ? kFewWideTarget : kFewTarget, kv_heads), kFewLeast, 0, many ? FEW : ALL, 0, nullptr, nullptr, nullptr};
 }
 Share lot_share(int kv_heads, int head_dim) {
-    return Share{kManyRows, target_of(head_dim > 128 ? kManyWideTarget : kManyTarget, kv_heads), kManyLeast, 1, LOT, nullptr, nullptr, nullptr};
+    return Share{kManyRows, target_of(head_dim > 128 ? kManyWideTarget : kManyTarget, kv_heads), kManyLeast, 1, LOT, 0, nullptr, nullptr, nullptr};
 }
 
 template <int D>
@@ -998,14 +984,13 @@ int launch(const AttnDesc& d, hipStream_t st) {
     const auto tiles_of = [&](int size) { return (rows + requests * (size - 1)) / size; };
     const int64_t lot_tiles = many ? tiles_of(kManyRows) : 0;
     const int64_t few_tiles = many ? std::min(tiles_of(kFewRows), requests * (d.n > 64 ? 1 : kSomeRows / kFewRows)) : tiles_of(kFewRows);
-    // A unit more than what the target makes for every tile, and no more than the longest row of the table allows.
     const int64_t blocks_of_row = (((int64_t)d.width << d.page_shift) + kBlock - 1) / kBlock + 1;
-    const auto units = [&](int64_t tiles, const Share& w) {
-        const int64_t most = tiles * ((blocks_of_row + w.least - 1) / w.least);
-        return std::max<int64_t>(std::min(most, tiles + w.target), 1) * d.kv_heads;
-    };
-    const int64_t lot_blocks = many ? units(lot_tiles, lot) : 0, blocks = lot_blocks + units(few_tiles, few);
+    const int64_t lot_units = many ? units_of_grid(lot_tiles, blocks_of_row, lot.target, lot.least) : 0;
+    const int64_t few_units = units_of_grid(few_tiles, blocks_of_row, few.target, few.least);
+    const int64_t lot_blocks = lot_units * d.kv_heads, blocks = lot_blocks + few_units * d.kv_heads;
     if (blocks > INT32_MAX) return QBLORA_ERR_UNSUPPORTED;
+    lot.grid_units = (int)lot_units;
+    few.grid_units = (int)few_units;
     const auto go = [&](auto kernel, int64_t count) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(kThreads), 0, st, d, lot, few, (int)lot_blocks);
     };

@@ -1,0 +1,115 @@
+"""How attention shares out a batch (csrc/attn_units.h), compiled for the host: whatever the lengths are, parts and cut tiles stay
+within their lists, and no tile is joined that a workgroup of the grid has not written.  No GPU is needed."""
+import ctypes as C
+import os
+import random
+import subprocess
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2407_17029_amd", "csrc")
+SHIM = """
+#include "attn_units.h"
+using namespace qblora;
+extern "C" {
+int64_t per_unit(int64_t all, int target, int least) { return blocks_per_unit(all, target, least); }
+void units(int tiles, int blocks, int64_t per, int slack, int* out) {
+    const Units u = units_of(Cost{tiles, blocks}, per, slack);
+    out[0] = u.tiles; out[1] = u.splits; out[2] = u.count; out[3] = u.cuts;
+}
+int64_t grid(int64_t tiles, int64_t blocks_of_row, int target, int least) { return units_of_grid(tiles, blocks_of_row, target, least); }
+int within(int count, int grid_units) { return units_within(count, grid_units); }
+int add(int a, int b) { return add_units(a, b); }
+int joined(int cuts, int total, int grid_units) { return cut_tiles(cuts, total, grid_units); }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def rules(tmp_path_factory):
+    d = tmp_path_factory.mktemp("attn_units")
+    (d / "shim.cpp").write_text(SHIM)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", f"-I{CSRC}", "-o", str(d / "shim.so"), str(d / "shim.cpp")], check=True)
+    L = C.CDLL(str(d / "shim.so"))
+    L.per_unit.argtypes, L.per_unit.restype = [C.c_int64, C.c_int, C.c_int], C.c_int64
+    L.units.argtypes = [C.c_int, C.c_int, C.c_int64, C.c_int, C.c_void_p]
+    L.grid.argtypes, L.grid.restype = [C.c_int64, C.c_int64, C.c_int, C.c_int], C.c_int64
+    return L
+
+
+# rows of a tile, units aimed at for a key / value head, least blocks of a unit, slack: as launch() has them for 1 to 64 heads
+FORMS = [(16, 1024 // kv, 8, 0) for kv in (1, 8, 64)] + [(128, 384 // kv, 16, 1) for kv in (1, 8, 64)]
+
+
+def share_out(rules, form, starts, T, group, contexts, row_positions):
+    """What a call of all requests in one form leaves: units, parts, cut tiles, the cut tiles that are joined, the grid's units."""
+    rows, target, least, slack = form
+    costs = []
+    for i, context in enumerate(contexts):
+        s0 = min(max(starts[i], 0), T)
+        fresh = min(max(starts[i + 1], s0), T) - s0
+        blocks = max(1, -(-min(context + fresh, row_positions) // 32))
+        costs.append((-(-fresh * group // rows), blocks) if fresh else (0, 0))
+    per = rules.per_unit(sum(t * b for t, b in costs), target, least)
+    requests = min(len(contexts), T)
+    grid = rules.grid((T * group + requests * (rows - 1)) // rows, row_positions // 32 + 1, target, least)
+    out = (C.c_int * 4)()
+    total = cuts = units = parts = cut = 0
+    for t, b in costs:
+        rules.units(t, b, per, slack, out)
+        assert out[0] == t and out[1] >= 1 and out[2] == t * out[1]
+        if out[1] > 1:
+            assert out[1] <= target                                        # the join holds one weight of each part
+            parts, cut = parts + out[2], cut + t
+        units += out[2]
+        total = rules.add(total, rules.within(out[2], grid))
+        assert 0 <= total < 1 << 27
+        cuts += out[3]
+    assert cuts == parts + (cut << 16)
+    assert parts <= 2 * target and cut <= target
+    return units, parts, cut, rules.joined(cuts, total, grid), grid
+
+
+def lengths(r, n):
+    return [r.choice([0, 1, r.randint(0, 300), r.randint(0, 5000), r.randint(0, 200000)]) for _ in range(n)]
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_requests_that_follow_each_other_fit_their_grid(rules, form):
+    r = random.Random(1)
+    some = 0
+    for _ in range(1500):
+        n, group = r.choice([1, 2, 5, 40, 300]), r.choice([1, 3, 8, 16])
+        fresh = [r.choice([0, 1, 1, r.randint(1, 40), r.randint(1, 2000)]) for _ in range(n)]
+        starts = [0]
+        for m in fresh:
+            starts.append(starts[-1] + m)
+        contexts = lengths(r, n)
+        row = -(-max(c + m for c, m in zip(contexts, fresh)) // 256) * 256 + 256
+        units, _, cut, joined, grid = share_out(rules, form, starts, starts[-1], group, contexts, row)
+        if starts[-1]:
+            assert units <= grid and joined == cut
+        some += cut > 0
+    assert some > 200
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_no_tile_is_joined_that_has_not_run(rules, form):
+    """Starts in any order count tokens more than once: more units than the grid has, and the tiles of those that never run
+    are not in the list."""
+    r = random.Random(2)
+    more = 0
+    for _ in range(1500):
+        n, T = r.choice([2, 5, 40, 300]), r.choice([1, 16, 64, 500])
+        starts = [r.choice([0, T, r.randint(-5, T + 5), 2**31 - 1]) for _ in range(n + 1)]
+        contexts = lengths(r, n)
+        units, _, cut, joined, grid = share_out(rules, form, starts, T, r.choice([1, 8]), contexts, r.choice([256, 3072, 300032]))
+        assert joined == (cut if units <= grid else 0)
+        more += units > grid and cut > 0
+    assert more > 20
+
+
+def test_an_example_of_starts_that_do_not_ascend(rules):
+    """Three requests of all 64 tokens, 8 heads each, over 3000 positions: 72 units where the grid has 63."""
+    units, _, cut, joined, grid = share_out(rules, (128, 384, 16, 1), [0, 64, 0, 64, 0, 64, 0], 64, 8, [3000] * 6, 3200)
+    assert (units, grid, cut, joined) == (72, 63, 12, 0)
