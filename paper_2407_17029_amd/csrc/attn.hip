@@ -169,7 +169,7 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
     __syncthreads();
     all = 0;
     for (int w = 0; w < kWaves; ++w) all += f.sums[w];
-    const int64_t per = blocks_per_unit(all, share.target, share.least);
+    const int per = blocks_per_unit(all, share.target, share.least);
     int units = 0, cuts = 0;                                           // in front of these requests
     for (int base = 0; base < d.n; base += kThreads) {
         const int i = base + tid;

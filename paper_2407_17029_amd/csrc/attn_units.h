@@ -12,15 +12,16 @@ constexpr int larger_of(int a, int b) { return a > b ? a : b; }
 
 struct Cost { int tiles, blocks; };            // of a request: its tiles, and the blocks of each
 
-// Blocks of a unit, from the blocks of all tiles
-constexpr int64_t blocks_per_unit(int64_t all, int target, int least) {
-    const int64_t per = all >> 32 ? (all + target - 1) / target : (int64_t)(((uint32_t)all + (uint64_t)target - 1) >> 32 ? (all + target - 1) / target
-                                                                                  : ((uint32_t)all + target - 1) / (uint32_t)target);
-    return per > least ? per : least;
+// Blocks of a unit, from the blocks of all tiles.  A tile is at most 2^25 + 1 blocks: a unit of kLongUnit is never cut, and no larger
+// one is told from it.  (The sum of all tiles may pass 2^32 times the target, where starts count tokens more than once.)
+constexpr int kLongUnit = 1 << 30;
+constexpr int blocks_per_unit(int64_t all, int target, int least) {
+    const int64_t per = all >> 31 ? (all + target - 1) / target : ((uint32_t)all + (uint32_t)target - 1) / (uint32_t)target;
+    return per >= kLongUnit ? kLongUnit : larger_of((int)per, least);
 }
 
 struct Units { int tiles, splits, count, cuts; };                      // cuts: parts, and cut tiles in the upper half
-constexpr Units units_of(const Cost& c, int64_t per, int slack) {
+constexpr Units units_of(const Cost& c, int per, int slack) {
     const int splits = larger_of(1, (int)(((uint32_t)c.blocks + (uint32_t)(slack ? per / 2 : per - 1)) / (uint32_t)per));
     const int count = c.tiles * splits;
     return {c.tiles, splits, count, splits > 1 ? count + (c.tiles << 16) : 0};

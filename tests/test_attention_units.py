@@ -113,3 +113,28 @@ def test_an_example_of_starts_that_do_not_ascend(rules):
     """Three requests of all 64 tokens, 8 heads each, over 3000 positions: 72 units where the grid has 63."""
     units, _, cut, joined, grid = share_out(rules, (128, 384, 16, 1), [0, 64, 0, 64, 0, 64, 0], 64, 8, [3000] * 6, 3200)
     assert (units, grid, cut, joined) == (72, 63, 12, 0)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_units_of_more_blocks_than_32_bits_count(rules, form):
+    """Sums of blocks up to 2^60: a tile is at most 2^25 blocks, so a unit of more needs no cut."""
+    rows, target, least, slack = form
+    out = (C.c_int * 4)()
+    sizes = [(1 << k) + d for k in range(20, 61) for d in (-1, 0, 1, 5)] + [target * ((1 << 32) * k + d) for k in (1, 2, 7) for d in (0, 1, 3, 100)]
+    for every in sizes:
+        per = rules.per_unit(every, target, least)
+        for blocks in (1, 100, 4096, 1 << 20, (1 << 25) + 1):
+            if blocks > every:
+                continue
+            rules.units(1, blocks, per, slack, out)
+            exact = max(-(-every // target), least)
+            assert out[1] == max(1, (blocks + (exact // 2 if slack else exact - 1)) // exact), (every, blocks)
+            assert out[1] <= target
+
+
+def test_batches_of_long_rows_and_many_tokens(rules):
+    """2048 requests that all count the same 2048 tokens of 16 heads, over the longest rows there are, in the single tokens' form for 64
+    key / value heads: 2^37 blocks in all, 2^33 a unit."""
+    for form in FORMS:
+        units, parts, cut, _, _ = share_out(rules, form, [0, 2048] * 2049, 2048, 16, [1 << 30] * 4096, 1 << 30)
+        assert units >= 4096 // 2 * 2048 * 16 // form[0]
