@@ -489,8 +489,9 @@ int qblora_rope_frequencies(int32_t rot, double base, int32_t kind, double facto
 
 /*
  * Attention of the new tokens over the paged cache.  Request i has context[i] positions in front of its new tokens
- * starts[i] .. starts[i+1] - 1 (int32 [n + 1], as qblora_page_tables writes them); its positions are in the pages that row i
- * of `table` (int32 [n, width]) lists, those of the new tokens among them.  For new token t at position
+ * starts[i] .. starts[i+1] - 1 (int32 [n + 1], ascending, as qblora_page_tables writes them; what requests that share tokens get is
+ * not specified); context[i] counts as the nearest number from 0 to 2^30 - 1.  Its positions are in the pages that row i of
+ * `table` (int32 [n, width], width * page <= 2^30) lists, those of the new tokens among them.  For new token t at position
  * p = context[i] + t - starts[i], query head h and the key / value head h / (heads / cache->heads):
  *   out[t, h] = sum_j e_j v_j / sum_j e_j,  e_j = exp(scale * q[t, h] . k_j),  over the positions j it sees:
  *   0 <= j <= p, j > p - window (window = 0: no limit), and j in a page that the table lists (entries outside 0 .. pages-1

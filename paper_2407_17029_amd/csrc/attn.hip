@@ -44,7 +44,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kFewRows = 16;
-constexpr int kBlock = 32;                     // positions of a step
+constexpr int kBlock = kAttnBlock;             // positions of a step
 constexpr int kManyRows = 128;
 constexpr float kNegInf = -__builtin_inff();
 // A maximum may grow by 2^8 before what was summed is rescaled: the weights stay below 2^8 and most steps do without the 64
@@ -82,7 +82,7 @@ struct Unit { int request, tile, split, splits, slot, cut; };
 struct Span { int start, fresh, context; };
 __device__ __forceinline__ Span span_of(const AttnDesc& d, int i) {
     const int s0 = min(max(d.starts[i], 0), d.T), s1 = min(max(d.starts[i + 1], s0), d.T);
-    return {s0, s1 - s0, min(max(d.context[i], 0), 1 << 30)};
+    return {s0, s1 - s0, context_of(d.context[i])};
 }
 
 // of a request that the whole wave works on
@@ -108,9 +108,7 @@ __device__ __forceinline__ int64_t sum_of_wave(int64_t x) {
 }
 
 __device__ __forceinline__ int blocks_of(const AttnDesc& d, const Span& s) {
-    const int limit = d.width << d.page_shift;
-    const int hi = min(s.context + s.fresh, limit), lo = d.window ? max(s.context + 1 - d.window, 0) : 0;
-    return hi > lo ? (hi + kBlock - 1) / kBlock - lo / kBlock : 1;
+    return blocks_of(s.context, s.fresh, d.width << d.page_shift, d.window);
 }
 // `some`: the rows up to which requests go to attend_few in this call, where both forms are there
 __device__ __forceinline__ Cost cost_of(const AttnDesc& d, const Span& s, const Share& w, int some) {

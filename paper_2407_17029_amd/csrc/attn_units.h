@@ -10,6 +10,18 @@ constexpr int kUnitsBound = 1 << 26;           // above any number of units of a
 constexpr int smaller(int a, int b) { return a < b ? a : b; }
 constexpr int larger_of(int a, int b) { return a > b ? a : b; }
 
+constexpr int kAttnBlock = 32;                 // positions of a block
+
+// A request's positions are counted in 32 bits: at most 2^30 new tokens behind at most 2^30 - 1 positions, which is as good as any larger
+// number, as a row of the table lists at most 2^30.
+constexpr int context_of(int context) { return smaller(larger_of(context, 0), (1 << 30) - 1); }
+
+// Blocks that hold what the new tokens see of the first `limit` positions
+constexpr int blocks_of(int context, int fresh, int limit, int window) {
+    const int hi = smaller(context + fresh, limit), lo = window ? larger_of(context + 1 - window, 0) : 0;
+    return hi > lo ? (hi + kAttnBlock - 1) / kAttnBlock - lo / kAttnBlock : 1;
+}
+
 struct Cost { int tiles, blocks; };            // of a request: its tiles, and the blocks of each
 
 // Blocks of a unit, from the blocks of all tiles.  A tile is at most 2^25 + 1 blocks: a unit of kLongUnit is never cut, and no larger

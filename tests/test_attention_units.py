@@ -18,6 +18,7 @@ void units(int tiles, int blocks, int64_t per, int slack, int* out) {
     out[0] = u.tiles; out[1] = u.splits; out[2] = u.count; out[3] = u.cuts;
 }
 int64_t grid(int64_t tiles, int64_t blocks_of_row, int target, int least) { return units_of_grid(tiles, blocks_of_row, target, least); }
+int blocks(int context, int fresh, int limit, int window) { return blocks_of(context_of(context), fresh, limit, window); }
 int within(int count, int grid_units) { return units_within(count, grid_units); }
 int add(int a, int b) { return add_units(a, b); }
 int joined(int cuts, int total, int grid_units) { return cut_tiles(cuts, total, grid_units); }
@@ -138,3 +139,16 @@ def test_batches_of_long_rows_and_many_tokens(rules):
     for form in FORMS:
         units, parts, cut, _, _ = share_out(rules, form, [0, 2048] * 2049, 2048, 16, [1 << 30] * 4096, 1 << 30)
         assert units >= 4096 // 2 * 2048 * 16 // form[0]
+
+
+def test_blocks_of_the_longest_requests(rules):
+    """Positions behind 2^30 are none of a table: the sums of lengths stay within 32 bits."""
+    most = 1 << 30
+    for context in (-5, 0, 1, most - 2, most - 1, most, 2 * most - 1):
+        for fresh in (1, 33, most - 1, most):
+            for limit in (0, 16, 4096, most):
+                for window in (0, 1, 4096, most):
+                    c = min(max(context, 0), most - 1)
+                    hi, lo = min(c + fresh, limit), max(c + 1 - window, 0) if window else 0
+                    want = -(-hi // 32) - lo // 32 if hi > lo else 1
+                    assert rules.blocks(context, fresh, limit, window) == want, (context, fresh, limit, window)
