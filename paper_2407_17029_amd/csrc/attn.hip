@@ -108,7 +108,7 @@ __device__ __forceinline__ int64_t sum_of_wave(int64_t x) {
 }
 
 __device__ __forceinline__ int blocks_of(const AttnDesc& d, const Span& s) {
-    return blocks_of(s.context, s.fresh, d.width << d.page_shift, d.window);
+    return qblora::blocks_of(s.context, s.fresh, d.width << d.page_shift, d.window);
 }
 // `some`: the rows up to which requests go to attend_few in this call, where both forms are there
 __device__ __forceinline__ Cost cost_of(const AttnDesc& d, const Span& s, const Share& w, int some) {
