@@ -11,6 +11,10 @@ typedef uint32_t bf16x4_any __attribute__((ext_vector_type(2), aligned(2)));
 __device__ __forceinline__ float bf16_lo(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
 
+// Threads of one launch.  A grid dimension has fewer than 2^32, and one of more is cut to its low 32 bits without an error: 2^24 + 77
+// tokens in workgroups of 256 left all but 77 unwritten.  Calls on more rows than this takes go in several launches.
+constexpr int64_t kMostThreads = (int64_t)1 << 30;
+
 struct TablesDesc {
     const int32_t* context; const int32_t* fresh; int n;
     int page_shift;

@@ -10,6 +10,8 @@
 // tokens come one to a workgroup, which is four times as many of them.  k_rope_any: parts of a head that are no multiple of
 // 16 features.  6693 tokens of 64 + 64 heads of 128 to the cache (658 MB): 130 us, 5.1 TB/s, where a large copy reaches 4.9; 1337 of 40 + 40 heads there and back (110 MB): 21.1 us, 5.2 TB/s; 64 single tokens of 32 + 32: 7 us, of which 3.5 are
 // an empty launch.
+#include <algorithm>
+
 #include "decoder.h"
 
 namespace qblora {
@@ -297,12 +299,32 @@ __global__ __launch_bounds__(kThreads) void k_rope(RopeDesc d, RopeGrid grid) {
     }
 }
 
+// Launches for all tokens, as many at a time as a grid takes with `tb` of them a workgroup: go(those tokens, workgroups).  A run of
+// slots that two launches share is written by one after the other.
+template <typename Go>
+void for_tokens(const RopeDesc& d, int tb, const Go& go) {
+    const int64_t most = kMostThreads / kThreads * tb;
+    for (int64_t t = 0; t < d.T; t += most) {
+        RopeDesc e = d;
+        e.T = std::min(most, d.T - t);
+        e.q += t * d.ldq;
+        e.q_out += t * d.ldq_out;
+        e.positions += t;
+        if (d.k) e.k += t * d.ldk;
+        if (d.k_out) e.k_out += t * d.ldk_out;
+        if (d.v) e.v += t * d.ldv;
+        if (d.slots) e.slots += t;
+        go(e, (unsigned)((e.T + tb - 1) / tb));
+    }
+}
+
 }  // namespace
 
 int launch_rope(const RopeDesc& d, hipStream_t st) {
     const int units = d.head_dim / 16, all = d.heads + d.kv_heads;
+    const dim3 threads(kThreads);
     if (d.head_dim % 16 != 0 || d.rot % 16 != 0 || units > kThreads / 8) {
-        hipLaunchKernelGGL(k_rope_any, dim3((unsigned)d.T), dim3(kThreads), 0, st, d);
+        for_tokens(d, 1, [&](const RopeDesc& e, unsigned blocks) { hipLaunchKernelGGL(k_rope_any, dim3(blocks), threads, 0, st, e); });
         return launch_status();
     }
     const bool prompts = d.kc && d.T >= kManyTokens;
@@ -312,8 +334,11 @@ int launch_rope(const RopeDesc& d, hipStream_t st) {
     RopeGrid g{groups, 0};
     const bool past = d.T * all * d.head_dim * 2 >= kPastBytes;
     if (d.vc) g.v_blocks = (d.kv_heads * d.head_dim / 4 + kThreads - 1) / kThreads;
-    const dim3 grid((unsigned)((d.T + tb - 1) / tb), g.qk_blocks + g.v_blocks), threads(kThreads);
-    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, threads, 0, st, d, g); };
+    const auto go = [&](auto kernel) {
+        for_tokens(d, tb, [&](const RopeDesc& e, unsigned blocks) {
+            hipLaunchKernelGGL(kernel, dim3(blocks, g.qk_blocks + g.v_blocks), threads, 0, st, e, g);
+        });
+    };
     if (tb == 8) {
         if (d.interleaved) go(past ? k_rope<8, true, true> : k_rope<8, true, false>);
         else go(past ? k_rope<8, false, true> : k_rope<8, false, false>);
