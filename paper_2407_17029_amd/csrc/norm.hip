@@ -266,9 +266,19 @@ constexpr int kColumnThreads = 512;
 int launch_rms_norm(const NormDesc& a, hipStream_t st) {
     const Plan p = plan_of(a.d);
     const bool past = past_caches(a.T, a.d);
-    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)a.T), dim3(p.threads), 0, st, a); };
-    if (p.chunks == 1) go(past ? k_rms_norm<1, true> : k_rms_norm<1, false>);
-    else go(past ? k_rms_norm<2, true> : k_rms_norm<2, false>);
+    const int64_t most = kMostThreads / p.threads;                       // rows of a launch
+    for (int64_t row = 0; row < a.T; row += most) {
+        NormDesc b = a;
+        b.x += row * a.d;
+        if (a.residual) b.residual += row * a.d;
+        if (a.residual) b.total += row * a.d;
+        b.y += row * a.d;
+        if (a.rstd) b.rstd += row;
+        const dim3 grid((unsigned)std::min(most, a.T - row)), threads(p.threads);
+        const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, threads, 0, st, b); };
+        if (p.chunks == 1) go(past ? k_rms_norm<1, true> : k_rms_norm<1, false>);
+        else go(past ? k_rms_norm<2, true> : k_rms_norm<2, false>);
+    }
     return launch_status();
 }
 

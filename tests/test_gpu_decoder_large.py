@@ -48,3 +48,19 @@ def test_rope_cache_of_many_tokens():
         s = slots[at:at + n]
         assert torch.equal(kc[s // page, 0, :, s % page].reshape(n, 1, dim), part), at
         assert torch.equal(vc[s // page, 0, (s % page) // 8, :, s % 8].reshape(n, 1, dim), x[at:at + n]), at
+
+
+@pytest.mark.parametrize("d", [3, 8])
+def test_norm_of_many_rows(d):
+    """2^26 rows and some of 64 threads each; the gradients' grid does not grow with the rows."""
+    from paper_2407_17029_amd import binding as qb
+    T, part = (1 << 26) + 9, 1 << 23
+    x, r, w = _normal(4, T, d), _normal(5, T, d), _normal(6, d)
+    print(f"norm T={T} d={d}", flush=True)
+    y, total, rstd = qb.qblora_rms_norm_fwd(x, w, 1e-5, residual=r, keep=True)
+    for i in range(0, T, part):
+        a = qb.qblora_rms_norm_fwd(x[i:i + part], w, 1e-5, residual=r[i:i + part], keep=True)
+        assert all(torch.equal(b[i:i + part], c) for b, c in zip((y, total, rstd), a)), i
+    dx, _ = qb.qblora_rms_norm_bwd(total, w, rstd, y, need_dw=False)
+    for i in (0, T // 2, T - 1000):
+        assert torch.equal(dx[i:i + 1000], qb.qblora_rms_norm_bwd(total[i:i + 1000], w, rstd[i:i + 1000], y[i:i + 1000], need_dw=False)[0])
