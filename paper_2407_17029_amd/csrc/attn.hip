@@ -986,7 +986,7 @@ int launch(const AttnDesc& d, hipStream_t st) {
     const int64_t lot_units = many ? units_of_grid(lot_tiles, blocks_of_row, lot.target, lot.least) : 0;
     const int64_t few_units = units_of_grid(few_tiles, blocks_of_row, few.target, few.least);
     const int64_t lot_blocks = lot_units * d.kv_heads, blocks = lot_blocks + few_units * d.kv_heads;
-    if (blocks > INT32_MAX) return QBLORA_ERR_UNSUPPORTED;
+    if (blocks * kThreads > UINT32_MAX) return QBLORA_ERR_UNSUPPORTED;     // (a longer grid would be cut without an error)
     lot.grid_units = (int)lot_units;
     few.grid_units = (int)few_units;
     const auto go = [&](auto kernel, int64_t count) {
