@@ -434,7 +434,8 @@ typedef struct qblora_kv_cache {
  *   positions int32 [tokens]: position of each new token in its request; 0 behind the last.
  *   slots     int64 [tokens]: where its key and value go; -1 where there is no page, and behind the last token.
  * `context` and the free list are not changed: a step that is accepted adds fresh to context and drops the first `taken`
- * free pages.  page as for the cache; tokens <= 2^31 - 1.  n = 0 and tokens = 0 are fine.
+ * free pages.  page as for the cache; tokens and n * width <= 2^31 - 1, n <= 2^30.  n = 0 and
+ * tokens = 0 are fine.
  */
 int qblora_page_tables(const int32_t* context, const int32_t* fresh, int32_t n, int32_t page, const int32_t* free_pages,
                        int32_t n_free, int32_t* table, int32_t width, int64_t tokens, int32_t* starts, int32_t* positions,

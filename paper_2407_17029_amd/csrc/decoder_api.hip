@@ -17,6 +17,8 @@ bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(
 
 constexpr int64_t kMostPositions = (int64_t)1 << 30;       // positions of a request and tokens of a call: 32-bit arithmetic
 
+constexpr int32_t kMostRequests = 1 << 30;                 // of page tables: their groups are rounded up in 32 bits
+
 int check_cache(const qblora_kv_cache* c) {
     if (!c || !c->k || !c->v) return QBLORA_ERR_NULL;
     if (c->pages <= 0 || c->heads <= 0 || c->head_dim <= 0 || c->page <= 0) return QBLORA_ERR_SHAPE;
@@ -67,7 +69,7 @@ int qblora_page_tables(const int32_t* context, const int32_t* fresh, int32_t n, 
                        int64_t* slots, int32_t* taken, void* stream) {
     if (n < 0 || n_free < 0 || width < 0 || tokens < 0 || tokens > INT32_MAX || page <= 0) return QBLORA_ERR_SHAPE;
     if ((int64_t)n * width > INT32_MAX) return QBLORA_ERR_SHAPE;
-    if (page_shift_of(page) < 0) return QBLORA_ERR_UNSUPPORTED;
+    if (page_shift_of(page) < 0 || n > kMostRequests) return QBLORA_ERR_UNSUPPORTED;
     if (!starts || !taken || (n && (!context || !fresh)) || (n && width && !table) || (n_free && !free_pages) ||
         (tokens && (!positions || !slots)))
         return QBLORA_ERR_NULL;

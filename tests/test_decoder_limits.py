@@ -11,3 +11,9 @@ def test_attention_of_more_workgroups_than_a_grid_holds(qb):  # noqa: F811
     for n, max_new in ((1 << 18, 1), (1 << 17, 100), (1 << 20, 1)):
         rc = qb.lib().qblora_paged_attention(A, 64 * 64, 64, C.byref(c), A, 8, A, A, n, n, 0.1, 0, max_new, A, 64 * 64, None, A, BIG, None)
         assert rc == UNSUPPORTED, (n, max_new)
+
+
+def test_tables_of_more_requests_than_their_arithmetic_holds(qb):  # noqa: F811
+    """Requests are counted in groups, rounded up, in 32 bits."""
+    for n, width in (((1 << 30) + 1, 1), (2**31 - 1, 1), (2**31 - 1, 0)):
+        assert qb.lib().qblora_page_tables(A, A, n, 16, A, 4, A, width, 100, A, A, A, A, None) == UNSUPPORTED, (n, width)
