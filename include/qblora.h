@@ -506,8 +506,8 @@ int qblora_rope_frequencies(int32_t rot, double base, int32_t kind, double facto
  *   max_new  the most new tokens of any request, as far as the caller knows: it chooses the kernel, and a wrong value costs
  *        time, not correctness
  *   workspace  at least qblora_paged_attention_workspace_bytes(), 16-byte aligned: partial results of long contexts
- * heads % cache->heads == 0.  T = 0 and n = 0 are no-ops.  A batch that makes 2^24 workgroups, one for every 16 rows of a request
- * at least (2^17 requests of 64 key / value heads), is not supported.
+ * heads % cache->heads == 0.  T = 0 and n = 0 are no-ops.  n, T <= 2^30.  A batch that makes 2^24 workgroups, one for
+ * every 16 rows of a request at least (2^17 requests of 64 key / value heads), is not supported.
  */
 size_t qblora_paged_attention_workspace_bytes(const qblora_kv_cache* cache, int32_t heads, int32_t max_new);
 int qblora_paged_attention(const qblora_bf16* q, int64_t ldq, int32_t heads, const qblora_kv_cache* cache,

@@ -17,7 +17,7 @@ bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(
 
 constexpr int64_t kMostPositions = (int64_t)1 << 30;       // positions of a request and tokens of a call: 32-bit arithmetic
 
-constexpr int32_t kMostRequests = 1 << 30;                 // of page tables: their groups are rounded up in 32 bits
+constexpr int32_t kMostRequests = 1 << 30;                 // they are counted in steps of up to 2^19, in 32 bits
 
 int check_cache(const qblora_kv_cache* c) {
     if (!c || !c->k || !c->v) return QBLORA_ERR_NULL;
@@ -149,7 +149,7 @@ int qblora_paged_attention(const qblora_bf16* q, int64_t ldq, int32_t heads, con
     if (rc) return rc;
     if (n < 0 || T < 0 || width < 0 || window < 0 || max_new < 0 || heads <= 0 || heads % cache->heads != 0)
         return QBLORA_ERR_SHAPE;
-    if (T > kMostPositions || (int64_t)width * cache->page > kMostPositions || window > kMostPositions ||
+    if (n > kMostRequests || T > kMostPositions || (int64_t)width * cache->page > kMostPositions || window > kMostPositions ||
         T * (heads / cache->heads) > INT32_MAX || cache->heads > 65535 ||
         heads / cache->heads > 32768)
         return QBLORA_ERR_UNSUPPORTED;

@@ -17,3 +17,11 @@ def test_tables_of_more_requests_than_their_arithmetic_holds(qb):  # noqa: F811
     """Requests are counted in groups, rounded up, in 32 bits."""
     for n, width in (((1 << 30) + 1, 1), (2**31 - 1, 1), (2**31 - 1, 0)):
         assert qb.lib().qblora_page_tables(A, A, n, 16, A, 4, A, width, 100, A, A, A, A, None) == UNSUPPORTED, (n, width)
+
+
+def test_attention_of_more_requests_than_its_loops_count(qb):  # noqa: F811
+    """They are taken 256 at a time, which passes 2^31 behind the last."""
+    c = cache(qb)
+    for n in ((1 << 30) + 1, 2**31 - 1):
+        rc = qb.lib().qblora_paged_attention(A, 8 * 128, 8, C.byref(c), A, 0, A, A, n, 1, 0.1, 0, 1, A, 8 * 128, None, A, BIG, None)
+        assert rc == UNSUPPORTED, n
