@@ -107,14 +107,16 @@ __device__ __forceinline__ int64_t sum_of_wave(int64_t x) {
     return x;
 }
 
-__device__ __forceinline__ int blocks_of(const AttnDesc& d, const Span& s) {
-    return qblora::blocks_of(s.context, s.fresh, d.width << d.page_shift, d.window);
+// of a tile of `rows` rows of this request.  (Charged with what all of the request's tokens see, 1500 tokens of 12 / 4 heads over 2000
+// with a window of 64 are cut in three parts a tile, two of them empty: 22.6 us where this takes 16.0.)
+__device__ __forceinline__ int tile_blocks(const AttnDesc& d, const Span& s, int rows) {
+    return blocks_of_tile(s.context, s.fresh, d.width << d.page_shift, d.window, quotient(d, rows - 2 + d.group));
 }
 // `some`: the rows up to which requests go to attend_few in this call, where both forms are there
 __device__ __forceinline__ Cost cost_of(const AttnDesc& d, const Span& s, const Share& w, int some) {
     const int64_t rows = (int64_t)s.fresh * d.group;
     if (rows == 0 || (w.form == FEW && rows > some) || (w.form == LOT && rows <= some)) return {0, 0};
-    return {(int)((rows + w.rows - 1) / w.rows), blocks_of(d, s)};
+    return {(int)((rows + w.rows - 1) / w.rows), tile_blocks(d, s, w.rows)};
 }
 
 // The unit number `want` of the batch; false: there are not so many.  With `first`, the number of cut tiles is left where
@@ -134,7 +136,7 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
             const int64_t rows = (int64_t)s.fresh * d.group;
             const bool between = rows > kFewRows && rows <= kSomeRows;
             if (__any(between)) {
-                const int64_t blocks = between ? (rows + kFewRows - 1) / kFewRows * blocks_of(d, s) : 0;
+                const int64_t blocks = between ? (rows + kFewRows - 1) / kFewRows * tile_blocks(d, s, kFewRows) : 0;
                 if (sum_of_wave(blocks) * d.kv_heads <= kSomeBlocks) some = kSomeRows;
             }
         }

@@ -22,6 +22,12 @@ constexpr int blocks_of(int context, int fresh, int limit, int window) {
     return hi > lo ? (hi + kAttnBlock - 1) / kAttnBlock - lo / kAttnBlock : 1;
 }
 
+// The same for one tile, whose rows are of at most `behind` tokens behind its first: with a window it sees fewer.
+constexpr int blocks_of_tile(int context, int fresh, int limit, int window, int behind) {
+    const int blocks = blocks_of(context, fresh, limit, window);
+    return window ? smaller(blocks, (window + behind + 2 * kAttnBlock - 2) / kAttnBlock) : blocks;
+}
+
 struct Cost { int tiles, blocks; };            // of a request: its tiles, and the blocks of each
 
 // Blocks of a unit, from the blocks of all tiles.  A tile is at most 2^25 + 1 blocks: a unit of kLongUnit is never cut, and no larger

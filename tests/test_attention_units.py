@@ -19,6 +19,7 @@ void units(int tiles, int blocks, int64_t per, int slack, int* out) {
 }
 int64_t grid(int64_t tiles, int64_t blocks_of_row, int target, int least) { return units_of_grid(tiles, blocks_of_row, target, least); }
 int blocks(int context, int fresh, int limit, int window) { return blocks_of(context_of(context), fresh, limit, window); }
+int tile_blocks(int context, int fresh, int limit, int window, int behind) { return blocks_of_tile(context, fresh, limit, window, behind); }
 int within(int count, int grid_units) { return units_within(count, grid_units); }
 int add(int a, int b) { return add_units(a, b); }
 int joined(int cuts, int total, int grid_units) { return cut_tiles(cuts, total, grid_units); }
@@ -152,3 +153,26 @@ def test_blocks_of_the_longest_requests(rules):
                     hi, lo = min(c + fresh, limit), max(c + 1 - window, 0) if window else 0
                     want = -(-hi // 32) - lo // 32 if hi > lo else 1
                     assert rules.blocks(context, fresh, limit, window) == want, (context, fresh, limit, window)
+
+
+@pytest.mark.parametrize("rows", [16, 128])
+def test_blocks_of_a_tile_are_those_that_it_sees(rules, rows):
+    """With a window, a tile of a long request is charged with its own positions: as many blocks as it touches at most, and no more
+    than two above what the longest of the request's tiles touches.  It was the whole request's 50 blocks for each tile of
+    1500 tokens over 2000 with a window of 64."""
+    r = random.Random(3)
+    cases = [(2000, 1500, 1 << 20, 64, 3)] + [(r.randint(0, 5000), r.randint(1, 3000), 16 * r.randint(1, 600), r.choice([0, 1, 64, r.randint(1, 6000)]),
+                                               r.choice([1, 3, 8, 40, 200])) for _ in range(300)]
+    for context, fresh, limit, window, group in cases:
+        most = 1
+        for row0 in range(0, fresh * group, rows):
+            first, last = row0 // group, (min(row0 + rows, fresh * group) - 1) // group
+            lo, hi = max(context + first + 1 - window, 0) if window else 0, min(context + last + 1, limit)
+            if hi > lo:
+                most = max(most, -(-hi // 32) - lo // 32)
+        got = rules.tile_blocks(context, fresh, limit, window, (rows - 2 + group) // group)
+        assert got >= most, (context, fresh, limit, window, group)
+        if window and fresh * group > rows and limit >= context + fresh:
+            assert got <= most + 2, (context, fresh, limit, window, group, got, most)
+        if not window:
+            assert got == rules.blocks(context, fresh, limit, 0)
