@@ -498,7 +498,8 @@ int qblora_rope_frequencies(int32_t rot, double base, int32_t kind, double facto
  *   0 <= j <= p, j > p - window (window = 0: no limit), and j in a page that the table lists (entries outside 0 .. pages-1
  *   and columns past `width` list none).
  * A token that sees nothing gets zeros (and lse = -inf).  What unseen positions hold does not matter, NaN and infinities
- * included.  Sums and statistics in fp32; the weights e_j are rounded to bf16 for the second product (the sum in the
+ * included.  Sums and statistics in fp32; for the second product the weights e_j have 16 significant bits where a request has at most
+ * 16 rows (new tokens times heads / cache->heads; 64 in small batches), and are rounded to bf16 where it has more (the sum in the
  * denominator is of the unrounded ones).
  *   q    bf16: token t, head h at q + t*ldq + h*head_dim; 16-byte aligned, ldq % 8 == 0
  *   out  bf16, likewise; rows of tokens that belong to no request are not written

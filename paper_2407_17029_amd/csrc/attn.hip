@@ -3,9 +3,11 @@
 //   out = sum_j e_j v_j / sum_j e_j,  e_j = exp(scale q.k_j - m),  over the positions j a row sees, in one pass: m is the
 //   maximum so far, and what was summed under a smaller one is multiplied by 2^(old - new) (the exponents are in base 2).
 //
-// Scores, maxima, sums and parts are fp32.  The weights e_j are rounded to bf16, as the matrix instruction takes the second
-// product's operands: 2^-9 of each, which many positions average out (0.002 of the result's size where an output's own rounding is
-// 0.0017); the sum below the line is of the unrounded ones.
+// Scores, maxima, sums and parts are fp32.  The matrix instruction takes the second product's operands in bf16.  attend_few, whose
+// matrix pipe is idle most of the time, multiplies a weight e_j in two parts, rounded and what that leaves: 2^-16 of it is lost
+// (64 tokens of 40 heads over 100 to 8000: 367 us with one part, 368 with two; one of 4095 16.6 and 16.8).  attend_many, which that pipe
+// bounds, rounds it once: up to 2^-8 of each, which many positions average out (0.0024 of the result's size in all, where an output's
+// own rounding is 0.0017).  The sum below the line is of the unrounded ones.
 //
 // A row is a query head of a new token; the rows of one request that share a key / value head go together, token by token
 // (row r: token r / group, head r % group of the group), so that the cache is read once for all of them.
@@ -382,12 +384,13 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
         const float a = exp2_of(m - m_use);
         m = m_new;
         l *= a;
-        uint32_t pw[4];
+        uint32_t pw[4], rest[4];                                       // the weights, and what their rounding leaves
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
             const float p0 = exp2_of(x[j] - m_use), p1 = exp2_of(x[j + 1] - m_use);
             l += p0 + p1;
             pw[j / 2] = pack_bf16(p0, p1);
+            rest[j / 2] = pack_bf16(p0 - bf16_lo(pw[j / 2]), p1 - bf16_hi(pw[j / 2]));
         }
         // lanes 16 g have the weights of positions 4 g .. and 16 + 4 g ..; their values are those of 8 g ..
         const auto to_octets = [](uint32_t& p, uint32_t& q) {
@@ -398,7 +401,10 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
         };
         to_octets(pw[0], pw[2]);
         to_octets(pw[1], pw[3]);
+        to_octets(rest[0], rest[2]);
+        to_octets(rest[1], rest[3]);
         const bf16x8 pf = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+        const bf16x8 rf = __builtin_bit_cast(bf16x8, make_uint4(rest[0], rest[1], rest[2], rest[3]));
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
@@ -430,6 +436,8 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
                 }
             }
         }
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[i]), rf, o[i], 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < DT; ++i) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[i]), pf, o[i], 0, 0, 0);
         if (step + 1 < steps) load_values(step + 1, id0, id1);
