@@ -4,8 +4,8 @@
 //   maximum so far, and what was summed under a smaller one is multiplied by 2^(old - new) (the exponents are in base 2).
 //
 // Scores, maxima, sums and parts are fp32.  The matrix instruction takes the second product's operands in bf16.  attend_few, whose
-// matrix pipe is idle most of the time, multiplies a weight e_j in two parts, rounded and what that leaves: 2^-16 of it is lost
-// (64 tokens of 40 heads over 100 to 8000: 367 us with one part, 368 with two; one of 4095 16.6 and 16.8).  attend_many, which that pipe
+// matrix pipe is idle most of the time, multiplies a weight e_j in two parts, cut to bf16 and what that leaves: 2^-16 of it is lost
+// (64 tokens of 40 heads over 100 to 8000: 367 us with one part, 369 with two; one of 4095 16.8 and 17.0).  attend_many, which that pipe
 // bounds, rounds it once: up to 2^-8 of each, which many positions average out (0.0024 of the result's size in all, where an output's
 // own rounding is 0.0017).  The sum below the line is of the unrounded ones.
 //
@@ -384,13 +384,16 @@ __device__ __forceinline__ void attend_few(const AttnDesc& d, const Share& share
         const float a = exp2_of(m - m_use);
         m = m_new;
         l *= a;
-        uint32_t pw[4], rest[4];                                       // the weights, and what their rounding leaves
+        // The weights cut to bf16, and what that leaves: of the same sign, and not 0 either where the weight is not, so that both products
+        // of an infinite value are that infinity.
+        uint32_t pw[4], rest[4];
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
             const float p0 = exp2_of(x[j] - m_use), p1 = exp2_of(x[j + 1] - m_use);
             l += p0 + p1;
-            pw[j / 2] = pack_bf16(p0, p1);
-            rest[j / 2] = pack_bf16(p0 - bf16_lo(pw[j / 2]), p1 - bf16_hi(pw[j / 2]));
+            const uint32_t w0 = __float_as_uint(p0) & 0xffff0000u, w1 = __float_as_uint(p1) & 0xffff0000u;
+            pw[j / 2] = w0 >> 16 | w1;
+            rest[j / 2] = pack_bf16(fmaxf(p0 - __uint_as_float(w0), p0 * 0x1p-24f), fmaxf(p1 - __uint_as_float(w1), p1 * 0x1p-24f));
         }
         // lanes 16 g have the weights of positions 4 g .. and 16 + 4 g ..; their values are those of 8 g ..
         const auto to_octets = [](uint32_t& p, uint32_t& q) {

@@ -28,3 +28,22 @@ def test_long_contexts_in_parts():
     out, _ = _run(b, 128 ** -0.5, max_new=1)
     want, _, mag = b.expected(128 ** -0.5)
     du.assert_bf16(out, want, WEIGHTS * mag, "out")
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(4, 4, 128), (8, 1, 64), (4, 2, 256)])
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+def test_values_that_are_not_finite_where_all_rows_see_them(heads, kv_heads, dim, bad):
+    """In the middle of a context, where no mask is: infinities and NaN pass through their feature as the formula has it, with weights
+    of every size, those that bf16 holds exactly (the largest is 1) among them."""
+    import decoder_util as du
+    b = _batch(33 + dim, [300, 90, 200], [1, 1, 2], 16, heads, kv_heads, dim)
+    for i in range(3):
+        for at, feature in ((5, 3), (40, 17), (70, 33)):
+            b.v[b.table[i, at // 16], at % 16, 0, feature] = bad
+        top = b.k[b.table[i, 2], 8, 0]                              # position 40 of every context has the largest weight
+        top[:] = 4.0 * np.sign(b.q[b.starts[i], 0])
+        b.q[b.starts[i]:b.starts[i + 1], :heads // kv_heads] = b.q[b.starts[i], 0]
+    out, _ = _run(b, dim ** -0.5, max_new=2)
+    want, _, mag = b.expected(dim ** -0.5)
+    assert not np.isfinite(want[:, 0, [3, 17, 33]]).any()
+    du.assert_bf16(out, want, np.nan_to_num(WEIGHTS * mag, posinf=0.0), "out")
