@@ -450,7 +450,7 @@ int qblora_page_tables(const int32_t* context, const int32_t* fresh, int32_t n, 
  *            outputs may be the inputs themselves (same strides), but must not overlap them otherwise.
  * The angle is formed in 64 bits and reduced to one turn before sine and cosine: at position 10^6 an fp32 angle is off by
  * 0.03 of a radian.  _bwd is the transposed operator, a turn the other way round: gradients in, gradients out.
- * T = 0 is a no-op.
+ * head_dim <= 1024, (heads + kv_heads) * head_dim < 2^28, T <= 2^30; T = 0 is a no-op.
  */
 typedef struct qblora_rope {
     int32_t rot;

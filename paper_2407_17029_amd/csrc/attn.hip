@@ -16,18 +16,18 @@
 // positions at a time straight from the pages into registers, in the operand order that the cache is stored in, with the
 // next 32 in flight behind them.  Scores are formed transposed, S^T = K Q^T, so that a lane holds eight positions of one row,
 // the operand of O^T = V^T P^T but for four exchanges between lanes.  The four waves of a workgroup take turns on the positions
-// and are joined in LDS.  64 single tokens of 40 heads over 100 to 8000 positions (2.3 GB): 368 us, 6.2 TB/s of what a kernel
+// and are joined in LDS.  64 single tokens of 40 heads over 100 to 8000 positions (2.3 GB): 369 us, 6.2 TB/s of what a kernel
 // that only reads gets 6.3 of; four of 64 heads, 8 of them with keys, over 30000 to 131000 (0.8 GB): 131 us, 6.2 TB/s; one of
-// 4095 (67 MB): 12.3 us and 4 of the join.
+// 4095 (67 MB): 12.4 to 14.6 us and 4 of the join.
 //
 // attend_many takes 128 rows, 32 a wave, and is bound by the matrix pipe and by the exponentials beside it.  64 positions at a
 // time go through LDS, in the order of the pages (copies of 1 KB that need no registers, two tiles in turn, one barrier a
 // tile); scores are transposed here too, so that a row's maximum and sum are a lane's own but for one exchange of halves.
-// 4096 tokens over 12288, 32 heads (962 GFLOP): 853 us, 1130 TFLOP/s, 0.84 of what the library's large product reaches on the
+// 4096 tokens over 12288, 32 heads (962 GFLOP): 865 us, 1110 TFLOP/s, 0.83 of what the library's large product reaches on the
 // chip; two workgroups a CU, the matrix pipe busy for 0.59 of the cycles and the vector ALU for 0.48, at a power-limited 1.7
 // GHz.  In small calls a tile takes 1.1 us of a workgroup alone on its CU and 1.9 of each of two, its start 3 to 5 us, the
-// store of a part up to 1.7.  Heads of 64 are bound by the exponentials (4096 tokens over 4000, 32 heads, 203 GFLOP: 241 us, 845
-// TFLOP/s), heads of 256 by one wave a SIMD (2000 over 2000, 16 heads, 98 GFLOP: 179 us, 550 TFLOP/s).
+// store of a part up to 1.7.  Heads of 64 are bound by the exponentials (4096 tokens over 4000, 32 heads, 203 GFLOP: 243 us, 840
+// TFLOP/s), heads of 256 by one wave a SIMD (2000 over 2000, 16 heads, 98 GFLOP: 175 us, 560 TFLOP/s).
 //
 // Work: requests differ by orders of magnitude, and only the device knows their lengths.  Every workgroup adds up the work
 // of all requests, which gives the number of positions that a workgroup takes if there are to be `target` of them, and finds
@@ -59,19 +59,19 @@ constexpr float kSlack = 8.0f;
 struct CutTile { int token0, rem0, rows, splits, slot, pad[3]; };
 enum { FEW = 1, LOT = 2, ALL = 3 };            // the requests of few rows, those of more, or all
 struct Share { int rows, target, least, slack, form, grid_units; int* cuts; CutTile* cut; float* part; };   // grid_units: a key / value head
-// Few rows: with 512 units 4 contexts of 30000 to 131000 take 148 us, with 1024 131, with 2048 138; single tokens of 16 x 1000 to
-// 8000 positions 55.6, 50.7 and 55.6.  With 4 blocks at least, one of 4095 takes 20.3, with 8 17.1, with 16 17.2.
-// Heads of 256 leave one workgroup a CU: 4 of 16 / 4 heads over 10000 to 60000 119 us with 1024, 111 with 512, 144 with 256 (64 of
-// 16 over 500 to 3000 241, 247 and 247).
+// Few rows: with 512 units 4 contexts of 30000 to 131000 take 151 us, with 1024 131, with 2048 139; single tokens of 16 x 1000 to
+// 8000 positions 55.9, 51.3 and 54.9.  With 4 blocks at least, one of 4095 takes 20.5, with 8 17.4, with 16 17.4.
+// Heads of 256 leave one workgroup a CU: 4 of 16 / 4 heads over 10000 to 60000 120 us with 1024, 112 with 512, 145 with 256 (64 of
+// 16 over 500 to 3000 242, 248 and 248).
 constexpr int kFewTarget = 1024, kFewWideTarget = 512, kFewLeast = 8;
-// More rows: every part costs 66 KB of writes and as many of reads, so there are fewer units than places.  175 tokens over 3985 take
-// 41 us with 384, 60 with 512, 46 with 256; 128 over 2000 22.5 with 16 blocks at least, 30 with 12, 24.5 with 24.  Without the
-// slack, 175 over 3985 took 54 us, with it 46; 1000 without a context 43.6 and 35.5.
+// More rows: every part costs 66 KB of writes and as many of reads, so there are fewer units than places.  175 tokens of 64 / 8
+// heads over 3985 take 42 us with 384, 60 with 512, 47 with 256; 128 of 32 heads over 2000 22.6 with 16 blocks at least, 30.0 with 12,
+// 24.3 with 24.  Without the slack, 175 over 3985 take 50 us, 128 over 2000 30.7, and 1000 of 40 heads without a context 39.1 instead of 29.8.
 // Heads of 256: 512 tokens of 16 heads over 2000 79 us with 384, which is one round and a half, and 51 with 256.
 constexpr int kManyTarget = 384, kManyWideTarget = 256, kManyLeast = 16;
 // Requests of up to kSomeRows rows go to attend_few, 16 rows at a time, if they do not make more than kSomeBlocks blocks in all:
-// what the chip takes at once in units of kFewLeast.  Four tokens of 8 heads a key head over 4000: 14.1 us that way, 20.8 in one
-// tile of 128 rows; 16 of those requests, above the limit, 48.9 and 43.7.
+// what the chip takes at once in units of kFewLeast.  Four tokens of 8 heads a key head over 4000: 14.0 us that way, 17.7 in one
+// tile of 128 rows; 16 of those requests over 1000 to 4000, above the limit, 49.7 and 37.3.
 constexpr int kSomeRows = 64, kSomeBlocks = 512 * kFewLeast;
 static_assert(2 * kFewTarget < 1 << 15 && 2 * kManyTarget < 1 << 15, "parts and cut tiles are counted in halves of a word");
 
@@ -259,7 +259,8 @@ __device__ __forceinline__ const qblora_bf16* value_row(const AttnDesc& d, const
     return d.vc + (((int64_t)id * d.kv_heads + kvh) * D << d.page_shift) + (in_page >> 3) * D * 8 + (in_page & 7);
 }
 
-// A part of the cache that this call reads once: no line is kept for it.  64 tokens of 40 heads over 100 to 8000: 411 us without,
+// A part of the cache, of which no line is kept: the call reads it once, or, with more than 16 rows to a key head, once for every 16 of
+// them, by workgroups that run side by side.  64 tokens of 40 heads over 100 to 8000: 411 us without,
 // 376 with values that way, 368 with both.
 __device__ __forceinline__ uint4 stream(const qblora_bf16* p) {
     return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p)));

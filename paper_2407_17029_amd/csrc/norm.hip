@@ -283,7 +283,9 @@ int launch_rms_norm(const NormDesc& a, hipStream_t st) {
 }
 
 int64_t rms_norm_bwd_parts(int64_t T, int d) {
-    const int64_t full = 256 * 1024 / plan_of(d).threads;                // what the chip holds at once
+    // 1024 threads of rows a CU.  With 4096 or 8192 features every CU has as many workgroups (4001 rows both ways 52 and 103 us); where
+    // the threads of a row do not divide 1024, some CUs have one more than others: 5120 features 82 us, 6144 100, 7168 119.
+    const int64_t full = 256 * 1024 / plan_of(d).threads;
     const int64_t some = (T + 3) / 4;                                    // four rows at least: 8001 x 600 25 us, with one 28.7
     return some < full ? some : full;
 }

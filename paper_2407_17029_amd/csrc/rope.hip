@@ -8,7 +8,8 @@
 // access.  Tokens of a prompt that go to the cache come eight to a workgroup, neighbouring lanes one behind the other, so that
 // eight keys' 16-byte octets are one 128-byte line of their page and eight values of a feature one 16-byte store; single
 // tokens come one to a workgroup, which is four times as many of them.  k_rope_any: parts of a head that are no multiple of
-// 16 features.  6693 tokens of 64 + 64 heads of 128 to the cache (658 MB): 130 us, 5.1 TB/s, where a large copy reaches 4.9; 1337 of 40 + 40 heads there and back (110 MB): 21.1 us, 5.2 TB/s; 64 single tokens of 32 + 32: 7 us, of which 3.5 are
+// 16 features, a turn for every pair of every head (4096 tokens of 32 + 32 heads of 80, there and back: 105 us with 20 features
+// turned, 33 by k_rope with all 80).  6693 tokens of 64 + 64 heads of 128 to the cache (658 MB): 130 us, 5.1 TB/s, where a large copy reaches 4.9; 1337 of 40 + 40 heads there and back (110 MB): 21.1 us, 5.2 TB/s; 64 single tokens of 32 + 32: 7 us, of which 3.5 are
 // an empty launch.
 #include <algorithm>
 
