@@ -162,8 +162,7 @@ __device__ __forceinline__ bool find_unit(const AttnDesc& d, const Share& share,
     }
     int64_t all = 0;
     for (int i = tid; i < d.n; i += kThreads) {
-        const Cost c = cost_of(d, span_of(d, i), share, kFewRows);
-        all += (int64_t)c.tiles * c.blocks;
+        all = add_blocks(all, cost_of(d, span_of(d, i), share, kFewRows));
     }
     all = sum_of_wave(all);
     if (lane == 0) f.sums[wave] = all;

@@ -38,6 +38,12 @@ constexpr int blocks_per_unit(int64_t all, int target, int least) {
     return per >= kLongUnit ? kLongUnit : larger_of((int)per, least);
 }
 
+// The blocks of one request more, from 2^50 on as good as any larger number
+constexpr int64_t add_blocks(int64_t all, const Cost& c) {
+    const int64_t sum = all + (int64_t)c.tiles * c.blocks;
+    return sum < (int64_t)1 << 50 ? sum : (int64_t)1 << 50;
+}
+
 struct Units { int tiles, splits, count, cuts; };                      // cuts: parts, and cut tiles in the upper half
 constexpr Units units_of(const Cost& c, int per, int slack) {
     const int splits = larger_of(1, (int)(((uint32_t)c.blocks + (uint32_t)(slack ? per / 2 : per - 1)) / (uint32_t)per));

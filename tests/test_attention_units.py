@@ -12,6 +12,7 @@ SHIM = """
 #include "attn_units.h"
 using namespace qblora;
 extern "C" {
+int64_t sum_blocks(int64_t all, int tiles, int blocks) { return add_blocks(all, Cost{tiles, blocks}); }
 int64_t per_unit(int64_t all, int target, int least) { return blocks_per_unit(all, target, least); }
 void units(int tiles, int blocks, int64_t per, int slack, int* out) {
     const Units u = units_of(Cost{tiles, blocks}, per, slack);
@@ -176,3 +177,15 @@ def test_blocks_of_a_tile_are_those_that_it_sees(rules, rows):
             assert got <= most + 2, (context, fresh, limit, window, group, got, most)
         if not window:
             assert got == rules.blocks(context, fresh, limit, 0)
+
+
+def test_blocks_of_any_number_of_requests(rules):
+    """2^30 requests that all count the most tokens over the longest rows pass 64 bits; a thread adds up 2^22 of them, 256 threads are summed."""
+    rules.sum_blocks.argtypes, rules.sum_blocks.restype = [C.c_int64, C.c_int, C.c_int], C.c_int64
+    all_ = 0
+    for _ in range(5000):
+        all_ = rules.sum_blocks(all_, 1 << 27, (1 << 25) + 1)
+        assert 0 < all_ * 256 < 1 << 63
+    for form in FORMS:
+        assert rules.per_unit(all_, form[1], form[2]) == rules.per_unit(1 << 60, form[1], form[2])
+    assert rules.sum_blocks(rules.sum_blocks(0, 3, 50), 7, 11) == 3 * 50 + 7 * 11
