@@ -542,6 +542,184 @@ int qblora_rms_norm_bwd(const qblora_bf16* total, const qblora_bf16* w, const fl
                         const qblora_bf16* dtotal, int64_t T, int32_t d, qblora_bf16* dx, float* dw, void* workspace,
                         size_t workspace_bytes, void* stream);
 
+/* ---- many adapters on one frozen projection ------------------------------------------------------------------------------
+ *
+ * A batch whose requests have adapters of their own, beside one shared 4-bit weight: the base product of all tokens is one
+ * call (qblora_linear_decode, or qblora_linear_fwd without adapter), the calls below add each request's own adapter term,
+ * forward and backward.  The conventions of the top hold.  Whatever the device-side integers hold, no call reads or writes
+ * outside the buffers described by its arguments.
+ */
+
+/*
+ * Adapters of one projection, by number.  The struct lives in host memory.
+ *   count             adapters, at most 8192
+ *   d_in, d_out, lambda1, lambda2   common to all, d_in % 64 == 0, d_out % 64 == 0, lambdas 1, 2, 4 or 8; the scale operators are
+ *                     the method's (QBLORA_OP_AVGPOOL_REPEAT)
+ *   R                 no adapter's inner rank is higher; R % 8 == 0, R <= 512
+ *   table             device, 16-byte aligned, qblora_adapter_table_bytes(count): the caller's, written by qblora_adapter_table
+ */
+typedef struct qblora_adapters {
+    int32_t count;
+    int32_t d_in;
+    int32_t d_out;
+    int32_t lambda1;
+    int32_t lambda2;
+    int32_t R;
+    void* table;
+} qblora_adapters;
+size_t qblora_adapter_table_bytes(int32_t count);
+
+/*
+ * Writes entries first .. first + n - 1 of the table from `list` (host array).  An entry keeps the addresses of its A and B
+ * (16-byte aligned, as they are for qblora_linear_fwd otherwise), which stay the caller's: what they hold when a later call
+ * runs is what that call uses, so that an optimizer may step them in place.  An entry without adapter (A or B NULL, or R = 0) adds
+ * nothing.
+ *   dA, dB   host arrays of n pointers (both or neither NULL): where qblora_adapters_bwd writes that entry's gradients, fp32
+ *            [d_in/lambda1, R] and [R, d_out/lambda2], 16-byte aligned; a NULL pointer, or no array: it writes none.  No two
+ *            entries may share them.
+ */
+int qblora_adapter_table(const qblora_adapters* adapters, int32_t first, int32_t n, const qblora_adapter* list,
+                         float* const* dA, float* const* dB, void* stream);
+
+/*
+ * The tokens of a batch by adapter.  Request i has the tokens starts[i] .. starts[i+1] - 1 (int32 [n + 1], ascending, as
+ * qblora_page_tables writes them) and adapter which[i] (int32 [n]; outside 0 .. count-1: none).
+ *   first   int32 [count + 1]: first[a] is where adapter a's tokens begin in `order`; first[count] tokens in all
+ *   order   int32 [T]: the tokens of adapter 0 in ascending order of their requests, those of adapter 1, ...; -1 behind the last
+ *   tiles   int32 [qblora_adapter_tiles(count, T)][4], 16-byte aligned: the tokens of every adapter that has some in runs of 64
+ *           (the last of an adapter shorter), in ascending order: {adapter, where the run begins in `order`, its tokens, 0};
+ *           0 behind the last
+ * All are written whole.  Tokens of no request, or with a number of T and above, belong to none.  Once for a batch: all projections
+ * of a model read the same.  n <= 8192, count <= 8192, T <= 2^20.
+ */
+int32_t qblora_adapter_tiles(int32_t count, int64_t T);
+int qblora_adapter_groups(const int32_t* starts, const int32_t* which, int32_t n, int32_t count, int64_t T, int32_t* first,
+                          int32_t* order, int32_t* tiles, void* stream);
+
+/*
+ * Adds the adapter terms.  For token t with adapter a, and C and E the method's scale operators:
+ *   Y[t] = bf16( Y[t] + E( V ) ),  V = (s_a U) B_a,  U = C(X[t]) A_a;
+ * sums in fp32, s_a U with 16 significant bits at least.  Rows of tokens without adapter stay as they are.
+ *   X      bf16: token t at X + t*ldx; 16-byte aligned, ldx % 8 == 0, ldx >= d_in
+ *   Y      bf16, likewise (ldy, d_out)
+ *   first, order, tiles   as qblora_adapter_groups wrote them for this batch and this count.  A token must not be listed twice.
+ *   saved  qblora_adapters_saved_bytes(), 16-byte aligned, or NULL: s U of every listed token, which the backward pass needs
+ *   workspace   at least qblora_adapters_workspace_bytes(), 256-byte aligned; the size serves both directions
+ * T = 0 is a no-op; T <= 2^20.
+ */
+size_t qblora_adapters_saved_bytes(const qblora_adapters* adapters, int64_t T);
+size_t qblora_adapters_workspace_bytes(const qblora_adapters* adapters, int64_t T);
+int qblora_adapters_fwd(const qblora_adapters* adapters, const int32_t* first, const int32_t* order, const int32_t* tiles,
+                        const qblora_bf16* X, int64_t ldx, int64_t T, qblora_bf16* Y, int64_t ldy, qblora_bf16* saved,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its backward pass: with dV[t] = s_a * (sums of lambda2 adjacent features of dY[t]) and dU = dV B_a^T,
+ *   dX[t] = bf16( dX[t] + (1/lambda1) * E1( dU A_a^T ) ), E1 repeating each value lambda1 times,
+ *   dA_a = sum over a's tokens of C(X[t])^T dU,   dB_a = sum over a's tokens of U^T dV.
+ *   dX      bf16, likewise (lddx, d_in): what the frozen weight's backward call wrote; NULL: not wanted
+ *   gradients   0: none (X and saved are ignored).  Else dA and dB of the table's entries that have a place for them are
+ *           overwritten, with zeros where the batch has no token of an adapter; sums in a fixed order, a repeated call repeats
+ *           its bits
+ *   saved   what qblora_adapters_fwd wrote for the same X, adapters and groups; NULL: s U is computed again from X
+ * T = 0: gradients are zero, nothing else happens.
+ */
+int qblora_adapters_bwd(const qblora_adapters* adapters, const int32_t* first, const int32_t* order, const int32_t* tiles,
+                        const qblora_bf16* X, int64_t ldx, const qblora_bf16* dY, int64_t lddy, int64_t T,
+                        const qblora_bf16* saved, qblora_bf16* dX, int64_t lddx, int32_t gradients, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* ---- the optimizer's step ------------------------------------------------------------------------------------------------ */
+
+/*
+ * One tensor that an AdamW step updates (host struct, device pointers at any multiple of their element size).
+ *   n         elements; 0 is fine
+ *   param     bf16 [n], what the layer calls read; may be NULL if there is a master
+ *   master    fp32 [n] or NULL: the weight that is stepped, param being its rounding.  Without it param itself is stepped and
+ *             rounded to one of its two neighbours by chance (see `seed`), so that steps far below its precision count in the mean
+ *   grad      fp32 [n]
+ *   m, v      the moments: fp32 [n] each (32 bits), or OCP E4M3 and E5M2 values [n] (8 bits) in units of m_scale and v_scale,
+ *             fp32 [ceil(n / 256)], powers of two, one for each 256 elements (NULL with 32 bits).  All zero before the first step
+ *             (as scales any finite numbers).
+ *   rate      factor of this tensor on the learning rate
+ *   decay     its weight decay
+ * No two tensors of a list may overlap.
+ */
+typedef struct qblora_adamw_tensor {
+    int64_t n;
+    qblora_bf16* param;
+    float* master;
+    const float* grad;
+    void* m;
+    void* v;
+    float* m_scale;
+    float* v_scale;
+    float rate;
+    float decay;
+} qblora_adamw_tensor;
+
+/*
+ * The tensors of a step as one list on the device: `plan` (caller's, 16-byte aligned, qblora_adamw_plan_bytes()) receives
+ * their description, and *list what the calls below take.  The addresses are kept until the plan is made anew; `bits` is 8 or 32.
+ * In all fewer than 2^30 blocks of 256 elements.
+ */
+typedef struct qblora_adamw_list {
+    int32_t count;
+    int32_t bits;
+    int64_t units;        /* pieces of at most 4096 elements of one tensor */
+    const void* plan;
+} qblora_adamw_list;
+size_t qblora_adamw_plan_bytes(const qblora_adamw_tensor* tensors, int32_t count);
+int qblora_adamw_plan(const qblora_adamw_tensor* tensors, int32_t count, int32_t bits, void* plan, size_t plan_bytes,
+                      qblora_adamw_list* list, void* stream);
+
+/*
+ * Norm of all gradients of a list and the factor that clips it:
+ *   out[0] = N = sqrt( sum g^2 ),  out[1] = min( 1, max_norm / (N + 1e-6) )   (NaN where N is not finite)
+ * computed in 64 bits in a fixed order (a repeated call repeats its bits) and rounded once.  out: fp32 [2], device.  max_norm > 0.
+ * workspace: at least qblora_grad_norm_workspace_bytes(), 16-byte aligned.
+ */
+size_t qblora_grad_norm_workspace_bytes(const qblora_adamw_list* list);
+int qblora_grad_norm(const qblora_adamw_list* list, double max_norm, float* out, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
+/*
+ * One step of AdamW on every tensor of a list.  With t the number of the step (1 is the first), f the factor on the gradients,
+ * and for each element
+ *   g = f * grad;  m = beta1 * m + (1 - beta1) * g;  v = beta2 * v + (1 - beta2) * g^2, both cut to 2^127 (a largest number of 8 bits
+ *   rounded up stays finite)
+ *   w = w * (1 - lr * rate * decay) - lr * rate / (1 - beta1^t) * m / ( sqrt(v) / sqrt(1 - beta2^t) + eps )
+ * in fp32, each operation of m and v rounded by itself in the order written, factors formed in 64 bits and rounded once.  w is
+ * the master copy, or param where there is none.  An element whose gradient is not finite keeps its weight and moments.
+ *
+ * Moments in 8 bits.  The step uses the moments before they are rounded.  A block's scale is the smallest power of two, 2^-126 at
+ * least, that brings its largest value within 448 (m) or 57344 (v).  In units of it a value is rounded to one of its two neighbours
+ * by chance, the nearer the likelier: rounded to the nearest, v with beta2 = 0.999 would not move at all where g^2 is within a
+ * few hundred times of it, as a step changes it by less than half of the 8 bits' spacing.  v is never rounded to zero.
+ * The random bits of element e of tensor number i (from 0 in the list) are, in 32-bit arithmetic,
+ *   x = e * 0x9E3779B1 + i * 0x632BE5AB + seed * 0x85157AF5 + t * 0xD168AAAD
+ *   x = (x ^ x >> 16) * 0x6C8E9CF5;  x = (x ^ x >> 15) * 0xB5297A4D;  x = x ^ x >> 16
+ * the low half for m, the high half for v, the high half of x * 0x9E3779B1 for a bf16 weight without master.
+ *
+ *   step    t >= 1.  device_step (may be NULL): int64 on the device, read in place of step when the call runs, so that a captured
+ *           graph may be replayed (a number below 1 there counts as 1); t counts with its low 32 bits in the random bits
+ *   lr      device_lr (may be NULL): fp32 on the device, likewise
+ *   clip    device, the two numbers of qblora_grad_norm, of which the second is f, or NULL: f = 1.  Where f is not finite
+ *           nothing is changed: a step with a broken gradient is left out.
+ * 0 <= beta < 1, eps > 0, lr finite.
+ */
+typedef struct qblora_adamw {
+    double lr;
+    double beta1;
+    double beta2;
+    double eps;
+    int64_t step;
+    const int64_t* device_step;
+    const float* device_lr;
+    uint32_t seed;
+} qblora_adamw;
+int qblora_adamw_step(const qblora_adamw_list* list, const qblora_adamw* how, const float* clip, void* stream);
+
 /*
  * Measurement hook.  Registers a pair of caller-created hipEvent_t (passed as void*) that the next
  * calls record on their stream immediately before and after ONE part of the work, so that a

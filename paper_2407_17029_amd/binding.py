@@ -37,7 +37,11 @@ EXPORTS = ["qblora_quantize_blockwise", "qblora_dequantize_bf16", "qblora_linear
            "qblora_noalloc_scratch_bytes", "qblora_linear_fwd_noalloc", "qblora_dense_min_tokens",
            "qblora_page_tables", "qblora_rope_fwd", "qblora_rope_bwd", "qblora_rope_cache", "qblora_rope_frequencies",
            "qblora_paged_attention_workspace_bytes", "qblora_paged_attention", "qblora_rms_norm_fwd",
-           "qblora_rms_norm_bwd_workspace_bytes", "qblora_rms_norm_bwd"]
+           "qblora_rms_norm_bwd_workspace_bytes", "qblora_rms_norm_bwd",
+           "qblora_adapter_table_bytes", "qblora_adapter_table", "qblora_adapter_tiles", "qblora_adapter_groups",
+           "qblora_adapters_saved_bytes", "qblora_adapters_workspace_bytes", "qblora_adapters_fwd", "qblora_adapters_bwd",
+           "qblora_adamw_plan_bytes", "qblora_adamw_plan", "qblora_grad_norm_workspace_bytes", "qblora_grad_norm",
+           "qblora_adamw_step"]
 
 PROFILE_FWD_GEMM, PROFILE_BWD_GEMM, PROFILE_MERGE, PROFILE_QUANTIZE = 0, 1, 2, 3
 PROFILE_ADAPTER_FWD, PROFILE_ADAPTER_BWD, PROFILE_ADAPTER_GRADS, PROFILE_GRAD_REDUCE = 4, 5, 6, 7
@@ -66,6 +70,25 @@ class CRope(C.Structure):
     _fields_ = [("rot", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_float), ("freq", C.c_void_p)]
 
 
+class CAdapters(C.Structure):
+    _fields_ = [("count", C.c_int32), ("d_in", C.c_int32), ("d_out", C.c_int32), ("lambda1", C.c_int32),
+                ("lambda2", C.c_int32), ("R", C.c_int32), ("table", C.c_void_p)]
+
+
+class CAdamWTensor(C.Structure):
+    _fields_ = [("n", C.c_int64), ("param", C.c_void_p), ("master", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p),
+                ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("rate", C.c_float), ("decay", C.c_float)]
+
+
+class CAdamWList(C.Structure):
+    _fields_ = [("count", C.c_int32), ("bits", C.c_int32), ("units", C.c_int64), ("plan", C.c_void_p)]
+
+
+class CAdamW(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64),
+                ("device_step", C.c_void_p), ("device_lr", C.c_void_p), ("seed", C.c_uint32)]
+
+
 # The same layouts for struct.pack: one call instead of a descriptor access per field (a description of a weight took 9 us
 # of the 10 that a small inference call spent in Python, now 2).
 _QWEIGHT, _ADAPTER = struct.Struct("=5i64s4x7Qi4x"), struct.Struct("=3if2Qi4x")
@@ -73,6 +96,8 @@ _FLOAT32 = np.dtype(np.float32)
 assert _QWEIGHT.size == C.sizeof(CQWeight) and _ADAPTER.size == C.sizeof(CAdapter)
 _KV_CACHE, _ROPE = struct.Struct("=4i2Q"), struct.Struct("=2if4xQ")
 assert _KV_CACHE.size == C.sizeof(CKVCache) and _ROPE.size == C.sizeof(CRope)
+_ADAPTERS, _ADAMW = struct.Struct("=6iQ"), struct.Struct("=4dq2QI4x")
+assert _ADAPTERS.size == C.sizeof(CAdapters) and _ADAMW.size == C.sizeof(CAdamW)
 
 
 class QBLoRAError(RuntimeError):
@@ -155,6 +180,21 @@ def lib():
         L.qblora_rms_norm_bwd_workspace_bytes.restype = C.c_size_t
         L.qblora_rms_norm_bwd_workspace_bytes.argtypes = [i64, i32]
         L.qblora_rms_norm_bwd.argtypes = [p, p, p, p, p, i64, i32, p, p, p, C.c_size_t, p]
+        for name in ("qblora_adapter_table_bytes", "qblora_adapters_saved_bytes", "qblora_adapters_workspace_bytes",
+                     "qblora_adamw_plan_bytes", "qblora_grad_norm_workspace_bytes"):
+            getattr(L, name).restype = C.c_size_t
+        L.qblora_adapter_table_bytes.argtypes = [i32]
+        L.qblora_adapter_table.argtypes = [p, i32, i32, p, p, p, p]
+        L.qblora_adapter_tiles.argtypes = [i32, i64]
+        L.qblora_adapter_groups.argtypes = [p, p, i32, i32, i64, p, p, p, p]
+        L.qblora_adapters_saved_bytes.argtypes = L.qblora_adapters_workspace_bytes.argtypes = [p, i64]
+        L.qblora_adapters_fwd.argtypes = [p, p, p, p, p, i64, i64, p, i64, p, p, C.c_size_t, p]
+        L.qblora_adapters_bwd.argtypes = [p, p, p, p, p, i64, p, i64, i64, p, p, i64, i32, p, C.c_size_t, p]
+        L.qblora_adamw_plan_bytes.argtypes = [p, i32]
+        L.qblora_adamw_plan.argtypes = [p, i32, i32, p, C.c_size_t, p, p]
+        L.qblora_grad_norm_workspace_bytes.argtypes = [p]
+        L.qblora_grad_norm.argtypes = [p, C.c_double, p, p, C.c_size_t, p]
+        L.qblora_adamw_step.argtypes = [p, p, p, p]
         L.qblora_noalloc_scratch_bytes.restype = C.c_size_t
         L.qblora_noalloc_scratch_bytes.argtypes = []
         L.qblora_linear_fwd_noalloc.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
@@ -837,3 +877,216 @@ def qblora_rms_norm_bwd(total: torch.Tensor, w: torch.Tensor, rstd: torch.Tensor
     if rc:
         _check(rc, "qblora_rms_norm_bwd")
     return dx, (dw if need_dw else None)
+
+
+# ---- many adapters on one frozen projection -------------------------------------------------------------
+
+class Adapters:
+    """The adapters of one projection, by number, and the device table that describes them (qblora_adapter_table)."""
+
+    def __init__(self, count, d_in, d_out, lambda1, lambda2, R, table):
+        self.count, self.d_in, self.d_out, self.lambda1, self.lambda2, self.R = count, d_in, d_out, lambda1, lambda2, R
+        self.table = table
+        self.adapters, self.grads = [None] * count, [None] * count       # what the table points to stays alive
+
+    def c_bytes(self) -> bytes:
+        return _ADAPTERS.pack(self.count, self.d_in, self.d_out, self.lambda1, self.lambda2, self.R, self.table.data_ptr())
+
+
+def qblora_adapter_table(adapters, d_in: int, d_out: int, lambda1: int = None, lambda2: int = None, R: int = None, grads=None,
+                         device=None, into: Adapters = None, first: int = 0) -> Adapters:
+    """The table of a list of Adapter (None: no adapter under that number).  R: room for adapters of higher ranks; grads: for
+    each adapter the fp32 tensors (dA, dB) that qblora_adapters_bwd writes, or None.  `into`: writes them to an existing table
+    instead, from number `first` on; the other entries stay."""
+    some = next((a for a in adapters if a is not None and a.A is not None and a.B is not None), None)
+    if into is None:
+        lambda1 = some.lambda1 if lambda1 is None else lambda1
+        lambda2 = some.lambda2 if lambda2 is None else lambda2
+        R = max(a.R for a in adapters if a is not None) if R is None else R
+        device = some.A.device if device is None else device
+        count = first + len(adapters)
+        table = torch.zeros(int(lib().qblora_adapter_table_bytes(count)), dtype=torch.uint8, device=device)
+        into = Adapters(count, d_in, d_out, lambda1, lambda2, R, table)
+    assert (into.d_in, into.d_out) == (d_in, d_out)
+    n = len(adapters)
+    empty = Adapter(None, None, into.lambda1, into.lambda2, 0.0)
+    for a in adapters:
+        if a is not None and a.A is not None and a.B is not None:
+            _address(a.A, _BF16, (d_in // into.lambda1, a.R))
+            _address(a.B, _BF16, (a.R, d_out // into.lambda2))
+    pairs = [None] * n if grads is None else list(grads)
+    assert len(pairs) == n
+    for a, g in zip(adapters, pairs):
+        if g is not None:
+            _address(g[0], _F32, tuple(a.A.shape))
+            _address(g[1], _F32, tuple(a.B.shape))
+    raw = b"".join((empty if a is None else a).c_bytes() for a in adapters)
+    dA, dB = ((C.c_void_p * n)(*[None if g is None else g[i].data_ptr() for g in pairs]) for i in (0, 1))
+    _check(lib().qblora_adapter_table(into.c_bytes(), first, n, raw, dA, dB, _current_stream()), "qblora_adapter_table")
+    into.adapters[first:first + n], into.grads[first:first + n] = list(adapters), pairs
+    return into
+
+
+def qblora_adapter_groups(starts: torch.Tensor, which: torch.Tensor, count: int, T: int, first: torch.Tensor = None,
+                          order: torch.Tensor = None, tiles: torch.Tensor = None):
+    """(first, order, tiles): the T tokens of a batch by adapter, which all projections share.  starts [n + 1], which [n]."""
+    n, = which.shape
+    L = lib()
+    room = L.qblora_adapter_tiles(count, T)
+    if first is None and order is None and tiles is None:                # one allocation; the tiles, which are 16 bytes each, lead it
+        whole = torch.empty(4 * room + count + 1 + T, dtype=_I32, device=which.device)
+        tiles, first, order = whole.split_with_sizes((4 * room, count + 1, T))
+        p_tiles = whole.data_ptr()
+        p_first, p_order, tiles = p_tiles + 16 * room, p_tiles + 16 * room + 4 * (count + 1), tiles.view(room, 4)
+    else:
+        first = torch.empty(count + 1, dtype=_I32, device=which.device) if first is None else first
+        order = torch.empty(T, dtype=_I32, device=which.device) if order is None else order
+        tiles = torch.empty((room, 4), dtype=_I32, device=which.device) if tiles is None else tiles
+        p_first, p_order, p_tiles = (_address(first, _I32, (count + 1,)), _address(order, _I32, (T,)),
+                                     _address(tiles, _I32, (room, 4)))
+    rc = L.qblora_adapter_groups(_address(starts, _I32, (n + 1,)), _address(which, _I32, (n,)), n, count, T, p_first, p_order,
+                                 p_tiles, _current_stream())
+    if rc:
+        _check(rc, "qblora_adapter_groups")
+    return first, order, tiles
+
+
+def _rows(t, T, width) -> int:
+    """Elements from one row of a bf16 [T, width] to the next: any number, features one behind the other."""
+    assert t.dtype is _BF16 and t.is_cuda and t.shape == (T, width)
+    if t.is_contiguous():
+        return width
+    row, feature = t.stride()
+    assert feature == 1 or width == 1
+    return row if T > 1 else max(row, width)
+
+
+def _groups(ads, groups, T):
+    first, order, tiles = groups
+    assert tiles.dim() == 2 and tiles.shape[0] == lib().qblora_adapter_tiles(ads.count, T)
+    return (_address(first, _I32, (ads.count + 1,)), _address(order, _I32, (T,)), _address(tiles, _I32, (tiles.shape[0], 4)))
+
+
+def qblora_adapters_saved_bytes(ads: Adapters, T: int) -> int:
+    return int(lib().qblora_adapters_saved_bytes(ads.c_bytes(), T))
+
+
+def qblora_adapters_workspace_bytes(ads: Adapters, T: int) -> int:
+    return int(lib().qblora_adapters_workspace_bytes(ads.c_bytes(), T))
+
+
+def _saved(saved, L, a, T):
+    if saved is None:
+        return None
+    assert saved.is_cuda and saved.is_contiguous() and saved.numel() * saved.element_size() >= L.qblora_adapters_saved_bytes(a, T)
+    return saved.data_ptr()
+
+
+def _adapters_workspace(workspace, L, a, T, device):
+    if workspace is None:
+        nbytes = L.qblora_adapters_workspace_bytes(a, T)
+        return torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def qblora_adapters_fwd(ads: Adapters, groups, X: torch.Tensor, Y: torch.Tensor, saved: torch.Tensor = None,
+                        workspace: torch.Tensor = None):
+    """Adds every token's adapter term to Y [T, d_out], in place.  groups: what qblora_adapter_groups returned."""
+    T = X.shape[0]
+    L, a = lib(), ads.c_bytes()
+    ldx, ldy = _rows(X, T, ads.d_in), _rows(Y, T, ads.d_out)
+    first, order, tiles = _groups(ads, groups, T)
+    ws, nbytes = _adapters_workspace(workspace, L, a, T, X.device)
+    rc = L.qblora_adapters_fwd(a, first, order, tiles, X.data_ptr(), ldx, T, Y.data_ptr(), ldy, _saved(saved, L, a, T),
+                               ws.data_ptr(), nbytes, _current_stream())
+    if rc:
+        _check(rc, "qblora_adapters_fwd")
+    return Y
+
+
+def qblora_adapters_bwd(ads: Adapters, groups, X, dY: torch.Tensor, dX: torch.Tensor = None, gradients: bool = True,
+                        saved: torch.Tensor = None, workspace: torch.Tensor = None):
+    """Adds the adapters' part to dX [T, d_in] (if given), in place, and writes the gradients of the table's adapters.  X may be
+    None without gradients; saved: what the forward call filled."""
+    T = dY.shape[0]
+    L, a = lib(), ads.c_bytes()
+    ldx = 0 if X is None else _rows(X, T, ads.d_in)
+    lddx = 0 if dX is None else _rows(dX, T, ads.d_in)
+    lddy = _rows(dY, T, ads.d_out)
+    first, order, tiles = _groups(ads, groups, T)
+    ws, nbytes = _adapters_workspace(workspace, L, a, T, dY.device)
+    rc = L.qblora_adapters_bwd(a, first, order, tiles, _ptr(X), ldx, dY.data_ptr(), lddy, T, _saved(saved, L, a, T), _ptr(dX),
+                               lddx, gradients, ws.data_ptr(), nbytes, _current_stream())
+    if rc:
+        _check(rc, "qblora_adapters_bwd")
+    return dX
+
+
+# ---- the optimizer's step -------------------------------------------------------------------------------
+
+class AdamWList:
+    """The tensors of a step: the C struct, and everything its device plan points to."""
+
+    def __init__(self, c, plan, tensors):
+        self.c, self.plan, self.tensors = c, plan, tensors
+        self.raw = bytes(c)
+        self.norm_bytes = int(lib().qblora_grad_norm_workspace_bytes(self.raw))
+
+
+def qblora_adamw_list(params, grads, m, v, master=None, m_scale=None, v_scale=None, rate=1.0, decay=0.0) -> AdamWList:
+    """One list of tensors for qblora_grad_norm and qblora_adamw_step, each argument a list with an entry for each tensor:
+    params bf16 (entries may be None where there is a master), grads fp32, moments m and v fp32, or float8_e4m3fn and float8_e5m2
+    with their scales; master fp32 or None; rate and decay: numbers for all, or a list."""
+    n = len(grads)
+    each = lambda x: list(x) if isinstance(x, (list, tuple)) else [x] * n  # noqa: E731
+    params, master, m_scale, v_scale, rate, decay = (each(x) for x in (params, master, m_scale, v_scale, rate, decay))
+    bits = 8 if n and m[0].dtype is torch.float8_e4m3fn else 32
+    types = (torch.float8_e4m3fn, torch.float8_e5m2) if bits == 8 else (_F32, _F32)
+    assert all(len(x) == n for x in (params, m, v, master, m_scale, v_scale, rate, decay))
+    c = (CAdamWTensor * max(n, 1))()
+    for i in range(n):
+        shape = grads[i].shape
+        k = grads[i].numel()
+        blocks = (-(-k // 256),)
+        c[i] = CAdamWTensor(k, None if params[i] is None else _address(params[i], _BF16, shape),
+                            None if master[i] is None else _address(master[i], _F32, shape), _address(grads[i], _F32, shape),
+                            _address(m[i], types[0], shape), _address(v[i], types[1], shape),
+                            _address(m_scale[i], _F32, blocks) if bits == 8 else None,
+                            _address(v_scale[i], _F32, blocks) if bits == 8 else None, rate[i], decay[i])
+    plan = torch.empty(int(lib().qblora_adamw_plan_bytes(c, n)), dtype=torch.uint8,
+                       device=grads[0].device if n else "cuda")
+    out = CAdamWList()
+    _check(lib().qblora_adamw_plan(c, n, bits, plan.data_ptr() or None, plan.numel(), C.byref(out), _current_stream()),
+           "qblora_adamw_plan")
+    return AdamWList(out, plan, (params, list(grads), list(m), list(v), master, m_scale, v_scale))
+
+
+def qblora_grad_norm(tensors: AdamWList, max_norm: float, out: torch.Tensor = None, workspace: torch.Tensor = None):
+    """fp32 [2] on the device: the norm of all gradients, and the factor that clips it to max_norm."""
+    dev = tensors.plan.device
+    if out is None:
+        out = torch.empty(2, dtype=_F32, device=dev)
+    if workspace is None:
+        workspace = torch.empty(tensors.norm_bytes, dtype=torch.uint8, device=dev)
+    rc = lib().qblora_grad_norm(tensors.raw, max_norm, _address(out, _F32, (2,)), workspace.data_ptr(),
+                                workspace.numel() * workspace.element_size(), _current_stream())
+    if rc:
+        _check(rc, "qblora_grad_norm")
+    return out
+
+
+def qblora_adamw_step(tensors: AdamWList, step, lr, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                      clip: torch.Tensor = None, seed: int = 0) -> None:
+    """One AdamW step on every tensor of the list, in place.  step, lr: numbers, or one-element tensors on the device (int64 and
+    fp32) that the call reads when it runs, as a captured graph needs; clip: what qblora_grad_norm returned."""
+    p_step = p_lr = 0
+    if isinstance(step, torch.Tensor):
+        assert step.numel() == 1
+        step, p_step = 1, _address(step, _I64, step.shape)
+    if isinstance(lr, torch.Tensor):
+        assert lr.numel() == 1
+        lr, p_lr = 0.0, _address(lr, _F32, lr.shape)
+    how = _ADAMW.pack(lr, beta1, beta2, eps, step, p_step, p_lr, seed & 0xffffffff)
+    rc = lib().qblora_adamw_step(tensors.raw, how, None if clip is None else _address(clip, _F32, (2,)), _current_stream())
+    if rc:
+        _check(rc, "qblora_adamw_step")

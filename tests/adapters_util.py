@@ -1,0 +1,236 @@
+"""Plain 64-bit forms of the operators on many adapters and of the optimizer's step, and the tensors of their tests.
+
+Everything here is numpy on the host, from the definitions in include/qblora.h."""
+import numpy as np
+import torch
+
+from paper_2407_17029_amd import synth
+
+DEV = "cuda:0"
+TILE = 64
+
+
+# ---- tensors -------------------------------------------------------------------------------------------------
+
+def dev_bf16(x):
+    return torch.from_numpy(synth.f32_to_bf16_bits(np.asarray(x, np.float32)).view(np.int16)).view(torch.bfloat16).to(DEV)
+
+
+def dev(x, dtype=np.int32):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype)).to(DEV)
+
+
+def bf16(x):
+    """The bf16 values nearest to x, as float64."""
+    return synth.bf16_bits_to_f32(synth.f32_to_bf16_bits(np.asarray(x, np.float32))).astype(np.float64)
+
+
+def host(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+# ---- tokens by adapter ---------------------------------------------------------------------------------------
+
+def tile_room(count, T):
+    return -(-T // TILE) + min(count, T)
+
+
+def groups(starts, which, count, T):
+    lists = [[] for _ in range(count)]
+    for i, a in enumerate(which):
+        if 0 <= a < count:
+            lists[a] += list(range(min(max(starts[i], 0), T), min(max(starts[i + 1], 0), T)))
+    first = np.concatenate([[0], np.cumsum([len(x) for x in lists])])
+    order = np.full(T, -1)
+    flat = [t for x in lists for t in x]
+    order[:len(flat)] = flat
+    tiles = [(a, first[a] + j, min(TILE, len(x) - j), 0) for a, x in enumerate(lists) for j in range(0, len(x), TILE)]
+    out = np.zeros((tile_room(count, T), 4), np.int64)
+    out[:len(tiles)] = np.array(tiles).reshape(-1, 4)
+    return first, order, out
+
+
+# ---- the adapter term ----------------------------------------------------------------------------------------
+
+def pool(x, lam):
+    return x.reshape(*x.shape[:-1], -1, lam).sum(-1)
+
+
+class Batch:
+    """Adapters of one projection and a batch of requests; float64 holding exact bf16 values."""
+
+    def __init__(self, seed, d_in, d_out, lam1, lam2, ranks, lengths, which, extra=0):
+        r = np.random.Generator(np.random.Philox(key=[seed, 11]))
+        self.d_in, self.d_out, self.lam1, self.lam2, self.ranks, self.which = d_in, d_out, lam1, lam2, ranks, list(which)
+        self.starts = np.concatenate([[0], np.cumsum(lengths)])
+        self.T = int(self.starts[-1]) + extra
+        self.count = len(ranks)
+        self.A = [bf16(r.uniform(-1, 1, (d_in // lam1, R)) * (lam1 / d_in) ** 0.5) for R in ranks]
+        self.B = [bf16(r.standard_normal((R, d_out // lam2)) * 0.3) for R in ranks]
+        self.s = [(0.5, 1.0, -2.0)[a % 3] for a in range(self.count)]
+        self.X, self.dX = (bf16(r.standard_normal((self.T, d_in))) for _ in range(2))
+        self.Y, self.dY = (bf16(r.standard_normal((self.T, d_out))) for _ in range(2))
+        self.owner = np.full(self.T, -1)
+        for i, a in enumerate(self.which):
+            if 0 <= a < self.count:
+                self.owner[self.starts[i]:self.starts[i + 1]] = a
+
+    def adapters(self, qb):
+        return [qb.Adapter(dev_bf16(A), dev_bf16(B), self.lam1, self.lam2, s) if R else None
+                for A, B, s, R in zip(self.A, self.B, self.s, self.ranks)]
+
+    def grads(self):
+        return [(torch.full(A.shape, float("nan"), device=DEV), torch.full(B.shape, float("nan"), device=DEV)) if R else None
+                for A, B, R in zip(self.A, self.B, self.ranks)]
+
+    def table(self, qb, R=None, grads=None):
+        return qb.qblora_adapter_table(self.adapters(qb), self.d_in, self.d_out, self.lam1, self.lam2,
+                                       R=max(self.ranks) if R is None else R, grads=grads, device=DEV)
+
+    def groups(self, qb):
+        return qb.qblora_adapter_groups(dev(self.starts), dev(self.which), self.count, self.T)
+
+    # Each result comes with a sum of the sizes of what it adds up, for the tolerances
+
+    def forward(self):
+        Y, size = self.Y.copy(), np.zeros_like(self.Y)
+        for a, R in enumerate(self.ranks):
+            t = self.owner == a
+            if not R or not t.any():
+                continue
+            P = pool(self.X[t], self.lam1) / self.lam1
+            Pabs = pool(np.abs(self.X[t]), self.lam1) / self.lam1
+            Y[t] += np.repeat(self.s[a] * (P @ self.A[a] @ self.B[a]), self.lam2, -1)
+            size[t] = np.repeat(abs(self.s[a]) * (Pabs @ np.abs(self.A[a]) @ np.abs(self.B[a])), self.lam2, -1)
+        return Y, size
+
+    def backward(self):
+        dX, size = self.dX.copy(), np.zeros_like(self.dX)
+        dA, dB, sA, sB = ([np.zeros(m.shape) for m in ms] for ms in (self.A, self.B, self.A, self.B))
+        for a, R in enumerate(self.ranks):
+            t = self.owner == a
+            if not R or not t.any():
+                continue
+            A, B, s = self.A[a], self.B[a], self.s[a]
+            for f, dest in ((lambda x: x, (dX, dA, dB)), (np.abs, (size, sA, sB))):
+                P, dV = pool(f(self.X[t]), self.lam1) / self.lam1, f(np.float64(s)) * pool(f(self.dY[t]), self.lam2)
+                dU = dV @ f(B).T
+                dest[0][t] += np.repeat(dU @ f(A).T, self.lam1, -1) / self.lam1
+                dest[1][a] += P.T @ dU
+                dest[2][a] += (P @ f(A)).T @ dV
+        return dX, dA, dB, size, sA, sB
+
+
+def half_step(x):
+    """Half the spacing of bf16 numbers at |x|."""
+    a = np.abs(x)
+    with np.errstate(invalid="ignore"):
+        e = np.floor(np.log2(np.where((a > 0) & np.isfinite(a), a, 1.0)))
+    return np.where(a > 0, np.exp2(e - 8.0), 0.0)
+
+
+def assert_rows(got, ref, size, owner, untouched, K, R, what):
+    """Rows of a bf16 array that had `size` added to them: U is off by its fp32 sums of K products (K * 2^-24 of their sizes at most) and
+    by the bf16 pair (2^-17), the sums of R products in fp32 by R * 2^-24, then one rounding of the whole to bf16.  Rows
+    without adapter keep their bits."""
+    g = host(got)
+    delta = size * (2.0 ** -17 + (K + 2 * R + 8) * 2.0 ** -24)
+    err = np.abs(g - ref)
+    allowed = delta + half_step(np.abs(ref) + delta)
+    worst = np.unravel_index(np.argmax(err - allowed), err.shape)
+    assert (err <= allowed).all(), f"{what}: off by {err[worst]:.3e} where {allowed[worst]:.3e} is allowed, at {worst}"
+    assert np.array_equal(g[owner < 0], untouched[owner < 0]), f"{what}: rows without adapter"
+
+
+def assert_grad(got, ref, size, terms, what):
+    """fp32 sums of `terms` products each of which is off by the narrow factor's parts (2^-17 of it, and its own sums, counted in
+    terms): all relative to the sum of sizes."""
+    g = got.cpu().numpy().astype(np.float64)
+    allowed = size * (2.0 ** -17 + (terms + 16) * 2.0 ** -24) + 1e-30
+    err = np.abs(g - ref)
+    assert np.isfinite(g).all(), f"{what}: not finite"
+    worst = np.unravel_index(np.argmax(err - allowed), err.shape)
+    assert (err <= allowed).all(), f"{what}: off by {err[worst]:.3e} where {allowed[worst]:.3e} is allowed, at {worst}"
+
+
+# ---- the optimizer's step ------------------------------------------------------------------------------------
+
+def wrap(x):
+    return x & np.uint64(0xffffffff)
+
+
+def random_bits(n, tensor, step, seed):
+    """32 bits of each of n elements."""
+    u = np.uint64
+    with np.errstate(over="ignore"):
+        x = np.arange(n, dtype=u) * u(0x9E3779B1) + u(tensor) * u(0x632BE5AB) + u(seed) * u(0x85157AF5) + u(step) * u(0xD168AAAD)
+        x = wrap(x)
+        x = wrap((x ^ (x >> u(16))) * u(0x6C8E9CF5))
+        x = wrap((x ^ (x >> u(15))) * u(0xB5297A4D))
+        return x ^ (x >> u(16))
+
+
+def block_scale(largest, top):
+    """Smallest power of two, 2^-126 at least, that brings the largest value within `top`."""
+    out = np.full(largest.shape, 2.0 ** -126)
+    for i, x in np.ndenumerate(largest):
+        if x > 0:
+            e = int(np.floor(np.log2(float(x) / top))) - 1
+            while float(x) > top * 2.0 ** e:
+                e += 1
+            out[i] = 2.0 ** max(e, -126)
+    return out
+
+
+def neighbours(a, mantissa, low):
+    """The values below and above a >= 0 with so many mantissa bits, equally spaced below `low`."""
+    with np.errstate(divide="ignore"):
+        e = np.floor(np.log2(np.maximum(a, low)))
+    step = np.exp2(np.maximum(e, np.log2(low)) - mantissa)
+    lower = np.floor(a / step) * step
+    return lower, lower + step
+
+
+class Moments8:
+    """Moments in 8 bits after a step, from m and v of the step in fp32 and its random bits."""
+
+    def __init__(self, m, v, random):
+        self.m, self.m_scale = self._round(m, 448.0, 3, 2.0 ** -6, random & np.uint64(0xffff), False)
+        self.v, self.v_scale = self._round(v, 57344.0, 2, 2.0 ** -14, random >> np.uint64(16), True)
+
+    @staticmethod
+    def _round(x, top, mantissa, low, r16, never_zero):
+        n = len(x)
+        pad = np.zeros(-(-n // 256) * 256)
+        pad[:n] = x
+        scale = block_scale(np.abs(pad.reshape(-1, 256)).max(1), top)
+        a = np.abs(x) / np.repeat(scale, 256)[:n]
+        lower, upper = neighbours(a, mantissa, low)
+        # the upper one if the part above the lower, with 16 random bits added, passes a whole step
+        part = (a - lower) / (upper - lower)
+        out = np.where(part + (r16.astype(np.float64) + 0.5) / 65536.0 >= 1.0, upper, lower)
+        if never_zero:
+            out = np.where((a > 0) & (out == 0), upper, out)
+        return np.copysign(out, x), scale
+
+
+def adamw(w, m, v, g, step, lr, beta1, beta2, eps, rate=1.0, decay=0.0, factor=1.0):
+    """(w, m, v) in float64; elements without a finite gradient as they were."""
+    ok = np.isfinite(g)
+    gf = np.where(ok, g, 0.0) * factor
+    m1, v1 = beta1 * m + (1.0 - beta1) * gf, beta2 * v + (1.0 - beta2) * gf * gf
+    c1, c2 = 1.0 - beta1 ** step, 1.0 - beta2 ** step
+    w1 = w * (1.0 - lr * rate * decay) - lr * rate / c1 * m1 / (np.sqrt(v1 / c2) + eps)
+    return np.where(ok, w1, w), np.where(ok, m1, m), np.where(ok, v1, v)
+
+
+def moments32(m, v, g, beta1, beta2, factor=1.0):
+    """m and v of a step in fp32, operation by operation."""
+    f = np.float32
+    with np.errstate(over="ignore"):
+        gf = (g.astype(f) * f(factor)).astype(f)
+        m1 = ((m.astype(f) * f(beta1)).astype(f) + (gf * f(1.0 - beta1)).astype(f)).astype(f)
+        v1 = ((v.astype(f) * f(beta2)).astype(f) + ((gf * gf).astype(f) * f(1.0 - beta2)).astype(f)).astype(f)
+    ok = np.isfinite(g)
+    most = f(2.0 ** 127)
+    return np.where(ok, np.clip(m1, -most, most), m.astype(f)), np.where(ok, np.minimum(v1, most), v.astype(f))
