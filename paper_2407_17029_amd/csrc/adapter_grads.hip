@@ -2,7 +2,7 @@
 //
 //   dA_a[m][r] = (1/lambda1) * pool( X^T dU ),   dB_a[r][j] = pool( dY^T (s U) ),   pool: sums of lambda adjacent features
 //
-// X and dY are contracted as they are (exact products), the narrow factors as bf16 pairs, and the features are added up in the
+// X and dY are contracted as they are (exact products), the narrow factors as three bf16 parts, and the features are added up in the
 // result's registers.  A workgroup has 128 features of X or dY and 128 r of one adapter and walks the adapter's tokens, 32 a
 // step, through LDS; both operands come out of the transposing read.  Few adapters with many tokens: the tokens go in slices, whose
 // partial sums a second launch adds up in a fixed order.
@@ -41,7 +41,8 @@ struct Job { const qblora_bf16* wide; int64_t ld; const qblora_bf16* narrow; flo
 // IS_B: the result is [R][width / LAM] (rows of the product are features), else [width / LAM][R] (rows are r)
 template <int LAM, bool IS_B>
 __device__ void gradient(const Grouped& g, const Job& job, int R, int ld_out, int p0, int p1, int i0, int r0, unsigned char* smem) {
-    unsigned char* const sw = smem; unsigned char* const sh = smem + kTile; unsigned char* const sl = smem + 2 * kTile;
+    unsigned char* const sw = smem; unsigned char* const sh = smem + kTile; unsigned char* const sm = smem + 2 * kTile;
+    unsigned char* const sl = smem + 3 * kTile;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, q = lane >> 4, s = lane & 15;
     const int64_t slice = (int64_t)g.T * g.R;
     f32x4 acc[4][4];
@@ -51,12 +52,12 @@ __device__ void gradient(const Grouped& g, const Job& job, int R, int ld_out, in
         for (int b = 0; b < 4; ++b) acc[a][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const int chunk = t & 15, row = t >> 4;                    // rows row and row + 16
     const bool wide_in = i0 + 8 * chunk < job.width, narrow_in = r0 + 8 * chunk < R;
-    uint4 rw[2], rh[2], rl[2];
+    uint4 rw[2], rh[2], rm[2], rl[2];
     auto fetch = [&](int p) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int at = p + row + 16 * i;
-            rw[i] = rh[i] = rl[i] = make_uint4(0, 0, 0, 0);
+            rw[i] = rh[i] = rm[i] = rl[i] = make_uint4(0, 0, 0, 0);
             if (at >= p1) continue;
             const int token = g.order[at];
             if (token < 0 || token >= g.T) continue;
@@ -64,7 +65,8 @@ __device__ void gradient(const Grouped& g, const Job& job, int R, int ld_out, in
             if (narrow_in) {
                 const int64_t from = (int64_t)at * g.R + r0 + 8 * chunk;
                 rh[i] = *reinterpret_cast<const uint4*>(job.narrow + from);
-                rl[i] = *reinterpret_cast<const uint4*>(job.narrow + slice + from);
+                rm[i] = *reinterpret_cast<const uint4*>(job.narrow + slice + from);
+                rl[i] = *reinterpret_cast<const uint4*>(job.narrow + 2 * slice + from);
             }
         }
     };
@@ -77,6 +79,7 @@ __device__ void gradient(const Grouped& g, const Job& job, int R, int ld_out, in
             const uint32_t to = (row + 16 * i) * kStride + 16 * chunk;
             *reinterpret_cast<uint4*>(sw + to) = rw[i];
             *reinterpret_cast<uint4*>(sh + to) = rh[i];
+            *reinterpret_cast<uint4*>(sm + to) = rm[i];
             *reinterpret_cast<uint4*>(sl + to) = rl[i];
         }
         __syncthreads();
@@ -86,10 +89,12 @@ __device__ void gradient(const Grouped& g, const Job& job, int R, int ld_out, in
         for (int a = 0; a < 4; ++a) wf[a] = tokens_of(sw + at + 2 * (w0 + 16 * a));
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            const bf16x8 h = tokens_of(sh + at + 2 * (n0 + 16 * b)), l = tokens_of(sl + at + 2 * (n0 + 16 * b));
+            const bf16x8 h = tokens_of(sh + at + 2 * (n0 + 16 * b)), m = tokens_of(sm + at + 2 * (n0 + 16 * b)),
+                         l = tokens_of(sl + at + 2 * (n0 + 16 * b));
 #pragma unroll
             for (int a = 0; a < 4; ++a) {
                 acc[a][b] = IS_B ? mma(wf[a], h, acc[a][b]) : mma(h, wf[a], acc[a][b]);
+                acc[a][b] = IS_B ? mma(wf[a], m, acc[a][b]) : mma(m, wf[a], acc[a][b]);
                 acc[a][b] = IS_B ? mma(wf[a], l, acc[a][b]) : mma(l, wf[a], acc[a][b]);
             }
         }
@@ -123,7 +128,7 @@ __device__ void gradient(const Grouped& g, const Job& job, int R, int ld_out, in
 
 template <int LAM1, int LAM2>
 __global__ __launch_bounds__(kThreads) void k_adapter_grads(AdapterGradDesc d, int tiles_a, int tiles_b) {
-    __shared__ __align__(16) unsigned char smem[3 * kTile];
+    __shared__ __align__(16) unsigned char smem[4 * kTile];
     const int a = blockIdx.y, z = blockIdx.z;
     const AdapterEntry e = d.g.table[a];
     if (!e.dA || !e.dB || e.R <= 0 || e.R > d.g.R) return;

@@ -45,20 +45,26 @@ struct RankDesc {
 int rank_splits(int tiles, int width, int R);
 int launch_rank_sums(const RankDesc& d, hipStream_t st);
 
-// out[token][n] += factor * sum_r U[place][r] * W[r][n / lam], U the sum of `splits` slices of part; W is B, or (back) the transpose
-// of A.  hi (may be NULL): U as a bf16 pair, [T][R] high parts, then as many residuals.  part2, hi2 (may be NULL): another sum of
-// splits2 slices that is written the same way.
+// U, the sum of the slices, as three bf16 parts [3][T][R]: high part and what is left of it, twice.  The second array may be absent.
+struct PartsDesc {
+    Grouped g;
+    const float* part; int splits; qblora_bf16* out;
+    const float* part2; int splits2; qblora_bf16* out2;
+};
+int launch_rank_parts(const PartsDesc& d, hipStream_t st);
+
+// out[token][n] += factor * sum_r U[place][r] * W[r][n / lam], U the parts that launch_rank_parts made, or (u NULL) the sum of
+// `splits` slices of part; W is B, or (back) the transpose of A
 struct SpreadDesc {
     Grouped g;
+    const qblora_bf16* u;
     const float* part; int splits;
-    qblora_bf16* hi;
-    const float* part2; int splits2; qblora_bf16* hi2;
-    qblora_bf16* out; int64_t ldo; int width, lam, back;     // out may be NULL
+    qblora_bf16* out; int64_t ldo; int width, lam, back;
     float factor;
 };
 int launch_spread(const SpreadDesc& d, hipStream_t st);
 
-// dA and dB of every entry that has a place for them, from X, dY and the bf16 pairs of s U and dU
+// dA and dB of every entry that has a place for them, from X, dY and the three bf16 parts of s U and of dU
 struct AdapterGradDesc {
     Grouped g;
     const qblora_bf16* X; int64_t ldx; int d_in, lam1;

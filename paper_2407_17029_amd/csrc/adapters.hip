@@ -165,106 +165,160 @@ __device__ __forceinline__ uint2 columns_of(const unsigned char* p) {
 
 __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
+// ---- copies into LDS ----------------------------------------------------------------------------------------------
+
+// 16 bytes a lane to lds_base + 16 * lane; no register is written
+__device__ __forceinline__ void copy16_to_lds(const void* p, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_base), "v"(p) : "memory", "m0");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+// At most n (uniform) of this wave's copies are under way; an odd n waits for one more
+__device__ __forceinline__ void wait_copies(int n) {
+    switch (n >> 1) {
+        case 0: asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); break;
+        case 1: asm volatile("s_waitcnt vmcnt(2)" ::: "memory"); break;
+        case 2: asm volatile("s_waitcnt vmcnt(4)" ::: "memory"); break;
+        case 3: asm volatile("s_waitcnt vmcnt(6)" ::: "memory"); break;
+        case 4: asm volatile("s_waitcnt vmcnt(8)" ::: "memory"); break;
+        case 5: asm volatile("s_waitcnt vmcnt(10)" ::: "memory"); break;
+        default: asm volatile("s_waitcnt vmcnt(12)" ::: "memory"); break;
+    }
+}
+// Every wave is here, with its reads of LDS behind it
+__device__ __forceinline__ void meet() {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // ---- rank sums ---------------------------------------------------------------------------------------------------
 //
-// Many tokens: steps of 64 inputs, Z's rows and W's through registers into LDS, double-buffered.  The matrix product's rows are r
+// Many tokens: steps of 64 inputs, Z's rows and W's copied straight into a ring of three stages in LDS.  The matrix product's rows are r
 // (16 a block, blocks dealt to the four waves), its columns tokens.  W's rows lie by input (A: the transposing read makes
-// the operand) or by r (B).  Both factors are bf16 as they are, the products exact, the sums fp32.
+// the operand) or by r (B).  Both factors are bf16 as they are, the products exact, the sums fp32.  The 16-byte chunks of
+// a row change places by its number, so that what a wave reads at once lies in different banks.
 constexpr int kRankThreads = 256, kRankRows = 256;         // r of a workgroup at most
-constexpr int kZStride = 128 + 16;                         // bytes of a token's 64 inputs in LDS
+constexpr int kRankStages = 3;
+constexpr int kZBytes = kTileTokens * 128;
 
-template <int LAM, bool BACK>
-constexpr int rank_w_bytes() { return BACK ? kRankRows * (128 / LAM + 16) : 64 / LAM * (kRankRows * 2 + 32); }
-template <int LAM, bool BACK>
-constexpr int rank_lds() { return 2 * (kTileTokens * kZStride + rank_w_bytes<LAM, BACK>()); }
+// Copies of W that a wave makes for a step, for so many r
+template <int LAM>
+__host__ __device__ constexpr int rank_w_copies(int R) { return (R * (8 / LAM) + kRankThreads - 1) / kRankThreads; }
+template <int LAM>
+int rank_lds(int R) { return kRankStages * (kZBytes + rank_w_copies<LAM>(std::min(R, kRankRows)) * kRankThreads * 16); }
+
+// Where the 16-byte chunks of a row in LDS go: chunk c of row `row` lies at c ^ swap(row, chunks of a row), so that what half a wave
+// reads at once fills all banks.  A transposing read takes two chunks of four neighbouring rows, and of four more `APART` rows on;
+// a row read takes one chunk of 16 rows.
+template <int APART>
+__device__ __forceinline__ int column_swap(int row, int chunks) {
+    const int u = (row & 3) | (APART == 8 ? row >> 1 & 4 : row & 4);
+    return chunks % 16 == 0 ? u << 1 : chunks % 8 == 0 ? u & 6 : chunks % 4 == 0 ? u >> 1 & 2 : 0;
+}
+__device__ __forceinline__ int row_swap(int row, int chunks) {
+    return chunks % 16 == 0 ? row & 15 : chunks % 8 == 0 ? row >> 1 & 7 : chunks % 4 == 0 ? row >> 2 & 3 : chunks % 2 == 0 ? row >> 3 & 1 : 0;
+}
 
 template <int LAM, bool BACK>
 __device__ void rank_many(const RankDesc& d, const Tile& tile, int step0, int step1, int r_base, float* part, unsigned char* smem) {
-    constexpr int kWBytes = rank_w_bytes<LAM, BACK>();
     constexpr int kWRows = 64 / LAM;                       // of A for a step
-    constexpr int kMost = BACK ? kRankRows * (8 / LAM) / kRankThreads : kWRows * (kRankRows / 8) / kRankThreads;   // copies a thread
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    constexpr int kMost = rank_w_copies<LAM>(kRankRows);
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int R = min(tile.R - r_base, kRankRows);
     const int J = d.width / LAM;
-    // Z: rows t >> 3 and 32 further, 16 bytes each
+    const int tb_n = (tile.tokens + 15) / 16;
+    // Z: copy i of a wave takes rows 8 (wave + 4 i) .. + 7, 128 bytes each
+    const int z_copies = tile.tokens > 32 ? 2 : 1;
     const unsigned char* z[2];
-    uint32_t z_to[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int l = (t >> 3) + 32 * i;
+        const int l = 8 * (wave + 4 * i) + (lane >> 3);
         const int token = min(max(d.g.order[tile.begin + min(l, tile.tokens - 1)], 0), d.g.T - 1);
-        z[i] = reinterpret_cast<const unsigned char*>(d.Z + (int64_t)token * d.ldz) + 16 * (t & 7);
-        z_to[i] = l * kZStride + 16 * (t & 7);
+        z[i] = reinterpret_cast<const unsigned char*>(d.Z + (int64_t)token * d.ldz) + (int64_t)step0 * 128 + 16 * ((lane & 7) ^ (lane >> 3));
     }
-    const bool two = tile.tokens > 32;
-    // W: chunks of 16 bytes
-    const int stride = BACK ? 128 / LAM + 16 : 2 * R + 32;                     // of a row in LDS
-    const int chunks = BACK ? R * (8 / LAM) : kWRows * (R / 8);
-    const unsigned char* w[kMost];
-    uint32_t w_to[kMost];
-    bool w_has[kMost];
+    // W: chunks of 16 bytes, `per` of them a row; places behind the last chunk fetch the first
+    const int per = BACK ? 8 / LAM : R / 8, chunks = R * (8 / LAM);
+    const int w_copies = rank_w_copies<LAM>(R);
+    const unsigned char* const w = reinterpret_cast<const unsigned char*>(BACK ? tile.entry->B + (int64_t)r_base * J : tile.entry->A + r_base);
+    uint32_t w_from[kMost];
 #pragma unroll
     for (int i = 0; i < kMost; ++i) {
-        const int c = t + i * kRankThreads;
-        w_has[i] = c < chunks;
-        const int per = BACK ? 8 / LAM : R / 8, row = c / per, col = c % per;
-        w[i] = BACK ? reinterpret_cast<const unsigned char*>(tile.entry->B + (int64_t)(r_base + row) * J) + 16 * col
-                    : reinterpret_cast<const unsigned char*>(tile.entry->A + (int64_t)row * tile.R + r_base) + 16 * col;
-        w_to[i] = row * stride + 16 * col;
+        int c = (i * 4 + wave) * 64 + lane;
+        if (c >= chunks) c = 0;
+        const int row = c / per, col = c % per ^ (BACK ? row_swap(row, per) : column_swap<LAM == 1 ? 8 : 4>(row, per));
+        w_from[i] = (uint32_t)row * (uint32_t)((BACK ? J : tile.R) * 2) + 16 * col;
     }
     const int64_t w_step = BACK ? 128 / LAM : (int64_t)kWRows * tile.R * 2;    // bytes to the next step
+    const unsigned char* w_at = w + step0 * w_step;
+    const int stage_bytes = kZBytes + w_copies * kRankThreads * 16;
+    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(smem)) + wave * 1024;
+    auto issue = [&](int buf) __attribute__((always_inline)) {
+        const uint32_t to = lds + buf * stage_bytes;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (i >= z_copies) break;
+            copy16_to_lds(z[i], to + i * 4096);
+            z[i] += 128;
+        }
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            if (i >= w_copies) break;
+            copy16_to_lds(w_at + w_from[i], to + kZBytes + i * 4096);
+        }
+        w_at += w_step;
+    };
     const int blocks = (R + 15) / 16, mine = (blocks - wave + 3) / 4;          // blocks wave, wave + 4, ...
-    const int tb_n = (tile.tokens + 15) / 16;
     f32x4 acc[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int b = 0; b < 4; ++b) acc[i][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    uint4 zr[2], wr[kMost];
-    auto fetch = [&](int step) __attribute__((always_inline)) {
-        zr[0] = *reinterpret_cast<const uint4*>(z[0] + (int64_t)step * 128);
-        if (two) zr[1] = *reinterpret_cast<const uint4*>(z[1] + (int64_t)step * 128);
+    // Offsets of this lane's operands in a stage: of Z by the half of a step, of W by that and by whether the block is an odd one of the
+    // wave's (blocks 4 further lie 8 chunks on, which a swap may turn; 16 chunks on it does not).  Rows of W behind R, and what lies
+    // behind the copied ones, make sums that are not kept.
+    const int g = lane >> 4, s = lane & 15, stride = 16 * per;
+    int z_off[2], w_off[2][2], which[2];
 #pragma unroll
-        for (int i = 0; i < kMost; ++i)
-            if (w_has[i]) wr[i] = *reinterpret_cast<const uint4*>(w[i] + step * w_step);
-    };
-    auto put = [&](int buf) __attribute__((always_inline)) {
-        unsigned char* const zs = smem + buf * (kTileTokens * kZStride + kWBytes);
-        *reinterpret_cast<uint4*>(zs + z_to[0]) = zr[0];
-        if (two) *reinterpret_cast<uint4*>(zs + z_to[1]) = zr[1];
+    for (int ks = 0; ks < 2; ++ks) {
+        z_off[ks] = s * 128 + 16 * ((4 * ks + g) ^ (s & 7));
+        const int k = (32 * ks + 8 * g) / LAM;                                 // first row of W of this lane's eight inputs
+        which[ks] = LAM == 4 ? (k & 3) >> 1 : k & 3;
 #pragma unroll
-        for (int i = 0; i < kMost; ++i)
-            if (w_has[i]) *reinterpret_cast<uint4*>(zs + kTileTokens * kZStride + w_to[i]) = wr[i];
-    };
-    const int g = lane >> 4, s = lane & 15;
+        for (int odd = 0; odd < 2; ++odd) {
+            if constexpr (BACK) {
+                const int row = 16 * (wave + 4 * odd) + s;
+                w_off[ks][odd] = kZBytes + row * stride + 16 * (k >> 3 ^ row_swap(row, per)) + 2 * (k & 4);
+            } else {
+                const int row = (k & ~3) + (s >> 2);
+                w_off[ks][odd] = kZBytes + row * stride + 16 * ((2 * (wave + 4 * odd) + ((s & 3) >> 1)) ^ column_swap<LAM == 1 ? 8 : 4>(row, per)) + 8 * (s & 1);
+            }
+        }
+    }
+    const int w_two = BACK ? 128 * stride : 256;                               // from a block to the second next of the wave's
     auto products = [&](int buf) __attribute__((always_inline)) {
-        const unsigned char* const zs = smem + buf * (kTileTokens * kZStride + kWBytes);
-        const unsigned char* const ws = zs + kTileTokens * kZStride;
+        const unsigned char* const at = smem + buf * stage_bytes;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             bf16x8 zf[4];
 #pragma unroll
             for (int b = 0; b < 4; ++b)
-                if (b < tb_n) zf[b] = *reinterpret_cast<const bf16x8*>(zs + (16 * b + s) * kZStride + 64 * ks + 16 * g);
+                if (b < tb_n) zf[b] = *reinterpret_cast<const bf16x8*>(at + z_off[ks] + b * 2048);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (i >= mine) break;
-                const int r0 = 16 * (wave + 4 * i);
+                const unsigned char* const from = at + w_off[ks][i & 1] + (i >> 1) * w_two;
                 bf16x8 wf;
-                const int k = (32 * ks + 8 * g) / LAM;                         // first row of W of this lane's eight inputs
-                if constexpr (BACK) {
-                    const unsigned char* row = ws + (r0 + s) * stride;         // a row of the last block may lie behind R: its sums are not kept
-                    if constexpr (LAM == 1) wf = *reinterpret_cast<const bf16x8*>(row + 2 * k);
-                    else wf = repeated<LAM>(*reinterpret_cast<const uint2*>(row + 2 * (k & ~3)), k & 3 ? (LAM == 4 ? (k & 3) >> 1 : k & 3) : 0);
+                if constexpr (BACK && LAM == 1) {
+                    wf = *reinterpret_cast<const bf16x8*>(from);
+                } else if constexpr (BACK) {
+                    wf = repeated<LAM>(*reinterpret_cast<const uint2*>(from), which[ks]);
+                } else if constexpr (LAM == 1) {
+                    const uint2 lo = columns_of(from), hi = columns_of(from + 4 * stride);     // four rows on the chunks are moved alike
+                    wf = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
                 } else {
-                    const unsigned char* at = ws + ((k & ~3) + (s >> 2)) * stride + 2 * r0 + 8 * (s & 3);
-                    if constexpr (LAM == 1) {
-                        const uint2 lo = columns_of(at), hi = columns_of(at + 4 * stride);
-                        wf = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
-                    } else {
-                        wf = repeated<LAM>(columns_of(at), LAM == 4 ? (k & 3) >> 1 : k & 3);
-                    }
+                    wf = repeated<LAM>(columns_of(from), which[ks]);
                 }
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
@@ -272,15 +326,16 @@ __device__ void rank_many(const RankDesc& d, const Tile& tile, int step0, int st
             }
         }
     };
-    fetch(step0);
-    put(0);
-    __syncthreads();
-    for (int step = step0; step < step1; ++step) {
-        const int buf = (step - step0) & 1;
-        if (step + 1 < step1) fetch(step + 1);
+    const int steps = step1 - step0, per_stage = z_copies + w_copies;
+    issue(0);
+    if (steps > 1) issue(1);
+    int buf = 0;
+    for (int step = 0; step < steps; ++step) {
+        wait_copies(step + 1 < steps ? per_stage : 0);
+        meet();                                                                // this stage is in, the one before it is free
+        if (step + 2 < steps) issue(buf == 0 ? 2 : buf - 1);
         products(buf);
-        if (step + 1 < step1) put(buf ^ 1);
-        __syncthreads();
+        buf = buf == 2 ? 0 : buf + 1;
     }
     const float f = d.factor * tile.entry->s;
 #pragma unroll
@@ -313,17 +368,25 @@ __global__ __launch_bounds__(kRankThreads) void k_rank_sums(RankDesc d) {
 
 // ---- spread ------------------------------------------------------------------------------------------------------
 //
-// Many tokens: U as a bf16 pair (high part and what is left: 16 significant bits) in registers, 16 tokens a wave, all r; steps of
-// 64 rows of outputs over W through LDS.  The matrix product's rows are outputs / lam, its columns tokens, so that a lane has 4
-// neighbouring rows of one token, 4 lam outputs.
+// U as a bf16 pair (high part and what is left: 16 significant bits) in registers, 16 tokens a wave, all r.  Steps of 128 outputs
+// (64 with lam = 1): the rows of W that serve them and the outputs as they were go straight into a ring in LDS.  The matrix
+// product's rows are outputs / lam, its columns tokens, so that a lane has 4 neighbouring rows of one token, 4 lam outputs.
+// The results of a step are stored behind the next barrier, before the next copies are issued: the newest operations a wave waits
+// around are then its copies alone, whose number it knows.
 constexpr int kSpreadThreads = 256;
-
-template <int KS>
-constexpr int spread_u_stride() { return 64 * KS + 16; }                       // bytes of a token's U in LDS
-template <int KS, bool BACK>
-constexpr int spread_w_bytes() { return BACK ? 64 * (64 * KS + 16) : 32 * KS * (128 + 32); }
-template <int KS, bool BACK>
-constexpr int spread_lds() { return std::max(2 * kTileTokens * spread_u_stride<KS>(), 2 * spread_w_bytes<KS, BACK>()); }
+// Rows of W for a step; half as many for inner ranks above 256, whose rows are long
+template <int LAM, int KS>
+__host__ __device__ constexpr int spread_rows() { return KS <= 8 ? (LAM == 1 ? 64 : 128 / LAM) : LAM == 1 ? 32 : LAM == 8 ? 16 : 64 / LAM; }
+template <int LAM, int KS>
+__host__ __device__ constexpr int spread_out_bytes() { return 2 * LAM * spread_rows<LAM, KS>(); }     // of a token, for a step
+template <int LAM, int KS>
+__host__ __device__ constexpr int spread_w_copies(int R) { return (R * (spread_rows<LAM, KS>() / 8) + kSpreadThreads - 1) / kSpreadThreads; }
+template <int LAM, int KS>
+__host__ __device__ constexpr int spread_stage_bytes(int R) {
+    return kTileTokens * spread_out_bytes<LAM, KS>() + spread_w_copies<LAM, KS>(R) * kSpreadThreads * 16;
+}
+// U of a tile in LDS, where the workgroup adds up the slices
+__host__ __device__ constexpr int spread_u_bytes(int tokens, int R) { return (tokens < kTileTokens ? tokens : kTileTokens) * 4 * R; }
 
 __device__ __forceinline__ void split_pair(float4 v, uint2* hi, uint2* lo) {
     hi->x = pack_bf16(v.x, v.y); hi->y = pack_bf16(v.z, v.w);
@@ -331,163 +394,241 @@ __device__ __forceinline__ void split_pair(float4 v, uint2* hi, uint2* lo) {
     lo->y = pack_bf16(v.z - bf16_lo(hi->y), v.w - bf16_hi(hi->y));
 }
 
-// Four neighbouring r of the sum of the slices
+// Four neighbouring r of the sum of the slices, always in the same order; eight loads under way together
 __device__ __forceinline__ float4 sum_slices(const float* part, int splits, int64_t slice, int64_t at) {
-    float4 v = *reinterpret_cast<const float4*>(part + at);
-    for (int z = 1; z < splits; ++z) {
-        const float4 w = *reinterpret_cast<const float4*>(part + z * slice + at);
-        v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int z0 = 0; z0 < splits; z0 += 8) {
+        float4 w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const float4*>(part + (int64_t)min(z0 + i, splits - 1) * slice + at);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (z0 + i < splits) { v.x += w[i].x; v.y += w[i].y; v.z += w[i].z; v.w += w[i].w; }
     }
     return v;
 }
 
-// The rows of one tile as a bf16 pair
-__device__ __forceinline__ void write_pairs(const Grouped& g, const Tile& tile, const float* part, int splits, qblora_bf16* hi) {
+// The U of a tile in LDS, 4 R bytes a token; where R is a multiple of 32 the 16-byte chunks change places by the token
+__device__ __forceinline__ int u_at(int l, int quad, int R) { return 4 * R * l + 16 * (quad ^ (R % 32 == 0 ? l & 7 : 0)); }
+__device__ __forceinline__ void sum_tile(const SpreadDesc& d, const Tile& tile, unsigned char* us) {
     const int quads = tile.R / 4;
-    const int64_t slice = (int64_t)g.T * g.R;
-    for (int i = threadIdx.x; i < tile.tokens * quads; i += kSpreadThreads) {
-        const int64_t at = (int64_t)(tile.begin + i / quads) * g.R + 4 * (i % quads);
-        uint2 h, l;
-        split_pair(sum_slices(part, splits, slice, at), &h, &l);
-        *reinterpret_cast<uint2*>(hi + at) = h;
-        *reinterpret_cast<uint2*>(hi + slice + at) = l;
-    }
+    const int64_t slice = (int64_t)d.g.T * d.g.R;
+    for (int i = threadIdx.x; i < tile.tokens * quads; i += kSpreadThreads)
+        *reinterpret_cast<float4*>(us + u_at(i / quads, i % quads, tile.R)) =
+            sum_slices(d.part, d.splits, slice, (int64_t)(tile.begin + i / quads) * d.g.R + 4 * (i % quads));
+    __syncthreads();
 }
 
-// LAM values of a row: out += v
+// 4 rows of LAM outputs each: what was there, at `from`, and f * v
 template <int LAM>
-__device__ __forceinline__ void add_outputs(qblora_bf16* out, const f32x4& v, float f) {
-    // 4 rows of LAM outputs each
+__device__ __forceinline__ void add_outputs(uint4* o, const unsigned char* from, const f32x4& v, float f, int chunk, int swap) {
     if constexpr (LAM == 1) {
-        uint2 o = *reinterpret_cast<uint2*>(out);
-        o.x = pack_bf16(bf16_lo(o.x) + f * v[0], bf16_hi(o.x) + f * v[1]);
-        o.y = pack_bf16(bf16_lo(o.y) + f * v[2], bf16_hi(o.y) + f * v[3]);
-        *reinterpret_cast<uint2*>(out) = o;
+        const uint2 w = *reinterpret_cast<const uint2*>(from + 16 * ((chunk >> 1) ^ swap) + 8 * (chunk & 1));
+        o->x = pack_bf16(bf16_lo(w.x) + f * v[0], bf16_hi(w.x) + f * v[1]);
+        o->y = pack_bf16(bf16_lo(w.y) + f * v[2], bf16_hi(w.y) + f * v[3]);
     } else {
 #pragma unroll
         for (int i = 0; i < LAM / 2; ++i) {
-            uint4 o = *reinterpret_cast<uint4*>(out + 8 * i);
-            uint32_t* w = reinterpret_cast<uint32_t*>(&o);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float x = f * v[(8 * i + 2 * j) / LAM];
-                w[j] = pack_bf16(bf16_lo(w[j]) + x, bf16_hi(w[j]) + x);
-            }
-            *reinterpret_cast<uint4*>(out + 8 * i) = o;
+            const uint4 w = *reinterpret_cast<const uint4*>(from + 16 * ((chunk * (LAM / 2) + i) ^ swap));
+            const float x = f * v[8 * i / LAM], y = f * v[(8 * i + 2) / LAM], z = f * v[(8 * i + 4) / LAM], u = f * v[(8 * i + 6) / LAM];
+            o[i] = make_uint4(pack_bf16(bf16_lo(w.x) + x, bf16_hi(w.x) + x), pack_bf16(bf16_lo(w.y) + y, bf16_hi(w.y) + y),
+                              pack_bf16(bf16_lo(w.z) + z, bf16_hi(w.z) + z), pack_bf16(bf16_lo(w.w) + u, bf16_hi(w.w) + u));
         }
     }
 }
 
 template <int LAM, bool BACK, int KS>
-__device__ void spread_many(const SpreadDesc& d, const Tile& tile, int j0, int j1, unsigned char* smem) {
-    constexpr int kUStride = spread_u_stride<KS>(), kWBytes = spread_w_bytes<KS, BACK>();
-    constexpr int kWStride = BACK ? 64 * KS + 16 : 128 + 32;
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, g = lane >> 4, s = lane & 15;
-    const int R = tile.R, J = d.width / LAM;
+__global__ __launch_bounds__(kSpreadThreads) void k_spread(SpreadDesc d, int rows, int stages) {       // rows: outputs / lam of a workgroup
+    extern __shared__ __align__(16) unsigned char smem[];
+    constexpr int kRows = spread_rows<LAM, KS>(), kOutBytes = spread_out_bytes<LAM, KS>(), kOutChunks = kOutBytes / 16;
+    constexpr int kBlocks = kRows / 16;                                        // of 16 rows of W, for a step
+    constexpr int kMost = spread_w_copies<LAM, KS>(32 * KS);
+    Tile tile;
+    if (!read_tile(d.g, blockIdx.x, &tile)) return;
+    const int J = d.width / LAM, j0 = blockIdx.y * rows, j1 = min(j0 + rows, J);
+    if (j0 >= j1) return;
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4, s = lane & 15;
+    const int R = tile.R;
     const int64_t slice = (int64_t)d.g.T * d.g.R;
     // token blocks: 1, 2 or 4 of them side by side, the other waves take other rows of W
     const int tbs = tile.tokens <= 16 ? 1 : tile.tokens <= 32 ? 2 : 4;
-    for (int i = t; i < 16 * tbs * KS * 8; i += kSpreadThreads) {
-        const int l = i / (KS * 8), r = 4 * (i % (KS * 8));
-        uint2 h = make_uint2(0, 0), lo = h;
-        if (l < tile.tokens && r < R) split_pair(sum_slices(d.part, d.splits, slice, (int64_t)(tile.begin + l) * d.g.R + r), &h, &lo);
-        *reinterpret_cast<uint2*>(smem + l * kUStride + 2 * r) = h;
-        *reinterpret_cast<uint2*>(smem + (kTileTokens + l) * kUStride + 2 * r) = lo;
+    // outputs: a copy is 1 KB of neighbouring tokens' 128 (64) outputs; what lies behind the row's end fetches its last chunk
+    constexpr int kTokensACopy = 1024 / kOutBytes;
+    const int o_copies = max(1, tbs * 16 / (4 * kTokensACopy));
+    const unsigned char* o_from[16 / kTokensACopy];
+    int o_col[16 / kTokensACopy];
+    const int o_last = 2 * d.width - 16;
+#pragma unroll
+    for (int i = 0; i < 16 / kTokensACopy; ++i) {
+        const int l = kTokensACopy * (wave + 4 * i) + lane / kOutChunks;
+        const int token = min(max(d.g.order[tile.begin + min(l, tile.tokens - 1)], 0), d.g.T - 1);
+        o_from[i] = reinterpret_cast<const unsigned char*>(d.out + (int64_t)token * d.ldo);
+        o_col[i] = 2 * LAM * j0 + 16 * (lane % kOutChunks ^ (l & (kOutChunks - 1)));
     }
-    __syncthreads();
+    // W: chunks of 16 bytes, `per` of them a row; places behind the last chunk, or behind the last row of outputs, fetch the first
+    const int per = BACK ? R / 8 : kRows / 8, chunks = R * (kRows / 8);
+    const int w_copies = spread_w_copies<LAM, KS>(R);
+    const unsigned char* const w = reinterpret_cast<const unsigned char*>(BACK ? tile.entry->A : tile.entry->B);
+    uint32_t w_from[kMost];
+    int w_row[kMost];                                                          // first of the step's outputs / lam that the chunk holds
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        int c = (i * 4 + wave) * 64 + lane;
+        if (c >= chunks) c = 0;
+        const int row = c / per, col = c % per ^ (BACK ? row_swap(row, per) : column_swap<8>(row, per));
+        w_from[i] = (uint32_t)row * (uint32_t)((BACK ? R : J) * 2) + 16 * col;
+        w_row[i] = BACK ? row : 8 * col;
+    }
+    const int stage_bytes = kTileTokens * kOutBytes + w_copies * kSpreadThreads * 16;
+    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(smem)) + wave * 1024;
+    auto issue = [&](int j, int buf) __attribute__((always_inline)) {
+        const uint32_t to = lds + buf * stage_bytes;
+#pragma unroll
+        for (int i = 0; i < 16 / kTokensACopy; ++i) {
+            if (i >= o_copies) break;
+            copy16_to_lds(o_from[i] + min(o_col[i] + 2 * LAM * (j - j0), o_last), to + i * 4096);
+        }
+        const unsigned char* const at = w + (BACK ? (int64_t)j * R * 2 : (int64_t)j * 2);
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            if (i >= w_copies) break;
+            copy16_to_lds(j + w_row[i] < J ? at + w_from[i] : w, to + kTileTokens * kOutBytes + i * 4096);
+        }
+    };
+    issue(j0, 0);
+    if (stages == 3 && j0 + kRows < j1) issue(j0 + kRows, 1);
+
     const int tb = wave % tbs, jb0 = wave / tbs, jb_step = 4 / tbs;
-    bf16x8 uh[KS], ul[KS];
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-        uh[k] = *reinterpret_cast<const bf16x8*>(smem + (16 * tb + s) * kUStride + 64 * k + 16 * g);
-        ul[k] = *reinterpret_cast<const bf16x8*>(smem + (kTileTokens + 16 * tb + s) * kUStride + 64 * k + 16 * g);
-    }
-    __syncthreads();
-    // W by chunks of 16 bytes: 8 a row of r (B), R / 8 a row of outputs (A); r behind R are zero
-    const unsigned char* w[KS];
-    uint32_t w_to[KS];
-    int w_row[KS];
-    bool w_has[KS];
-#pragma unroll
-    for (int i = 0; i < KS; ++i) {
-        const int c = t + i * kSpreadThreads;
-        const int row = BACK ? c / (4 * KS) : c >> 3, col = BACK ? c % (4 * KS) : c & 7;
-        w_row[i] = BACK ? row : 8 * col;                                       // first of its outputs / lam in the step
-        w_has[i] = BACK ? 8 * col < R : row < R;
-        w[i] = BACK ? reinterpret_cast<const unsigned char*>(tile.entry->A + (int64_t)row * R) + 16 * col
-                    : reinterpret_cast<const unsigned char*>(tile.entry->B + (int64_t)row * J) + 16 * col;
-        w_to[i] = row * kWStride + 16 * col;
-    }
-    uint4 wr[KS];
-    auto fetch = [&](int j) __attribute__((always_inline)) {
-        const int64_t by = BACK ? (int64_t)j * R * 2 : (int64_t)j * 2;
-#pragma unroll
-        for (int i = 0; i < KS; ++i)
-            wr[i] = w_has[i] && j + w_row[i] < J ? *reinterpret_cast<const uint4*>(w[i] + by) : make_uint4(0, 0, 0, 0);
-    };
-    auto put = [&](int buf) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < KS; ++i) *reinterpret_cast<uint4*>(smem + buf * kWBytes + w_to[i]) = wr[i];
-    };
     const int l = 16 * tb + s;
     const int token = l < tile.tokens ? d.g.order[tile.begin + l] : -1;
     const bool real = token >= 0 && token < d.g.T;
     qblora_bf16* const out = d.out + (int64_t)(real ? token : 0) * d.ldo;
-    fetch(j0);
-    put(0);
-    __syncthreads();
-    for (int j = j0; j < j1; j += 64) {
-        const int buf = ((j - j0) >> 6) & 1;
-        if (j + 64 < j1) fetch(j + 64);
-        for (int jb = jb0; jb < 4; jb += jb_step) {
+    bf16x8 uh[KS], ul[KS];
+    const int l_real = min(l, tile.tokens - 1);
+    if (!d.u) {
+        unsigned char* const us = smem + stages * spread_stage_bytes<LAM, KS>(d.g.R);
+        sum_tile(d, tile, us);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const int r = 32 * k + 8 * g;
+            uint2 h0 = make_uint2(0, 0), h1 = h0, l0 = h0, l1 = h0;
+            if (r < R) {
+                split_pair(*reinterpret_cast<const float4*>(us + u_at(l_real, r / 4, R)), &h0, &l0);
+                split_pair(*reinterpret_cast<const float4*>(us + u_at(l_real, r / 4 + 1, R)), &h1, &l1);
+            }
+            uh[k] = __builtin_bit_cast(bf16x8, make_uint4(h0.x, h0.y, h1.x, h1.y));
+            ul[k] = __builtin_bit_cast(bf16x8, make_uint4(l0.x, l0.y, l1.x, l1.y));
+        }
+    } else {
+        const qblora_bf16* const row = d.u + (int64_t)(tile.begin + l_real) * d.g.R;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const int r = 32 * k + 8 * g;
+            uint4 h = make_uint4(0, 0, 0, 0), lo = h;
+            if (r < R) {
+                h = *reinterpret_cast<const uint4*>(row + r);
+                lo = *reinterpret_cast<const uint4*>(row + slice + r);
+            }
+            uh[k] = __builtin_bit_cast(bf16x8, h);
+            ul[k] = __builtin_bit_cast(bf16x8, lo);
+        }
+    }
+    const int last = (R - 1) / 32;                                             // step of r that may hold r behind R
+    const bool behind = 32 * last + 8 * g >= R;
+    // Offsets of this lane's operands in a stage.  B: the rows of 32 r lie a whole number of times 16 rows on, where the chunks are
+    // moved alike, and so do four rows; a block's chunks change places with the block's number.  A: 8 chunks on, likewise.
+    constexpr int kWAt = kTileTokens * kOutBytes;
+    int w_off[BACK ? 4 : 1];
+    if constexpr (BACK) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w_off[k] = kWAt + s * 2 * R + 16 * ((4 * k + g) ^ row_swap(s, per));
+    } else {
+        const int row = 8 * g + (s >> 2);
+        w_off[0] = row * (2 * kRows) + 16 * (((s & 3) >> 1) ^ column_swap<8>(row, kRows / 8)) + 8 * (s & 1);
+    }
+    uint4 result[kBlocks][LAM == 1 ? 1 : LAM / 2];
+    int result_at[kBlocks];
+    auto store = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) {
+            if (jb0 + i * jb_step >= kBlocks || result_at[i] >= J || !real) continue;
+            qblora_bf16* const o = out + (int64_t)result_at[i] * LAM;
+            if constexpr (LAM == 1) *reinterpret_cast<uint2*>(o) = make_uint2(result[i][0].x, result[i][0].y);
+            else
+#pragma unroll
+                for (int e = 0; e < LAM / 2; ++e) *reinterpret_cast<uint4*>(o + 8 * e) = result[i][e];
+        }
+    };
+    const int per_stage = o_copies + w_copies;
+    int buf = 0;
+    for (int j = j0; j < j1; j += kRows) {
+        wait_copies(stages == 3 && j + kRows < j1 ? per_stage : 0);
+        meet();                                                                // this step is in, the stage of the one before is free
+        if (j > j0) store();
+        const int ahead = j + (stages - 1) * kRows;
+        if (ahead < j1) issue(ahead, buf == 0 ? stages - 1 : buf - 1);
+        const unsigned char* const os = smem + buf * stage_bytes;
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) {
+            const int jb = jb0 + i * jb_step;
+            if (jb >= kBlocks) break;
             f32x4 acc{0.0f, 0.0f, 0.0f, 0.0f};
-            const unsigned char* const ws = smem + buf * kWBytes;
+            const unsigned char* const block = BACK ? os + jb * (32 * R) : os + kWAt + (w_off[0] ^ (32 * jb));
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
+                if (k > last) break;
                 bf16x8 wf;
                 if constexpr (BACK) {
-                    wf = *reinterpret_cast<const bf16x8*>(ws + (16 * jb + s) * kWStride + 64 * k + 16 * g);
+                    wf = *reinterpret_cast<const bf16x8*>(block + w_off[k & 3] + 256 * (k >> 2));
                 } else {
-                    const unsigned char* at = ws + (32 * k + 8 * g + (s >> 2)) * kWStride + 32 * jb + 8 * (s & 3);
-                    const uint2 lo = columns_of(at), hi = columns_of(at + 4 * kWStride);
+                    const uint2 lo = columns_of(block + 64 * k * kRows), hi = columns_of(block + 64 * k * kRows + 8 * kRows);
                     wf = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
                 }
+                if (k == last && behind) wf = __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0));    // U is 0 there, W may be anything
                 acc = mma(wf, uh[k], acc);
                 acc = mma(wf, ul[k], acc);
             }
-            const int at = j + 16 * jb + 4 * g;
-            if (real && at < J) add_outputs<LAM>(out + (int64_t)at * LAM, acc, d.factor);
+            result_at[i] = j + 16 * jb + 4 * g;
+            add_outputs<LAM>(result[i], os + l * kOutBytes, acc, d.factor, 4 * jb + g, l & (kOutChunks - 1));
         }
-        if (j + 64 < j1) put(buf ^ 1);
-        __syncthreads();
+        buf = buf == stages - 1 ? 0 : buf + 1;
     }
+    store();
 }
 
-template <int LAM, bool BACK, int KS>
-__global__ __launch_bounds__(kSpreadThreads) void k_spread(SpreadDesc d, int rows) {       // rows: outputs / lam of a workgroup
-    extern __shared__ __align__(16) unsigned char smem[];
+// U as three bf16 parts, 24 significant bits: the sums of the slices of one or two arrays
+__global__ __launch_bounds__(256) void k_rank_parts(PartsDesc d) {
     Tile tile;
     if (!read_tile(d.g, blockIdx.x, &tile)) return;
-    if (blockIdx.y == 0) {
-        if (d.hi) write_pairs(d.g, tile, d.part, d.splits, d.hi);
-        if (d.hi2) write_pairs(d.g, tile, d.part2, d.splits2, d.hi2);
+    const bool second = blockIdx.y != 0;
+    const float* const part = second ? d.part2 : d.part;
+    qblora_bf16* const out = second ? d.out2 : d.out;
+    const int splits = second ? d.splits2 : d.splits, quads = tile.R / 4;
+    const int64_t slice = (int64_t)d.g.T * d.g.R;
+    for (int i = blockIdx.z * 256 + threadIdx.x; i < tile.tokens * quads; i += gridDim.z * 256) {
+        const int64_t at = (int64_t)(tile.begin + i / quads) * d.g.R + 4 * (i % quads);
+        const float4 v = sum_slices(part, splits, slice, at);
+        uint2 h, m, l;
+        split_pair(v, &h, &m);
+        l.x = pack_bf16(v.x - bf16_lo(h.x) - bf16_lo(m.x), v.y - bf16_hi(h.x) - bf16_hi(m.x));
+        l.y = pack_bf16(v.z - bf16_lo(h.y) - bf16_lo(m.y), v.w - bf16_hi(h.y) - bf16_hi(m.y));
+        *reinterpret_cast<uint2*>(out + at) = h;
+        *reinterpret_cast<uint2*>(out + slice + at) = m;
+        *reinterpret_cast<uint2*>(out + 2 * slice + at) = l;
     }
-    if (!d.out) return;
-    const int j0 = blockIdx.y * rows, j1 = min(j0 + rows, d.width / LAM);
-    if (j0 >= j1) return;
-    spread_many<LAM, BACK, KS>(d, tile, j0, j1, smem);
 }
 
+// Every CU's whole LDS may be asked for
 template <typename K>
-int allow_lds(K kernel, int bytes) {
-    return bytes <= 65536 || hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess
+int allow_lds(K kernel) {
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess
                ? QBLORA_OK : QBLORA_ERR_LAUNCH;
 }
 
 template <int LAM, bool BACK>
 int rank_sums(const RankDesc& d, hipStream_t st) {
-    constexpr int lds = rank_lds<LAM, BACK>();
-    const int rc = allow_lds(k_rank_sums<LAM, BACK>, lds);
+    const int lds = rank_lds<LAM>(d.g.R);
+    const int rc = allow_lds(k_rank_sums<LAM, BACK>);
     if (rc) return rc;
     k_rank_sums<LAM, BACK><<<dim3(d.g.tile_room, d.splits, (d.g.R + kRankRows - 1) / kRankRows), kRankThreads, lds, st>>>(d);
     return launch_status();
@@ -495,13 +636,16 @@ int rank_sums(const RankDesc& d, hipStream_t st) {
 
 template <int LAM, bool BACK, int KS>
 int spread(const SpreadDesc& d, hipStream_t st) {
-    constexpr int lds = spread_lds<KS, BACK>();
-    const int rc = allow_lds(k_spread<LAM, BACK, KS>, lds);
+    const int rc = allow_lds(k_spread<LAM, BACK, KS>);
     if (rc) return rc;
-    const int J = d.width / LAM, steps = (J + 63) / 64;
+    constexpr int kRows = spread_rows<LAM, KS>();
+    const int J = d.width / LAM, steps = (J + kRows - 1) / kRows;
     const int parts = std::min(steps, std::max(1, 1024 / d.g.tile_room));
-    const int rows = (steps + parts - 1) / parts * 64;
-    k_spread<LAM, BACK, KS><<<dim3(d.g.tile_room, d.out ? (J + rows - 1) / rows : 1), kSpreadThreads, lds, st>>>(d, rows);
+    const int rows = (steps + parts - 1) / parts * kRows;
+    // three stages in the ring where two workgroups still fit a CU, else two if these do, else three if they fit at all
+    const int stage = spread_stage_bytes<LAM, KS>(d.g.R), more = d.u ? 0 : spread_u_bytes(d.g.T, d.g.R), half = 80 * 1024;
+    const int stages = 3 * stage + more <= half ? 3 : 2 * stage + more <= half ? 2 : 3 * stage + more <= 2 * half ? 3 : 2;
+    k_spread<LAM, BACK, KS><<<dim3(d.g.tile_room, (J + rows - 1) / rows), kSpreadThreads, stages * stage + more, st>>>(d, rows, stages);
     return launch_status();
 }
 template <int LAM, bool BACK>
@@ -521,7 +665,7 @@ int launch_adapter_table(const TableDesc& d, hipStream_t st) {
 
 int launch_adapter_groups(const GroupsDesc& d, hipStream_t st) {
     const int lds = (2 * ((d.n + 3) & ~3) + 2 * d.count + kGroupRequests) * 4;
-    const int rc = allow_lds(k_adapter_groups, lds);
+    const int rc = allow_lds(k_adapter_groups);
     if (rc) return rc;
     k_adapter_groups<<<std::max(1, (d.n + kGroupRequests - 1) / kGroupRequests), kGroupThreads, lds, st>>>(d);
     return launch_status();
@@ -545,6 +689,12 @@ int launch_rank_sums(const RankDesc& d, hipStream_t st) {
         case 4: return rank_sums<4, false>(d, st);
         default: return rank_sums<8, false>(d, st);
     }
+}
+
+int launch_rank_parts(const PartsDesc& d, hipStream_t st) {
+    const int z = std::max(1, std::min(kTileTokens * d.g.R / 1024, 512 / d.g.tile_room));
+    k_rank_parts<<<dim3(d.g.tile_room, d.out2 ? 2 : 1, z), 256, 0, st>>>(d);
+    return launch_status();
 }
 
 int launch_spread(const SpreadDesc& d, hipStream_t st) {

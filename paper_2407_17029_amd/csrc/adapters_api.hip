@@ -36,6 +36,10 @@ int check_rows(const void* p, int64_t ld, int width) {
     if (ld < width || ld % 8 || !aligned(p, 16)) return QBLORA_ERR_SHAPE;
     return QBLORA_OK;
 }
+// From so many tokens on, or inner ranks whose sums do not fit LDS beside the rest, sums that are cut into slices are added up once, in
+// a launch of their own, and not by every workgroup that needs them
+bool parts_pay(int64_t T, int R) { return T >= 1024 || R > 256; }
+
 int tile_room(int count, int64_t T) { return (int)((T + kTileTokens - 1) / kTileTokens + std::min<int64_t>(count, T)); }
 
 Grouped grouped(const qblora_adapters* a, const int32_t* first, const int32_t* order, const int32_t* tiles, int64_t T) {
@@ -45,7 +49,7 @@ Grouped grouped(const qblora_adapters* a, const int32_t* first, const int32_t* o
     return g;
 }
 
-// The workspace, in this order: partial sums of the rank sums on X and on dY, the bf16 pairs of s U and dU, partial gradients
+// The workspace, in this order: partial sums of the rank sums on X and on dY, the bf16 parts of s U and dU, partial gradients
 struct Space { size_t part_x, part_y, su, du, grads, all; };
 Space space_of(const qblora_adapters* a, int64_t T) {
     const int tiles = tile_room(a->count, T);
@@ -53,7 +57,7 @@ Space space_of(const qblora_adapters* a, int64_t T) {
     Space s{};
     s.part_x = up256(rows * 4 * rank_splits(tiles, a->d_in, a->R));
     s.part_y = up256(rows * 4 * rank_splits(tiles, a->d_out, a->R));
-    s.su = s.du = up256(rows * 4);
+    s.su = s.du = up256(rows * 6);
     const int splits = adapter_grad_splits(a->count, T, a->d_in, a->d_out, a->R);
     if (splits > 1)
         s.grads = up256((size_t)splits * a->count * ((size_t)a->d_in / a->lambda1 + a->d_out / a->lambda2) * a->R * 4);
@@ -139,7 +143,7 @@ int qblora_adapter_groups(const int32_t* starts, const int32_t* which, int32_t n
 }
 
 size_t qblora_adapters_saved_bytes(const qblora_adapters* a, int64_t T) {
-    return check_adapters(a) || T < 0 || T > kMostGroupTokens ? 0 : (size_t)T * a->R * 4;
+    return check_adapters(a) || T < 0 || T > kMostGroupTokens ? 0 : (size_t)T * a->R * 6;
 }
 
 size_t qblora_adapters_workspace_bytes(const qblora_adapters* a, int64_t T) {
@@ -164,7 +168,14 @@ int qblora_adapters_fwd(const qblora_adapters* a, const int32_t* first, const in
     u.part = reinterpret_cast<float*>(workspace); u.splits = rank_splits(u.g.tile_room, a->d_in, a->R);
     if ((rc = launch_rank_sums(u, as_stream(stream)))) return rc;
     SpreadDesc v{};
-    v.g = u.g; v.part = u.part; v.splits = u.splits; v.hi = saved;
+    v.g = u.g; v.part = u.part; v.splits = u.splits;
+    if (saved || parts_pay(T, a->R)) {
+        PartsDesc w{};
+        w.g = u.g; w.part = u.part; w.splits = u.splits;
+        w.out = saved ? saved : reinterpret_cast<qblora_bf16*>(reinterpret_cast<unsigned char*>(workspace) + s.part_x + s.part_y);
+        if ((rc = launch_rank_parts(w, as_stream(stream)))) return rc;
+        v.u = w.out;
+    }
     v.out = Y; v.ldo = ldy; v.width = a->d_out; v.lam = a->lambda2; v.back = 0; v.factor = 1.0f;
     return launch_spread(v, as_stream(stream));
 }
@@ -202,15 +213,23 @@ int qblora_adapters_bwd(const qblora_adapters* a, const int32_t* first, const in
         u.part = part_x; u.splits = rank_splits(u.g.tile_room, a->d_in, a->R);
         if ((rc = launch_rank_sums(u, st))) return rc;
     }
-    SpreadDesc v{};
-    v.g = w.g;
-    if (again) { v.part2 = part_x; v.splits2 = u.splits; v.hi2 = su; }
+    PartsDesc p{};
+    p.g = w.g;
+    if (again) { p.part2 = part_x; p.splits2 = u.splits; p.out2 = su; }
     u.Z = dY; u.ldz = lddy; u.width = a->d_out; u.lam = a->lambda2; u.back = 1; u.factor = 1.0f;
     u.part = part_y; u.splits = rank_splits(u.g.tile_room, a->d_out, a->R);
     if ((rc = launch_rank_sums(u, st))) return rc;
-    v.part = part_y; v.splits = u.splits; v.hi = gradients ? du : nullptr;
-    v.out = dX; v.ldo = lddx; v.width = a->d_in; v.lam = a->lambda1; v.back = 1; v.factor = 1.0f / a->lambda1;
-    if ((rc = launch_spread(v, st))) return rc;
+    SpreadDesc v{};
+    v.g = w.g; v.part = part_y; v.splits = u.splits;
+    if (gradients || parts_pay(T, a->R)) {
+        p.part = part_y; p.splits = u.splits; p.out = du;
+        if ((rc = launch_rank_parts(p, st))) return rc;
+        v.u = du;
+    }
+    if (dX) {
+        v.out = dX; v.ldo = lddx; v.width = a->d_in; v.lam = a->lambda1; v.back = 1; v.factor = 1.0f / a->lambda1;
+        if ((rc = launch_spread(v, st))) return rc;
+    }
     if (!gradients) return QBLORA_OK;
     w.X = X; w.ldx = ldx; w.dY = dY; w.lddy = lddy; w.su = saved ? saved : su; w.du = du;
     w.part = reinterpret_cast<float*>(at + s.part_x + s.part_y + s.su + s.du);
