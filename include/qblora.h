@@ -706,7 +706,7 @@ int qblora_grad_norm(const qblora_adamw_list* list, double max_norm, float* out,
  *   lr      device_lr (may be NULL): fp32 on the device, likewise
  *   clip    device, the two numbers of qblora_grad_norm, of which the second is f, or NULL: f = 1.  Where f is not finite
  *           nothing is changed: a step with a broken gradient is left out.
- * 0 <= beta < 1, eps > 0, lr finite.
+ * 0 <= beta < 1, eps >= 1e-15, lr finite.
  */
 typedef struct qblora_adamw {
     double lr;

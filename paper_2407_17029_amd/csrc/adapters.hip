@@ -374,16 +374,22 @@ __global__ __launch_bounds__(kRankThreads) void k_rank_sums(RankDesc d) {
 // The results of a step are stored behind the next barrier, before the next copies are issued: the newest operations a wave waits
 // around are then its copies alone, whose number it knows.
 constexpr int kSpreadThreads = 256;
-// Rows of W for a step; half as many for inner ranks above 256, whose rows are long
-template <int LAM, int KS>
-__host__ __device__ constexpr int spread_rows() { return KS <= 8 ? (LAM == 1 ? 64 : 128 / LAM) : LAM == 1 ? 32 : LAM == 8 ? 16 : 64 / LAM; }
-template <int LAM, int KS>
-__host__ __device__ constexpr int spread_out_bytes() { return 2 * LAM * spread_rows<LAM, KS>(); }     // of a token, for a step
-template <int LAM, int KS>
-__host__ __device__ constexpr int spread_w_copies(int R) { return (R * (spread_rows<LAM, KS>() / 8) + kSpreadThreads - 1) / kSpreadThreads; }
-template <int LAM, int KS>
+// Rows of W for a step of a tile of up to ROOM tokens; half as many where the inner rank is so large that the ring would leave room for
+// one workgroup a CU only
+template <int LAM, int KS, int ROOM>
+__host__ __device__ constexpr int spread_rows() {
+    return (ROOM == 16 ? KS < 8 : KS <= 8) ? (LAM == 1 ? 64 : 128 / LAM) : LAM == 1 ? 32 : LAM == 8 ? 16 : 64 / LAM;
+}
+template <int LAM, int KS, int ROOM>
+__host__ __device__ constexpr int spread_out_bytes() { return 2 * LAM * spread_rows<LAM, KS, ROOM>(); }     // of a token, for a step
+template <int LAM, int KS, int ROOM>
+__host__ __device__ constexpr int spread_w_copies(int R) { return (R * (spread_rows<LAM, KS, ROOM>() / 8) + kSpreadThreads - 1) / kSpreadThreads; }
+// Bytes of a stage that hold outputs of up to ROOM tokens: a copy of each wave at least
+template <int LAM, int KS, int ROOM>
+__host__ __device__ constexpr int spread_out_room() { return ROOM * spread_out_bytes<LAM, KS, ROOM>() < 4096 ? 4096 : ROOM * spread_out_bytes<LAM, KS, ROOM>(); }
+template <int LAM, int KS, int ROOM>
 __host__ __device__ constexpr int spread_stage_bytes(int R) {
-    return kTileTokens * spread_out_bytes<LAM, KS>() + spread_w_copies<LAM, KS>(R) * kSpreadThreads * 16;
+    return spread_out_room<LAM, KS, ROOM>() + spread_w_copies<LAM, KS, ROOM>(R) * kSpreadThreads * 16;
 }
 // U of a tile in LDS, where the workgroup adds up the slices
 __host__ __device__ constexpr int spread_u_bytes(int tokens, int R) { return (tokens < kTileTokens ? tokens : kTileTokens) * 4 * R; }
@@ -437,29 +443,27 @@ __device__ __forceinline__ void add_outputs(uint4* o, const unsigned char* from,
     }
 }
 
-template <int LAM, bool BACK, int KS>
-__global__ __launch_bounds__(kSpreadThreads) void k_spread(SpreadDesc d, int rows, int stages) {       // rows: outputs / lam of a workgroup
-    extern __shared__ __align__(16) unsigned char smem[];
-    constexpr int kRows = spread_rows<LAM, KS>(), kOutBytes = spread_out_bytes<LAM, KS>(), kOutChunks = kOutBytes / 16;
+// Rows j0 .. j1 - 1 of W for a tile of at most ROOM tokens; `rows_u`: LDS behind the ring
+template <int LAM, bool BACK, int KS, int ROOM>
+__device__ void spread_tile(const SpreadDesc& d, const Tile& tile, int j0, int j1, int stages, unsigned char* smem, unsigned char* rows_u) {
+    constexpr int kRows = spread_rows<LAM, KS, ROOM>(), kOutBytes = spread_out_bytes<LAM, KS, ROOM>(), kOutChunks = kOutBytes / 16;
     constexpr int kBlocks = kRows / 16;                                        // of 16 rows of W, for a step
-    constexpr int kMost = spread_w_copies<LAM, KS>(32 * KS);
-    Tile tile;
-    if (!read_tile(d.g, blockIdx.x, &tile)) return;
-    const int J = d.width / LAM, j0 = blockIdx.y * rows, j1 = min(j0 + rows, J);
-    if (j0 >= j1) return;
+    constexpr int kMost = spread_w_copies<LAM, KS, ROOM>(32 * KS);
+    const int J = d.width / LAM;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4, s = lane & 15;
     const int R = tile.R;
     const int64_t slice = (int64_t)d.g.T * d.g.R;
     // token blocks: 1, 2 or 4 of them side by side, the other waves take other rows of W
-    const int tbs = tile.tokens <= 16 ? 1 : tile.tokens <= 32 ? 2 : 4;
+    const int tbs = ROOM == 16 || tile.tokens <= 16 ? 1 : tile.tokens <= 32 ? 2 : 4;
     // outputs: a copy is 1 KB of neighbouring tokens' 128 (64) outputs; what lies behind the row's end fetches its last chunk
     constexpr int kTokensACopy = 1024 / kOutBytes;
+    constexpr int kOutCopies = ROOM / (4 * kTokensACopy) > 0 ? ROOM / (4 * kTokensACopy) : 1;
     const int o_copies = max(1, tbs * 16 / (4 * kTokensACopy));
-    const unsigned char* o_from[16 / kTokensACopy];
-    int o_col[16 / kTokensACopy];
+    const unsigned char* o_from[kOutCopies];
+    int o_col[kOutCopies];
     const int o_last = 2 * d.width - 16;
 #pragma unroll
-    for (int i = 0; i < 16 / kTokensACopy; ++i) {
+    for (int i = 0; i < kOutCopies; ++i) {
         const int l = kTokensACopy * (wave + 4 * i) + lane / kOutChunks;
         const int token = min(max(d.g.order[tile.begin + min(l, tile.tokens - 1)], 0), d.g.T - 1);
         o_from[i] = reinterpret_cast<const unsigned char*>(d.out + (int64_t)token * d.ldo);
@@ -467,7 +471,7 @@ __global__ __launch_bounds__(kSpreadThreads) void k_spread(SpreadDesc d, int row
     }
     // W: chunks of 16 bytes, `per` of them a row; places behind the last chunk, or behind the last row of outputs, fetch the first
     const int per = BACK ? R / 8 : kRows / 8, chunks = R * (kRows / 8);
-    const int w_copies = spread_w_copies<LAM, KS>(R);
+    const int w_copies = spread_w_copies<LAM, KS, ROOM>(R);
     const unsigned char* const w = reinterpret_cast<const unsigned char*>(BACK ? tile.entry->A : tile.entry->B);
     uint32_t w_from[kMost];
     int w_row[kMost];                                                          // first of the step's outputs / lam that the chunk holds
@@ -479,12 +483,13 @@ __global__ __launch_bounds__(kSpreadThreads) void k_spread(SpreadDesc d, int row
         w_from[i] = (uint32_t)row * (uint32_t)((BACK ? R : J) * 2) + 16 * col;
         w_row[i] = BACK ? row : 8 * col;
     }
-    const int stage_bytes = kTileTokens * kOutBytes + w_copies * kSpreadThreads * 16;
+    constexpr int kWAt = spread_out_room<LAM, KS, ROOM>();
+    const int stage_bytes = kWAt + w_copies * kSpreadThreads * 16;
     const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(smem)) + wave * 1024;
     auto issue = [&](int j, int buf) __attribute__((always_inline)) {
         const uint32_t to = lds + buf * stage_bytes;
 #pragma unroll
-        for (int i = 0; i < 16 / kTokensACopy; ++i) {
+        for (int i = 0; i < kOutCopies; ++i) {
             if (i >= o_copies) break;
             copy16_to_lds(o_from[i] + min(o_col[i] + 2 * LAM * (j - j0), o_last), to + i * 4096);
         }
@@ -492,7 +497,7 @@ __global__ __launch_bounds__(kSpreadThreads) void k_spread(SpreadDesc d, int row
 #pragma unroll
         for (int i = 0; i < kMost; ++i) {
             if (i >= w_copies) break;
-            copy16_to_lds(j + w_row[i] < J ? at + w_from[i] : w, to + kTileTokens * kOutBytes + i * 4096);
+            copy16_to_lds(j + w_row[i] < J ? at + w_from[i] : w, to + kWAt + i * 4096);
         }
     };
     issue(j0, 0);
@@ -506,15 +511,14 @@ __global__ __launch_bounds__(kSpreadThreads) void k_spread(SpreadDesc d, int row
     bf16x8 uh[KS], ul[KS];
     const int l_real = min(l, tile.tokens - 1);
     if (!d.u) {
-        unsigned char* const us = smem + stages * spread_stage_bytes<LAM, KS>(d.g.R);
-        sum_tile(d, tile, us);
+        sum_tile(d, tile, rows_u);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             const int r = 32 * k + 8 * g;
             uint2 h0 = make_uint2(0, 0), h1 = h0, l0 = h0, l1 = h0;
             if (r < R) {
-                split_pair(*reinterpret_cast<const float4*>(us + u_at(l_real, r / 4, R)), &h0, &l0);
-                split_pair(*reinterpret_cast<const float4*>(us + u_at(l_real, r / 4 + 1, R)), &h1, &l1);
+                split_pair(*reinterpret_cast<const float4*>(rows_u + u_at(l_real, r / 4, R)), &h0, &l0);
+                split_pair(*reinterpret_cast<const float4*>(rows_u + u_at(l_real, r / 4 + 1, R)), &h1, &l1);
             }
             uh[k] = __builtin_bit_cast(bf16x8, make_uint4(h0.x, h0.y, h1.x, h1.y));
             ul[k] = __builtin_bit_cast(bf16x8, make_uint4(l0.x, l0.y, l1.x, l1.y));
@@ -537,7 +541,6 @@ __global__ __launch_bounds__(kSpreadThreads) void k_spread(SpreadDesc d, int row
     const bool behind = 32 * last + 8 * g >= R;
     // Offsets of this lane's operands in a stage.  B: the rows of 32 r lie a whole number of times 16 rows on, where the chunks are
     // moved alike, and so do four rows; a block's chunks change places with the block's number.  A: 8 chunks on, likewise.
-    constexpr int kWAt = kTileTokens * kOutBytes;
     int w_off[BACK ? 4 : 1];
     if constexpr (BACK) {
 #pragma unroll
@@ -571,12 +574,12 @@ __global__ __launch_bounds__(kSpreadThreads) void k_spread(SpreadDesc d, int row
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) {
             const int jb = jb0 + i * jb_step;
-            if (jb >= kBlocks) break;
+            if (jb >= kBlocks) continue;
             f32x4 acc{0.0f, 0.0f, 0.0f, 0.0f};
             const unsigned char* const block = BACK ? os + jb * (32 * R) : os + kWAt + (w_off[0] ^ (32 * jb));
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                if (k > last) break;
+                if (k > last) continue;
                 bf16x8 wf;
                 if constexpr (BACK) {
                     wf = *reinterpret_cast<const bf16x8*>(block + w_off[k & 3] + 256 * (k >> 2));
@@ -595,6 +598,133 @@ __global__ __launch_bounds__(kSpreadThreads) void k_spread(SpreadDesc d, int row
     }
     store();
 }
+
+template <int LAM, bool BACK, int KS>
+__global__ __launch_bounds__(kSpreadThreads) void k_spread(SpreadDesc d, int rows, int stages) {       // rows: of W, for a workgroup
+    extern __shared__ __align__(16) unsigned char smem[];
+    Tile tile;
+    if (!read_tile(d.g, blockIdx.x, &tile)) return;
+    const int j0 = blockIdx.y * rows, j1 = min(j0 + rows, d.width / LAM);
+    if (j0 >= j1) return;
+    spread_tile<LAM, BACK, KS, kTileTokens>(d, tile, j0, j1, stages, smem, smem + stages * spread_stage_bytes<LAM, KS, kTileTokens>(d.g.R));
+}
+
+// Few tokens of a batch.  Up to kFewTile of a tile, the usual thing while requests decode, are multiplied in the vector ALU: bound by the
+// stream of B, of which every row is read once, straight into registers, eight loads a thread under way at any time, the first of
+// them before U is there.  A piece is 256 rows of outputs: a thread has 8 neighbouring ones and every eighth r, and the eight
+// shares are added in LDS.  Tiles of more tokens go 16 at a time through the matrix pipe.
+constexpr int kFewTile = 4, kFewRows = 256, kFewAhead = 8;
+
+template <int LAM, int KS, int MT>
+__device__ void spread_few(const SpreadDesc& d, const Tile& tile, int j0, int j1, unsigned char* smem) {
+    constexpr int kLoads = 4 * KS, kAhead = kLoads < kFewAhead ? kLoads : kFewAhead;
+    const int t = threadIdx.x, share = t >> 5, R = tile.R, J = d.width / LAM, col = 8 * (t & 31);
+    float* const us = reinterpret_cast<float*>(smem);                          // [R][MT]
+    float* const sums = us + 32 * KS * MT;                                     // [8 shares][MT][256]
+    const qblora_bf16* const B = tile.entry->B + (int64_t)share * J;
+    // No load is conditional, as loads behind a branch are waited for together: rows behind R and outputs behind the last fetch others
+    // once more, which are not used.
+    uint4 w[kAhead];
+    auto load = [&](int i, int j) __attribute__((always_inline)) {            // row share + 8 i of the piece at j
+        w[i % kAhead] = load16(B + (int64_t)(8 * i < R ? 8 * i : 0) * J + min(j + col, J - 8));
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) load(i, j0);
+    qblora_bf16* out[MT];
+    bool real[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int token = d.g.order[tile.begin + min(m, tile.tokens - 1)];
+        real[m] = m < tile.tokens && token >= 0 && token < d.g.T;
+        out[m] = d.out + (int64_t)min(max(token, 0), d.g.T - 1) * d.ldo;
+    }
+    const int quads = R / 4;
+    const int64_t slice = (int64_t)d.g.T * d.g.R;
+    for (int i = t; i < MT * quads; i += kSpreadThreads) {
+        const int m = i / quads, r = 4 * (i % quads);
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (m < tile.tokens) v = sum_slices(d.part, d.splits, slice, (int64_t)(tile.begin + m) * d.g.R + r);
+        us[r * MT + m] = v.x; us[(r + 1) * MT + m] = v.y; us[(r + 2) * MT + m] = v.z; us[(r + 3) * MT + m] = v.w;
+    }
+    __syncthreads();
+    for (int j = j0; j < j1; j += kFewRows) {
+        const bool mine = j + t < j1;
+        const int64_t at = (int64_t)min(j + t, J - 1) * LAM;                     // the outputs of row j + t
+        qblora_bf16 was[MT][LAM];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) __builtin_memcpy(was[m], __builtin_assume_aligned(out[m] + at, 2 * LAM), 2 * LAM);
+        float acc[MT][8];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[m][e] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const uint4 v = w[i % kAhead];
+            if (i + kAhead < kLoads) load(i + kAhead, j);
+            else load(i + kAhead - kLoads, j + kFewRows);
+            if (8 * i >= R) continue;
+            const float b[8] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y), bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w)};
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const float u = us[(share + 8 * i) * MT + m];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[m][e] = __fmaf_rn(u, b[e], acc[m][e]);
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            float4* const to = reinterpret_cast<float4*>(sums + (share * MT + m) * kFewRows + col);
+            to[0] = make_float4(acc[m][0], acc[m][1], acc[m][2], acc[m][3]);
+            to[1] = make_float4(acc[m][4], acc[m][5], acc[m][6], acc[m][7]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            if (!mine || !real[m]) continue;
+            float v = 0.0f;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v += sums[(q * MT + m) * kFewRows + t];
+            v *= d.factor;
+            qblora_bf16* const o = out[m] + at;
+            if constexpr (LAM == 1) {
+                o[0] = (qblora_bf16)pack_bf16(bf16_bits_to_float(was[m][0]) + v, 0.0f);
+            } else {
+                uint32_t pair[LAM / 2];
+#pragma unroll
+                for (int e = 0; e < LAM / 2; ++e) pair[e] = pack_bf16(bf16_bits_to_float(was[m][2 * e]) + v, bf16_bits_to_float(was[m][2 * e + 1]) + v);
+                __builtin_memcpy(__builtin_assume_aligned(o, 2 * LAM), pair, 2 * LAM);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+template <int LAM, int KS>
+__device__ __forceinline__ void spread_few(const SpreadDesc& d, const Tile& tile, int j0, int j1, unsigned char* smem) {
+    if (tile.tokens == 1) spread_few<LAM, KS, 1>(d, tile, j0, j1, smem);
+    else if (tile.tokens == 2) spread_few<LAM, KS, 2>(d, tile, j0, j1, smem);
+    else spread_few<LAM, KS, kFewTile>(d, tile, j0, j1, smem);
+}
+
+template <int LAM, int KS>
+__global__ __launch_bounds__(kSpreadThreads, 2) void k_spread_few(SpreadDesc d, int rows, int stages) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    Tile whole;
+    if (!read_tile(d.g, blockIdx.y, &whole)) return;
+    const int j0 = blockIdx.x * rows, j1 = min(j0 + rows, d.width / LAM);
+    if (j0 >= j1) return;
+    for (int from = 0; from < whole.tokens; from += 16) {
+        const Tile tile{whole.begin + from, min(whole.tokens - from, 16), whole.R, whole.entry};
+        if (from) __syncthreads();
+        if (tile.tokens > kFewTile) spread_tile<LAM, false, KS, 16>(d, tile, j0, j1, stages, smem, smem + stages * spread_stage_bytes<LAM, KS, 16>(d.g.R));
+        else if (KS > 1 && tile.R <= 32) spread_few<LAM, 1>(d, tile, j0, j1, smem);
+        else if (KS > 2 && tile.R <= 64) spread_few<LAM, 2>(d, tile, j0, j1, smem);
+        else if (KS > 4 && tile.R <= 128) spread_few<LAM, 4>(d, tile, j0, j1, smem);
+        else spread_few<LAM, KS>(d, tile, j0, j1, smem);
+    }
+}
+constexpr int few_bytes(int KS, int MT) { return 4 * MT * (32 * KS + 8 * kFewRows); }
 
 // U as three bf16 parts, 24 significant bits: the sums of the slices of one or two arrays
 __global__ __launch_bounds__(256) void k_rank_parts(PartsDesc d) {
@@ -634,22 +764,44 @@ int rank_sums(const RankDesc& d, hipStream_t st) {
     return launch_status();
 }
 
+// Stages of a ring beside `more` bytes of LDS: three where two workgroups still fit a CU, else two if these do, else three if they fit at all
+int ring_stages(int stage, int more) {
+    const int half = 80 * 1024;
+    return 3 * stage + more <= half ? 3 : 2 * stage + more <= half ? 2 : 3 * stage + more <= 2 * half ? 3 : 2;
+}
+
 template <int LAM, bool BACK, int KS>
 int spread(const SpreadDesc& d, hipStream_t st) {
     const int rc = allow_lds(k_spread<LAM, BACK, KS>);
     if (rc) return rc;
-    constexpr int kRows = spread_rows<LAM, KS>();
+    constexpr int kRows = spread_rows<LAM, KS, kTileTokens>();
     const int J = d.width / LAM, steps = (J + kRows - 1) / kRows;
     const int parts = std::min(steps, std::max(1, 1024 / d.g.tile_room));
     const int rows = (steps + parts - 1) / parts * kRows;
-    // three stages in the ring where two workgroups still fit a CU, else two if these do, else three if they fit at all
-    const int stage = spread_stage_bytes<LAM, KS>(d.g.R), more = d.u ? 0 : spread_u_bytes(d.g.T, d.g.R), half = 80 * 1024;
-    const int stages = 3 * stage + more <= half ? 3 : 2 * stage + more <= half ? 2 : 3 * stage + more <= 2 * half ? 3 : 2;
+    const int more = d.u ? 0 : spread_u_bytes(std::min(d.g.T, kTileTokens), d.g.R), stage = spread_stage_bytes<LAM, KS, kTileTokens>(d.g.R);
+    const int stages = ring_stages(stage, more);
     k_spread<LAM, BACK, KS><<<dim3(d.g.tile_room, (J + rows - 1) / rows), kSpreadThreads, stages * stage + more, st>>>(d, rows, stages);
+    return launch_status();
+}
+
+template <int LAM, int KS>
+int spread_few_tokens(const SpreadDesc& d, hipStream_t st) {
+    const int rc = allow_lds(k_spread_few<LAM, KS>);
+    if (rc) return rc;
+    const int J = d.width / LAM, pieces = (J + kFewRows - 1) / kFewRows;
+    // one round of workgroups, two a CU, while that gives each few pieces (40 adapters, 860 pieces: 512 workgroups 12.6 us, 2048 16.2); else
+    // more and smaller ones, which even out at the end (100 adapters, 4500 pieces: 1024 125 us, 2048 119)
+    const int parts = std::min(pieces, std::max(1, (pieces * d.g.tile_room <= 2048 ? 512 : 2048) / d.g.tile_room));
+    const int rows = (pieces + parts - 1) / parts * kFewRows;
+    const int more = spread_u_bytes(16, d.g.R), stage = spread_stage_bytes<LAM, KS, 16>(d.g.R), stages = ring_stages(stage, more);
+    const int lds = std::max(d.g.T > kFewTile ? stages * stage + more : 0, few_bytes(KS, d.g.T >= 3 ? 4 : d.g.T));
+    k_spread_few<LAM, KS><<<dim3((J + rows - 1) / rows, d.g.tile_room), kSpreadThreads, lds, st>>>(d, rows, stages);
     return launch_status();
 }
 template <int LAM, bool BACK>
 int spread_by_rank(const SpreadDesc& d, hipStream_t st) {
+    if constexpr (!BACK)
+        if (!d.u) return d.g.R <= 64 ? spread_few_tokens<LAM, 2>(d, st) : d.g.R <= 128 ? spread_few_tokens<LAM, 4>(d, st) : spread_few_tokens<LAM, 8>(d, st);
     if (d.g.R <= 64) return spread<LAM, BACK, 2>(d, st);
     if (d.g.R <= 128) return spread<LAM, BACK, 4>(d, st);
     if (d.g.R <= 256) return spread<LAM, BACK, 8>(d, st);

@@ -303,7 +303,7 @@ int qblora_adamw_step(const qblora_adamw_list* list, const qblora_adamw* how, co
     if (!(how->beta1 >= 0.0 && how->beta1 < 1.0) || !(how->beta2 >= 0.0 && how->beta2 < 1.0) || !(how->eps > 0.0) ||
         !std::isfinite(how->eps) || (!how->device_lr && !std::isfinite(how->lr)) || (!how->device_step && how->step < 1))
         return QBLORA_ERR_SHAPE;
-    if ((float)how->beta1 == 1.0f || (float)how->beta2 == 1.0f || (float)how->eps == 0.0f) return QBLORA_ERR_SHAPE;
+    if ((float)how->beta1 == 1.0f || (float)how->beta2 == 1.0f || (float)how->eps < 1e-15f) return QBLORA_ERR_SHAPE;
     if (list->units == 0) return QBLORA_OK;
     StepDesc d{};
     d.entries = entries_of(list); d.units = units_of(list); d.n_units = list->units; d.bits = list->bits;

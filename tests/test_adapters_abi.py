@@ -192,7 +192,7 @@ def test_step(qb):
         ({}, 0), (dict(list_=None), NULL), (dict(how=None), NULL), (dict(list_=qb.CAdamWList(0, 7, 0, None)), UNSUPPORTED),
         (dict(how=how(beta1=1.0)), SHAPE), (dict(how=how(beta1=-0.1)), SHAPE), (dict(how=how(beta2=math.nan)), SHAPE),
         (dict(how=how(beta2=1.0)), SHAPE), (dict(how=how(beta2=1.0 - 1e-12)), SHAPE), (dict(how=how(eps=0.0)), SHAPE),
-        (dict(how=how(eps=1e-60)), SHAPE), (dict(how=how(eps=math.inf)), SHAPE), (dict(how=how(lr=math.nan)), SHAPE),
+        (dict(how=how(eps=1e-60)), SHAPE), (dict(how=how(eps=9e-16)), SHAPE), (dict(how=how(eps=math.inf)), SHAPE), (dict(how=how(lr=math.nan)), SHAPE),
         (dict(how=how(step=0)), SHAPE), (dict(how=how(step=0, device_step=A)), 0), (dict(how=how(lr=math.nan, device_lr=A)), 0)])
 
 
