@@ -373,7 +373,8 @@ __global__ __launch_bounds__(kRankThreads) void k_rank_sums(RankDesc d) {
 // product's rows are outputs / lam, its columns tokens, so that a lane has 4 neighbouring rows of one token, 4 lam outputs.
 // The results of a step are stored behind the next barrier, before the next copies are issued: the newest operations a wave waits
 // around are then its copies alone, whose number it knows.
-constexpr int kSpreadThreads = 256;
+constexpr int kWideWaves = 8, kFewWaves = 4;                                  // of a workgroup, for tiles of up to 64 tokens and of up to 16
+constexpr int kFewThreads = 64 * kFewWaves;
 // Rows of W for a step of a tile of up to ROOM tokens; half as many where the inner rank is so large that the ring would leave room for
 // one workgroup a CU only
 template <int LAM, int KS, int ROOM>
@@ -382,14 +383,21 @@ __host__ __device__ constexpr int spread_rows() {
 }
 template <int LAM, int KS, int ROOM>
 __host__ __device__ constexpr int spread_out_bytes() { return 2 * LAM * spread_rows<LAM, KS, ROOM>(); }     // of a token, for a step
+// Copies of W that a wave makes for a step
 template <int LAM, int KS, int ROOM>
-__host__ __device__ constexpr int spread_w_copies(int R) { return (R * (spread_rows<LAM, KS, ROOM>() / 8) + kSpreadThreads - 1) / kSpreadThreads; }
+__host__ __device__ constexpr int spread_w_copies(int R) {
+    constexpr int threads = 64 * (ROOM == 16 ? kFewWaves : kWideWaves);
+    return (R * (spread_rows<LAM, KS, ROOM>() / 8) + threads - 1) / threads;
+}
 // Bytes of a stage that hold outputs of up to ROOM tokens: a copy of each wave at least
 template <int LAM, int KS, int ROOM>
-__host__ __device__ constexpr int spread_out_room() { return ROOM * spread_out_bytes<LAM, KS, ROOM>() < 4096 ? 4096 : ROOM * spread_out_bytes<LAM, KS, ROOM>(); }
+__host__ __device__ constexpr int spread_out_room() {
+    constexpr int least = 1024 * (ROOM == 16 ? kFewWaves : kWideWaves), bytes = ROOM * spread_out_bytes<LAM, KS, ROOM>();
+    return bytes < least ? least : bytes;
+}
 template <int LAM, int KS, int ROOM>
 __host__ __device__ constexpr int spread_stage_bytes(int R) {
-    return spread_out_room<LAM, KS, ROOM>() + spread_w_copies<LAM, KS, ROOM>(R) * kSpreadThreads * 16;
+    return spread_out_room<LAM, KS, ROOM>() + spread_w_copies<LAM, KS, ROOM>(R) * 1024 * (ROOM == 16 ? kFewWaves : kWideWaves);
 }
 // U of a tile in LDS, where the workgroup adds up the slices
 __host__ __device__ constexpr int spread_u_bytes(int tokens, int R) { return (tokens < kTileTokens ? tokens : kTileTokens) * 4 * R; }
@@ -416,10 +424,10 @@ __device__ __forceinline__ float4 sum_slices(const float* part, int splits, int6
 
 // The U of a tile in LDS, 4 R bytes a token; where R is a multiple of 32 the 16-byte chunks change places by the token
 __device__ __forceinline__ int u_at(int l, int quad, int R) { return 4 * R * l + 16 * (quad ^ (R % 32 == 0 ? l & 7 : 0)); }
-__device__ __forceinline__ void sum_tile(const SpreadDesc& d, const Tile& tile, unsigned char* us) {
+__device__ __forceinline__ void sum_tile(const SpreadDesc& d, const Tile& tile, unsigned char* us, int threads) {
     const int quads = tile.R / 4;
     const int64_t slice = (int64_t)d.g.T * d.g.R;
-    for (int i = threadIdx.x; i < tile.tokens * quads; i += kSpreadThreads)
+    for (int i = threadIdx.x; i < tile.tokens * quads; i += threads)
         *reinterpret_cast<float4*>(us + u_at(i / quads, i % quads, tile.R)) =
             sum_slices(d.part, d.splits, slice, (int64_t)(tile.begin + i / quads) * d.g.R + 4 * (i % quads));
     __syncthreads();
@@ -448,7 +456,7 @@ template <int LAM, bool BACK, int KS, int ROOM>
 __device__ void spread_tile(const SpreadDesc& d, const Tile& tile, int j0, int j1, int stages, unsigned char* smem, unsigned char* rows_u) {
     constexpr int kRows = spread_rows<LAM, KS, ROOM>(), kOutBytes = spread_out_bytes<LAM, KS, ROOM>(), kOutChunks = kOutBytes / 16;
     constexpr int kBlocks = kRows / 16;                                        // of 16 rows of W, for a step
-    constexpr int kMost = spread_w_copies<LAM, KS, ROOM>(32 * KS);
+    constexpr int kMost = spread_w_copies<LAM, KS, ROOM>(32 * KS), kWaves = ROOM == 16 ? kFewWaves : kWideWaves;
     const int J = d.width / LAM;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4, s = lane & 15;
     const int R = tile.R;
@@ -457,14 +465,14 @@ __device__ void spread_tile(const SpreadDesc& d, const Tile& tile, int j0, int j
     const int tbs = ROOM == 16 || tile.tokens <= 16 ? 1 : tile.tokens <= 32 ? 2 : 4;
     // outputs: a copy is 1 KB of neighbouring tokens' 128 (64) outputs; what lies behind the row's end fetches its last chunk
     constexpr int kTokensACopy = 1024 / kOutBytes;
-    constexpr int kOutCopies = ROOM / (4 * kTokensACopy) > 0 ? ROOM / (4 * kTokensACopy) : 1;
-    const int o_copies = max(1, tbs * 16 / (4 * kTokensACopy));
+    constexpr int kOutCopies = ROOM / (kWaves * kTokensACopy) > 0 ? ROOM / (kWaves * kTokensACopy) : 1;
+    const int o_copies = max(1, tbs * 16 / (kWaves * kTokensACopy));
     const unsigned char* o_from[kOutCopies];
     int o_col[kOutCopies];
     const int o_last = 2 * d.width - 16;
 #pragma unroll
     for (int i = 0; i < kOutCopies; ++i) {
-        const int l = kTokensACopy * (wave + 4 * i) + lane / kOutChunks;
+        const int l = kTokensACopy * (wave + kWaves * i) + lane / kOutChunks;
         const int token = min(max(d.g.order[tile.begin + min(l, tile.tokens - 1)], 0), d.g.T - 1);
         o_from[i] = reinterpret_cast<const unsigned char*>(d.out + (int64_t)token * d.ldo);
         o_col[i] = 2 * LAM * j0 + 16 * (lane % kOutChunks ^ (l & (kOutChunks - 1)));
@@ -477,33 +485,33 @@ __device__ void spread_tile(const SpreadDesc& d, const Tile& tile, int j0, int j
     int w_row[kMost];                                                          // first of the step's outputs / lam that the chunk holds
 #pragma unroll
     for (int i = 0; i < kMost; ++i) {
-        int c = (i * 4 + wave) * 64 + lane;
+        int c = (i * kWaves + wave) * 64 + lane;
         if (c >= chunks) c = 0;
         const int row = c / per, col = c % per ^ (BACK ? row_swap(row, per) : column_swap<8>(row, per));
         w_from[i] = (uint32_t)row * (uint32_t)((BACK ? R : J) * 2) + 16 * col;
         w_row[i] = BACK ? row : 8 * col;
     }
     constexpr int kWAt = spread_out_room<LAM, KS, ROOM>();
-    const int stage_bytes = kWAt + w_copies * kSpreadThreads * 16;
+    const int stage_bytes = kWAt + w_copies * kWaves * 1024;
     const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(smem)) + wave * 1024;
     auto issue = [&](int j, int buf) __attribute__((always_inline)) {
         const uint32_t to = lds + buf * stage_bytes;
 #pragma unroll
         for (int i = 0; i < kOutCopies; ++i) {
             if (i >= o_copies) break;
-            copy16_to_lds(o_from[i] + min(o_col[i] + 2 * LAM * (j - j0), o_last), to + i * 4096);
+            copy16_to_lds(o_from[i] + min(o_col[i] + 2 * LAM * (j - j0), o_last), to + i * kWaves * 1024);
         }
         const unsigned char* const at = w + (BACK ? (int64_t)j * R * 2 : (int64_t)j * 2);
 #pragma unroll
         for (int i = 0; i < kMost; ++i) {
             if (i >= w_copies) break;
-            copy16_to_lds(j + w_row[i] < J ? at + w_from[i] : w, to + kWAt + i * 4096);
+            copy16_to_lds(j + w_row[i] < J ? at + w_from[i] : w, to + kWAt + i * kWaves * 1024);
         }
     };
     issue(j0, 0);
     if (stages == 3 && j0 + kRows < j1) issue(j0 + kRows, 1);
 
-    const int tb = wave % tbs, jb0 = wave / tbs, jb_step = 4 / tbs;
+    const int tb = wave % tbs, jb0 = wave / tbs, jb_step = kWaves / tbs;
     const int l = 16 * tb + s;
     const int token = l < tile.tokens ? d.g.order[tile.begin + l] : -1;
     const bool real = token >= 0 && token < d.g.T;
@@ -511,7 +519,7 @@ __device__ void spread_tile(const SpreadDesc& d, const Tile& tile, int j0, int j
     bf16x8 uh[KS], ul[KS];
     const int l_real = min(l, tile.tokens - 1);
     if (!d.u) {
-        sum_tile(d, tile, rows_u);
+        sum_tile(d, tile, rows_u, 64 * kWaves);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             const int r = 32 * k + 8 * g;
@@ -575,7 +583,7 @@ __device__ void spread_tile(const SpreadDesc& d, const Tile& tile, int j0, int j
         for (int i = 0; i < kBlocks; ++i) {
             const int jb = jb0 + i * jb_step;
             if (jb >= kBlocks) continue;
-            f32x4 acc{0.0f, 0.0f, 0.0f, 0.0f};
+            f32x4 acc{0.0f, 0.0f, 0.0f, 0.0f}, acc_lo = acc;                        // two chains of products
             const unsigned char* const block = BACK ? os + jb * (32 * R) : os + kWAt + (w_off[0] ^ (32 * jb));
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
@@ -589,8 +597,9 @@ __device__ void spread_tile(const SpreadDesc& d, const Tile& tile, int j0, int j
                 }
                 if (k == last && behind) wf = __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0));    // U is 0 there, W may be anything
                 acc = mma(wf, uh[k], acc);
-                acc = mma(wf, ul[k], acc);
+                acc_lo = mma(wf, ul[k], acc_lo);
             }
+            acc += acc_lo;
             result_at[i] = j + 16 * jb + 4 * g;
             add_outputs<LAM>(result[i], os + l * kOutBytes, acc, d.factor, 4 * jb + g, l & (kOutChunks - 1));
         }
@@ -600,7 +609,7 @@ __device__ void spread_tile(const SpreadDesc& d, const Tile& tile, int j0, int j
 }
 
 template <int LAM, bool BACK, int KS>
-__global__ __launch_bounds__(kSpreadThreads) void k_spread(SpreadDesc d, int rows, int stages) {       // rows: of W, for a workgroup
+__global__ __launch_bounds__(64 * kWideWaves) void k_spread(SpreadDesc d, int rows, int stages) {       // rows: of W, for a workgroup
     extern __shared__ __align__(16) unsigned char smem[];
     Tile tile;
     if (!read_tile(d.g, blockIdx.x, &tile)) return;
@@ -640,7 +649,7 @@ __device__ void spread_few(const SpreadDesc& d, const Tile& tile, int j0, int j1
     }
     const int quads = R / 4;
     const int64_t slice = (int64_t)d.g.T * d.g.R;
-    for (int i = t; i < MT * quads; i += kSpreadThreads) {
+    for (int i = t; i < MT * quads; i += kFewThreads) {
         const int m = i / quads, r = 4 * (i % quads);
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (m < tile.tokens) v = sum_slices(d.part, d.splits, slice, (int64_t)(tile.begin + m) * d.g.R + r);
@@ -708,7 +717,7 @@ __device__ __forceinline__ void spread_few(const SpreadDesc& d, const Tile& tile
 }
 
 template <int LAM, int KS>
-__global__ __launch_bounds__(kSpreadThreads, 2) void k_spread_few(SpreadDesc d, int rows, int stages) {
+__global__ __launch_bounds__(kFewThreads, 2) void k_spread_few(SpreadDesc d, int rows, int stages) {
     extern __shared__ __align__(16) unsigned char smem[];
     Tile whole;
     if (!read_tile(d.g, blockIdx.y, &whole)) return;
@@ -780,7 +789,7 @@ int spread(const SpreadDesc& d, hipStream_t st) {
     const int rows = (steps + parts - 1) / parts * kRows;
     const int more = d.u ? 0 : spread_u_bytes(std::min(d.g.T, kTileTokens), d.g.R), stage = spread_stage_bytes<LAM, KS, kTileTokens>(d.g.R);
     const int stages = ring_stages(stage, more);
-    k_spread<LAM, BACK, KS><<<dim3(d.g.tile_room, (J + rows - 1) / rows), kSpreadThreads, stages * stage + more, st>>>(d, rows, stages);
+    k_spread<LAM, BACK, KS><<<dim3(d.g.tile_room, (J + rows - 1) / rows), 64 * kWideWaves, stages * stage + more, st>>>(d, rows, stages);
     return launch_status();
 }
 
@@ -795,7 +804,7 @@ int spread_few_tokens(const SpreadDesc& d, hipStream_t st) {
     const int rows = (pieces + parts - 1) / parts * kFewRows;
     const int more = spread_u_bytes(16, d.g.R), stage = spread_stage_bytes<LAM, KS, 16>(d.g.R), stages = ring_stages(stage, more);
     const int lds = std::max(d.g.T > kFewTile ? stages * stage + more : 0, few_bytes(KS, d.g.T >= 3 ? 4 : d.g.T));
-    k_spread_few<LAM, KS><<<dim3((J + rows - 1) / rows, d.g.tile_room), kSpreadThreads, lds, st>>>(d, rows, stages);
+    k_spread_few<LAM, KS><<<dim3((J + rows - 1) / rows, d.g.tile_room), kFewThreads, lds, st>>>(d, rows, stages);
     return launch_status();
 }
 template <int LAM, bool BACK>
