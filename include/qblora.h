@@ -573,7 +573,7 @@ size_t qblora_adapter_table_bytes(int32_t count);
  * Writes entries first .. first + n - 1 of the table from `list` (host array).  An entry keeps the addresses of its A and B
  * (16-byte aligned, as they are for qblora_linear_fwd otherwise), which stay the caller's: what they hold when a later call
  * runs is what that call uses, so that an optimizer may step them in place.  An entry without adapter (A or B NULL, or R = 0) adds
- * nothing.
+ * nothing.  Every entry has to be written before a call reads the table.
  *   dA, dB   host arrays of n pointers (both or neither NULL): where qblora_adapters_bwd writes that entry's gradients, fp32
  *            [d_in/lambda1, R] and [R, d_out/lambda2], 16-byte aligned; a NULL pointer, or no array: it writes none.  No two
  *            entries may share them.
@@ -601,7 +601,7 @@ int qblora_adapter_groups(const int32_t* starts, const int32_t* which, int32_t n
  *   Y[t] = bf16( Y[t] + E( V ) ),  V = (s_a U) B_a,  U = C(X[t]) A_a;
  * sums in fp32, s_a U with 16 significant bits at least.  Rows of tokens without adapter stay as they are.
  *   X      bf16: token t at X + t*ldx; 16-byte aligned, ldx % 8 == 0, ldx >= d_in
- *   Y      bf16, likewise (ldy, d_out)
+ *   Y      bf16, likewise (ldy, d_out); no part of X
  *   first, order, tiles   as qblora_adapter_groups wrote them for this batch and this count.  A token must not be listed twice.
  *   saved  qblora_adapters_saved_bytes(), 16-byte aligned, or NULL: s U of every listed token, which the backward pass needs
  *   workspace   at least qblora_adapters_workspace_bytes(), 256-byte aligned; the size serves both directions
@@ -617,7 +617,7 @@ int qblora_adapters_fwd(const qblora_adapters* adapters, const int32_t* first, c
  * Its backward pass: with dV[t] = s_a * (sums of lambda2 adjacent features of dY[t]) and dU = dV B_a^T,
  *   dX[t] = bf16( dX[t] + (1/lambda1) * E1( dU A_a^T ) ), E1 repeating each value lambda1 times,
  *   dA_a = sum over a's tokens of C(X[t])^T dU,   dB_a = sum over a's tokens of U^T dV.
- *   dX      bf16, likewise (lddx, d_in): what the frozen weight's backward call wrote; NULL: not wanted
+ *   dX      bf16, likewise (lddx, d_in): what the frozen weight's backward call wrote, no part of X or dY; NULL: not wanted
  *   gradients   0: none (X and saved are ignored).  Else dA and dB of the table's entries that have a place for them are
  *           overwritten, with zeros where the batch has no token of an adapter; sums in a fixed order, a repeated call repeats
  *           its bits

@@ -5,7 +5,7 @@
 namespace qblora {
 
 // A pointer that was read from memory, as one to device memory: through a pointer that might lie anywhere the compiler makes accesses
-// that count as LDS accesses too, and waits for all of them at each one's first use (256 tokens on 100 adapters 473 us instead of 1xx).
+// that count as LDS accesses too, and waits for all of them at each one's first use (256 single tokens on 100 adapters, the outputs' part: 473 us instead of 186).
 template <typename T>
 __device__ __forceinline__ __attribute__((address_space(1))) T* in_memory(T* p) { return (__attribute__((address_space(1))) T*)p; }
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

@@ -159,7 +159,7 @@ int qblora_adapters_fwd(const qblora_adapters* a, const int32_t* first, const in
     if (rc || T == 0) return rc;
     if ((rc = check_rows(X, ldx, a->d_in))) return rc;
     if ((rc = check_rows(Y, ldy, a->d_out))) return rc;
-    if (!aligned(saved, 16)) return QBLORA_ERR_SHAPE;
+    if (!aligned(saved, 16) || X == Y) return QBLORA_ERR_SHAPE;
     const Space s = space_of(a, T);
     if (!workspace || workspace_bytes < s.all || !aligned(workspace, 256)) return QBLORA_ERR_WORKSPACE;
     RankDesc u{};
@@ -197,7 +197,7 @@ int qblora_adapters_bwd(const qblora_adapters* a, const int32_t* first, const in
     if (gradients && (rc = check_rows(X, ldx, a->d_in))) return rc;
     if ((rc = check_rows(dY, lddy, a->d_out))) return rc;
     if (dX && (rc = check_rows(dX, lddx, a->d_in))) return rc;
-    if (!aligned(saved, 16)) return QBLORA_ERR_SHAPE;
+    if (!aligned(saved, 16) || dX == dY || (gradients && dX == X)) return QBLORA_ERR_SHAPE;
     const Space s = space_of(a, T);
     if (!workspace || workspace_bytes < s.all || !aligned(workspace, 256)) return QBLORA_ERR_WORKSPACE;
     unsigned char* at = reinterpret_cast<unsigned char*>(workspace);

@@ -161,9 +161,13 @@ def wrap(x):
 
 def random_bits(n, tensor, step, seed):
     """32 bits of each of n elements."""
+    return random_bits_at(np.arange(n), tensor, step, seed)
+
+
+def random_bits_at(elements, tensor, step, seed):
     u = np.uint64
     with np.errstate(over="ignore"):
-        x = np.arange(n, dtype=u) * u(0x9E3779B1) + u(tensor) * u(0x632BE5AB) + u(seed) * u(0x85157AF5) + u(step) * u(0xD168AAAD)
+        x = wrap(elements.astype(u)) * u(0x9E3779B1) + u(tensor) * u(0x632BE5AB) + u(seed) * u(0x85157AF5) + u(step) * u(0xD168AAAD)
         x = wrap(x)
         x = wrap((x ^ (x >> u(16))) * u(0x6C8E9CF5))
         x = wrap((x ^ (x >> u(15))) * u(0xB5297A4D))

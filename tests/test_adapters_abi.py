@@ -98,14 +98,14 @@ def test_forward(qb):
     def call(**k):
         return qb.lib().qblora_adapters_fwd(*[C.byref(k[x]) if x == "ads" and k[x] else k[x] for x in FWD], None)
 
-    good = dict(ads=adapters(qb), first=A, order=A, tiles=A, X=A, ldx=512, T=10, Y=A, ldy=256, saved=A, ws=A, ws_bytes=BIG)
+    good = dict(ads=adapters(qb), first=A, order=A, tiles=A, X=A, ldx=512, T=10, Y=2 * A, ldy=256, saved=A, ws=A, ws_bytes=BIG)
     need = qb.lib().qblora_adapters_workspace_bytes(C.byref(good["ads"]), 10)
     assert need > 0 and need % 256 == 0
     check(call, good, [(dict(ads=adapters(qb, **c)), code) for c, code in BAD_ADAPTERS] + [
         (dict(ads=None), NULL), (dict(T=-1), SHAPE), (dict(T=(1 << 20) + 1), UNSUPPORTED), (dict(ldx=504), SHAPE), (dict(ldx=516), SHAPE),
         (dict(ldy=248), SHAPE), (dict(ldy=260), SHAPE), (dict(X=A + 8), SHAPE), (dict(Y=A + 2), SHAPE), (dict(saved=A + 8), SHAPE),
         (dict(tiles=A + 8), SHAPE), (dict(ws=None), WORKSPACE), (dict(ws=A + 16), WORKSPACE), (dict(ws_bytes=need - 1), WORKSPACE),
-        (dict(T=0), 0), (dict(T=0, X=None, Y=None, order=None, tiles=None, ws=None, ws_bytes=0), 0)] + [
+        (dict(Y=A), SHAPE), (dict(T=0), 0), (dict(T=0, X=None, Y=None, order=None, tiles=None, ws=None, ws_bytes=0), 0)] + [
         ({name: None}, NULL) for name in ("first", "order", "tiles", "X", "Y")])
 
 
@@ -113,13 +113,13 @@ def test_backward(qb):
     def call(**k):
         return qb.lib().qblora_adapters_bwd(*[C.byref(k[x]) if x == "ads" and k[x] else k[x] for x in BWD], None)
 
-    good = dict(ads=adapters(qb), first=A, order=A, tiles=A, X=A, ldx=512, dY=A, lddy=256, T=10, saved=A, dX=A, lddx=512, gradients=1, ws=A,
+    good = dict(ads=adapters(qb), first=A, order=A, tiles=A, X=A, ldx=512, dY=2 * A, lddy=256, T=10, saved=A, dX=3 * A, lddx=512, gradients=1, ws=A,
                 ws_bytes=BIG)
     need = qb.lib().qblora_adapters_workspace_bytes(C.byref(good["ads"]), 10)
     check(call, good, [(dict(ads=adapters(qb, **c)), code) for c, code in BAD_ADAPTERS] + [
         (dict(T=-1), SHAPE), (dict(T=(1 << 20) + 1), UNSUPPORTED), (dict(ldx=508), SHAPE), (dict(lddy=252), SHAPE),
         (dict(lddx=500), SHAPE), (dict(X=A + 8), SHAPE), (dict(dY=A + 8), SHAPE), (dict(dX=A + 8), SHAPE), (dict(saved=A + 4), SHAPE),
-        (dict(dX=None, gradients=0), NULL), (dict(ws=None), WORKSPACE), (dict(ws_bytes=need - 1), WORKSPACE),
+        (dict(dX=None, gradients=0), NULL), (dict(dX=A), SHAPE), (dict(dX=2 * A), SHAPE), (dict(ws=None), WORKSPACE), (dict(ws_bytes=need - 1), WORKSPACE),
         (dict(T=0, gradients=0), 0), (dict(T=0, dX=None, gradients=0), NULL)] + [
         ({name: None}, NULL) for name in ("ads", "first", "order", "tiles", "X", "dY")])
 

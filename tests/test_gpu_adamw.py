@@ -287,6 +287,38 @@ def test_captured_step(qb, bits):
         assert int(step) == i
 
 
+def test_more_elements_than_32_bits_count(qb):
+    """A tensor of 2^32 elements and some: its ends and the places around 2^31 and 2^32, by a step of cut-out pieces."""
+    n, step, lr = (1 << 32) + 777, 3, 1e-2
+    g = torch.zeros(n, device=au.DEV)
+    p = torch.zeros(n, dtype=torch.bfloat16, device=au.DEV)
+    m, v = torch.zeros(n, dtype=torch.float8_e4m3fn, device=au.DEV), torch.zeros(n, dtype=torch.float8_e5m2, device=au.DEV)
+    ms, vs = torch.zeros(-(-n // 256), device=au.DEV), torch.zeros(-(-n // 256), device=au.DEV)
+    r = np.random.Generator(np.random.Philox(key=[3, 3]))
+    places = [0, (1 << 31) - 256, (1 << 32) - 256, 1 << 32, n - 9 - 256]
+    values = {}
+    for at in places:
+        at -= at % 256
+        k = min(512, n - at)
+        values[at] = np.asarray(r.standard_normal(k), np.float32).astype(np.float64)
+        g[at:at + k] = torch.from_numpy(values[at]).float()
+    lst = qb.qblora_adamw_list([p], [g], [m], [v], m_scale=[ms], v_scale=[vs])
+    norm = qb.qblora_grad_norm(lst, 1e9)
+    # overlapping pieces hold the last values written
+    kept = {at: g[at:at + len(x)].cpu().numpy().astype(np.float64) for at, x in values.items()}
+    qb.qblora_adamw_step(lst, step, lr, B1, B2, EPS, seed=2)
+    assert norm[0] > 10 and torch.isfinite(norm).all()
+    bits = {at: au.random_bits_at(np.arange(at, at + len(x)), 0, step, 2) for at, x in kept.items()}
+    for at, x in kept.items():
+        zero = np.zeros(len(x))
+        w, _, _ = au.adamw(zero, zero, zero, x, step, lr, B1, B2, EPS)
+        m1, v1 = au.moments32(zero, zero, x, B1, B2)
+        want = au.Moments8(m1.astype(np.float64), v1.astype(np.float64), bits[at])
+        assert np.array_equal(au.host(m[at:at + len(x)]), want.m) and np.array_equal(au.host(v[at:at + len(x)]), want.v), at
+        got = au.host(p[at:at + len(x)])
+        assert (np.abs(got - w) <= 2 * au.half_step(np.where(w == 0, 1e-30, w)) + 1e-7).all(), at
+
+
 def test_empty_list(qb):
     lst = qb.qblora_adamw_list([], [], [], [], master=[])
     out = qb.qblora_grad_norm(lst, 2.0)

@@ -126,6 +126,51 @@ def test_backward(qb, layer, kept):
         au.assert_grad(g[1], wB[a], sB[a], b.d_in + b.T, f"dB of {a}")
 
 
+RULES = [  # inner rank, lambdas, tokens of each adapter: both sides of what chooses a kernel's form
+    (256, 2, 2, [1, 2, 3, 4, 5]), (256, 2, 2, [8, 9, 15, 16, 17]), (256, 1, 1, [20, 33, 36, 48, 52]), (264, 2, 2, [1, 4, 5, 17]),
+    (128, 4, 4, [4, 5, 21, 36]), (32, 8, 8, [1, 3, 5, 64, 68]), (64, 2, 8, [2, 6, 70]), (24, 2, 1, [3, 63, 65]),
+    (16, 2, 2, [1000, 23]), (16, 2, 2, [1000, 24]), (48, 1, 4, [1000, 25, 300])]
+
+
+@pytest.mark.parametrize("R,lam1,lam2,tokens", RULES)
+def test_around_the_rules(qb, R, lam1, lam2, tokens):
+    """Forward, and the backward pass without gradients, which takes other forms than the one with them."""
+    b = au.Batch(R + len(tokens), 512, 832, lam1, lam2, [R if i % 2 == 0 else max(8, R // 2 // 8 * 8) for i in range(len(tokens))], tokens,
+                 list(range(len(tokens))), extra=0)
+    table, groups = b.table(qb), b.groups(qb)
+    X, Y, dY, dX = (au.dev_bf16(t) for t in (b.X, b.Y, b.dY, b.dX))
+    qb.qblora_adapters_fwd(table, groups, X, Y)
+    want, size = b.forward()
+    au.assert_rows(Y, want, size, b.owner, b.Y, b.d_in, R, "Y")
+    qb.qblora_adapters_bwd(table, groups, None, dY, dX=dX, gradients=False)
+    want, _, _, size, _, _ = b.backward()
+    au.assert_rows(dX, want, size, b.owner, b.dX, b.d_out, R, "dX")
+
+
+def test_rows_far_apart(qb):
+    """Arrays whose rows lie 2^24 elements apart, so that the last ones begin beyond 2^32 elements."""
+    b = au.Batch(60, 256, 384, 2, 2, [32, 16], [150, 3, 150], [0, 1, 1])
+    far = 1 << 24
+
+    def spread(x):
+        out = torch.empty((b.T - 1) * far + x.shape[1], dtype=torch.bfloat16, device=au.DEV).as_strided(x.shape, (far, 1))
+        out.copy_(au.dev_bf16(x))
+        return out
+
+    grads = b.grads()
+    table, groups = b.table(qb, grads=grads), b.groups(qb)
+    X, Y, dY, dX = (spread(t) for t in (b.X, b.Y, b.dY, b.dX))
+    qb.qblora_adapters_fwd(table, groups, X, Y)
+    qb.qblora_adapters_bwd(table, groups, X, dY, dX=dX)
+    want, size = b.forward()
+    au.assert_rows(Y, want, size, b.owner, b.Y, b.d_in, 32, "Y")
+    wX, wA, wB, sX, sA, sB = b.backward()
+    au.assert_rows(dX, wX, sX, b.owner, b.dX, b.d_out, 32, "dX")
+    for a, g in enumerate(grads):
+        au.assert_grad(g[0], wA[a], sA[a], b.d_out + b.T, "dA")
+        au.assert_grad(g[1], wB[a], sB[a], b.d_in + b.T, "dB")
+
+
 def test_backward_of_long_groups(qb):
     """Enough tokens of few adapters that the gradients are summed in slices."""
     b = au.Batch(21, 128, 192, 2, 2, [16, 8, 24], [1500, 700, 1, 1333], [0, 2, 1, 0], 3)
@@ -144,6 +189,7 @@ def test_backward_of_long_groups(qb):
 
 @pytest.mark.parametrize("dx,gradients", [(True, False), (False, True)])
 def test_half_a_backward_pass(qb, dx, gradients):
+    """What is not asked for stays, and what is has the bits of the whole pass."""
     b = au.Batch(*LAYERS[5])
     grads = b.grads()
     table, groups = b.table(qb, grads=grads), b.groups(qb)
