@@ -785,10 +785,16 @@ int spread(const SpreadDesc& d, hipStream_t st) {
     if (rc) return rc;
     constexpr int kRows = spread_rows<LAM, KS, kTileTokens>();
     const int J = d.width / LAM, steps = (J + kRows - 1) / kRows;
-    const int parts = std::min(steps, std::max(1, 1024 / d.g.tile_room));
-    const int rows = (steps + parts - 1) / parts * kRows;
     const int more = d.u ? 0 : spread_u_bytes(std::min(d.g.T, kTileTokens), d.g.R), stage = spread_stage_bytes<LAM, KS, kTileTokens>(d.g.R);
     const int stages = ring_stages(stage, more);
+    // one round of workgroups where that fills nine tenths of the chip with eight steps each at least, else smaller ones in about
+    // 1024: 125 tiles of 2048 rows 39 us with 500 workgroups, 42 with 1000 (4096 rows, R = 256: 94 with 250, 106 with 1000);
+    // 88 of 2560 rows 25.4 with 440, 22.4 with 970
+    const int slots = stages * stage + more <= 80 * 1024 ? 512 : 256;
+    int parts = slots / d.g.tile_room;
+    if (10 * parts * d.g.tile_room < 9 * slots || steps < 8 * parts) parts = 1024 / d.g.tile_room;
+    parts = std::min(steps, std::max(1, parts));
+    const int rows = (steps + parts - 1) / parts * kRows;
     k_spread<LAM, BACK, KS><<<dim3(d.g.tile_room, (J + rows - 1) / rows), 64 * kWideWaves, stages * stage + more, st>>>(d, rows, stages);
     return launch_status();
 }
@@ -832,9 +838,12 @@ int launch_adapter_groups(const GroupsDesc& d, hipStream_t st) {
     return launch_status();
 }
 
+// Slices of the inputs: as many workgroups as the CUs take at once (three each up to R = 128, by LDS, two above), but 16 steps a slice where
+// that makes 512 workgroups all the same.  85 tiles of 13824 inputs: 5 slices 39 us, 8 32; 123 tiles of 4096: 4 slices 21.5 us, 6 23.5; of
+// 8192 with R = 256: 2 slices 73 us, 4 48, 6 66.
 int rank_splits(int tiles, int width, int R) {
-    const int steps = width / 64, wanted = std::max(1, 512 / std::max(1, tiles));
-    return std::min({steps, wanted, 16});
+    const int steps = width / 64, wanted = std::min((R <= 128 ? 768 : 512) / std::max(1, tiles), std::max(steps / 16, 512 / std::max(1, tiles)));
+    return std::max(1, std::min({steps, wanted, 16}));
 }
 
 int launch_rank_sums(const RankDesc& d, hipStream_t st) {
