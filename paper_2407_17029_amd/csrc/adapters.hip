@@ -127,17 +127,24 @@ __global__ __launch_bounds__(kGroupThreads) void k_adapter_groups(GroupsDesc d) 
 
 // ---- what the halves share ---------------------------------------------------------------------------------------
 
-struct Tile { int begin, tokens, R; const AdapterEntry* entry; };
+// A tile and its adapter, with numbers that keep all accesses inside the arrays; ok: they are those of a tile with an adapter
+struct Tile { int begin, tokens, R; float s; const qblora_bf16* A; const qblora_bf16* B; bool ok; };
 
-// The tile's description, if it is one: numbers out of range make none.
-__device__ __forceinline__ bool read_tile(const Grouped& g, int at, Tile* tile) {
+// Nothing here waits for the adapter's description, so that a caller may ask for the tile's tokens at the same time.
+__device__ __forceinline__ Tile read_tile(const Grouped& g, int at) {
     const int4 e = reinterpret_cast<const int4*>(g.tiles)[at];
-    if (e.x < 0 || e.x >= g.count || e.y < 0 || e.z <= 0 || e.z > kTileTokens || e.y > g.T - e.z) return false;
-    const AdapterEntry* entry = g.table + e.x;
-    const int R = entry->R;
-    if (R <= 0 || R > g.R) return false;
-    *tile = {e.y, e.z, R, entry};
-    return true;
+    const AdapterEntry* const entry = g.table + min(max(e.x, 0), g.count - 1);
+    const uint4 matrices = *reinterpret_cast<const uint4*>(entry);
+    const uint2 rank = *reinterpret_cast<const uint2*>(&entry->R);
+    Tile tile;
+    tile.begin = min(max(e.y, 0), g.T - 1);
+    tile.tokens = min(min(max(e.z, 1), kTileTokens), g.T - tile.begin);
+    tile.A = reinterpret_cast<const qblora_bf16*>((uint64_t)matrices.y << 32 | matrices.x);
+    tile.B = reinterpret_cast<const qblora_bf16*>((uint64_t)matrices.w << 32 | matrices.z);
+    tile.R = (int)rank.x;
+    tile.s = __uint_as_float(rank.y);
+    tile.ok = e.x >= 0 && e.x < g.count && e.y == tile.begin && e.z == tile.tokens && tile.R > 0 && tile.R <= g.R;
+    return tile;
 }
 
 // Eight values of four of them, each twice; and so on: the operand of eight inputs from the lam-th part of as many rows
@@ -221,7 +228,7 @@ __device__ __forceinline__ int row_swap(int row, int chunks) {
 }
 
 template <int LAM, bool BACK>
-__device__ void rank_many(const RankDesc& d, const Tile& tile, int step0, int step1, int r_base, float* part, unsigned char* smem) {
+__device__ void rank_many(const RankDesc& d, const Tile& tile, const int (&tokens)[2], int step0, int step1, int r_base, float* part, unsigned char* smem) {
     constexpr int kWRows = 64 / LAM;                       // of A for a step
     constexpr int kMost = rank_w_copies<LAM>(kRankRows);
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -233,14 +240,13 @@ __device__ void rank_many(const RankDesc& d, const Tile& tile, int step0, int st
     const unsigned char* z[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int l = 8 * (wave + 4 * i) + (lane >> 3);
-        const int token = min(max(d.g.order[tile.begin + min(l, tile.tokens - 1)], 0), d.g.T - 1);
+        const int token = min(max(tokens[i], 0), d.g.T - 1);
         z[i] = reinterpret_cast<const unsigned char*>(d.Z + (int64_t)token * d.ldz) + (int64_t)step0 * 128 + 16 * ((lane & 7) ^ (lane >> 3));
     }
     // W: chunks of 16 bytes, `per` of them a row; places behind the last chunk fetch the first
     const int per = BACK ? 8 / LAM : R / 8, chunks = R * (8 / LAM);
     const int w_copies = rank_w_copies<LAM>(R);
-    const unsigned char* const w = reinterpret_cast<const unsigned char*>(BACK ? tile.entry->B + (int64_t)r_base * J : tile.entry->A + r_base);
+    const unsigned char* const w = reinterpret_cast<const unsigned char*>(BACK ? tile.B + (int64_t)r_base * J : tile.A + r_base);
     uint32_t w_from[kMost];
 #pragma unroll
     for (int i = 0; i < kMost; ++i) {
@@ -337,7 +343,7 @@ __device__ void rank_many(const RankDesc& d, const Tile& tile, int step0, int st
         products(buf);
         buf = buf == 2 ? 0 : buf + 1;
     }
-    const float f = d.factor * tile.entry->s;
+    const float f = d.factor * tile.s;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (i >= mine) break;
@@ -356,14 +362,16 @@ __device__ void rank_many(const RankDesc& d, const Tile& tile, int step0, int st
 template <int LAM, bool BACK>
 __global__ __launch_bounds__(kRankThreads) void k_rank_sums(RankDesc d) {
     extern __shared__ __align__(16) unsigned char smem[];
-    Tile tile;
-    if (!read_tile(d.g, blockIdx.x, &tile)) return;
+    const Tile tile = read_tile(d.g, blockIdx.x);
+    int tokens[2];                                             // of the rows that this lane copies
+#pragma unroll
+    for (int i = 0; i < 2; ++i) tokens[i] = d.g.order[tile.begin + min(8 * ((int)(threadIdx.x >> 6) + 4 * i) + (int)(threadIdx.x >> 3 & 7), tile.tokens - 1)];
     const int r_base = blockIdx.z * kRankRows, split = blockIdx.y;
-    if (r_base >= tile.R) return;
+    if (!tile.ok || r_base >= tile.R) return;
     const int all = d.width / 64;
     const int step0 = (int)((int64_t)all * split / d.splits), step1 = (int)((int64_t)all * (split + 1) / d.splits);
     float* const part = d.part + (int64_t)split * d.g.T * d.g.R;
-    rank_many<LAM, BACK>(d, tile, step0, step1, r_base, part, smem);
+    rank_many<LAM, BACK>(d, tile, tokens, step0, step1, r_base, part, smem);
 }
 
 // ---- spread ------------------------------------------------------------------------------------------------------
@@ -480,7 +488,7 @@ __device__ void spread_tile(const SpreadDesc& d, const Tile& tile, int j0, int j
     // W: chunks of 16 bytes, `per` of them a row; places behind the last chunk, or behind the last row of outputs, fetch the first
     const int per = BACK ? R / 8 : kRows / 8, chunks = R * (kRows / 8);
     const int w_copies = spread_w_copies<LAM, KS, ROOM>(R);
-    const unsigned char* const w = reinterpret_cast<const unsigned char*>(BACK ? tile.entry->A : tile.entry->B);
+    const unsigned char* const w = reinterpret_cast<const unsigned char*>(BACK ? tile.A : tile.B);
     uint32_t w_from[kMost];
     int w_row[kMost];                                                          // first of the step's outputs / lam that the chunk holds
 #pragma unroll
@@ -611,10 +619,9 @@ __device__ void spread_tile(const SpreadDesc& d, const Tile& tile, int j0, int j
 template <int LAM, bool BACK, int KS>
 __global__ __launch_bounds__(64 * kWideWaves) void k_spread(SpreadDesc d, int rows, int stages) {       // rows: of W, for a workgroup
     extern __shared__ __align__(16) unsigned char smem[];
-    Tile tile;
-    if (!read_tile(d.g, blockIdx.x, &tile)) return;
+    const Tile tile = read_tile(d.g, blockIdx.x);
     const int j0 = blockIdx.y * rows, j1 = min(j0 + rows, d.width / LAM);
-    if (j0 >= j1) return;
+    if (!tile.ok || j0 >= j1) return;
     spread_tile<LAM, BACK, KS, kTileTokens>(d, tile, j0, j1, stages, smem, smem + stages * spread_stage_bytes<LAM, KS, kTileTokens>(d.g.R));
 }
 
@@ -630,7 +637,7 @@ __device__ void spread_few(const SpreadDesc& d, const Tile& tile, int j0, int j1
     const int t = threadIdx.x, share = t >> 5, R = tile.R, J = d.width / LAM, col = 8 * (t & 31);
     float* const us = reinterpret_cast<float*>(smem);                          // [R][MT]
     float* const sums = us + 32 * KS * MT;                                     // [8 shares][MT][256]
-    const qblora_bf16* const B = tile.entry->B + (int64_t)share * J;
+    const qblora_bf16* const B = tile.B + (int64_t)share * J;
     // No load is conditional, as loads behind a branch are waited for together: rows behind R and outputs behind the last fetch others
     // once more, which are not used.
     uint4 w[kAhead];
@@ -719,12 +726,13 @@ __device__ __forceinline__ void spread_few(const SpreadDesc& d, const Tile& tile
 template <int LAM, int KS>
 __global__ __launch_bounds__(kFewThreads, 2) void k_spread_few(SpreadDesc d, int rows, int stages) {
     extern __shared__ __align__(16) unsigned char smem[];
-    Tile whole;
-    if (!read_tile(d.g, blockIdx.y, &whole)) return;
+    const Tile whole = read_tile(d.g, blockIdx.y);
     const int j0 = blockIdx.x * rows, j1 = min(j0 + rows, d.width / LAM);
-    if (j0 >= j1) return;
+    if (!whole.ok || j0 >= j1) return;
     for (int from = 0; from < whole.tokens; from += 16) {
-        const Tile tile{whole.begin + from, min(whole.tokens - from, 16), whole.R, whole.entry};
+        Tile tile = whole;
+        tile.begin += from;
+        tile.tokens = min(whole.tokens - from, 16);
         if (from) __syncthreads();
         if (tile.tokens > kFewTile) spread_tile<LAM, false, KS, 16>(d, tile, j0, j1, stages, smem, smem + stages * spread_stage_bytes<LAM, KS, 16>(d.g.R));
         else if (KS > 1 && tile.R <= 32) spread_few<LAM, 1>(d, tile, j0, j1, smem);
@@ -737,8 +745,8 @@ constexpr int few_bytes(int KS, int MT) { return 4 * MT * (32 * KS + 8 * kFewRow
 
 // U as three bf16 parts, 24 significant bits: the sums of the slices of one or two arrays
 __global__ __launch_bounds__(256) void k_rank_parts(PartsDesc d) {
-    Tile tile;
-    if (!read_tile(d.g, blockIdx.x, &tile)) return;
+    const Tile tile = read_tile(d.g, blockIdx.x);
+    if (!tile.ok) return;
     const bool second = blockIdx.y != 0;
     const float* const part = second ? d.part2 : d.part;
     qblora_bf16* const out = second ? d.out2 : d.out;
