@@ -811,11 +811,13 @@ template <int LAM, int KS>
 int spread_few_tokens(const SpreadDesc& d, hipStream_t st) {
     const int rc = allow_lds(k_spread_few<LAM, KS>);
     if (rc) return rc;
-    const int J = d.width / LAM, pieces = (J + kFewRows - 1) / kFewRows;
-    // one round of workgroups, two a CU, while that gives each few pieces (40 adapters, 860 pieces: 512 workgroups 12.6 us, 2048 16.2); else
-    // more and smaller ones, which even out at the end (100 adapters, 4500 pieces: 1024 125 us, 2048 119)
+    // Pieces of 256 rows of outputs, or of 64 where those would leave most CUs idle.  One round of workgroups, two a CU, while that gives
+    // each few pieces (40 adapters, 860 pieces: 512 workgroups 12.6 us, 2048 16.2); else more and smaller ones, which even out at
+    // the end (100 adapters, 4500 pieces: 1024 125 us, 2048 119).
+    const int J = d.width / LAM, piece = d.g.tile_room * ((J + kFewRows - 1) / kFewRows) < 256 ? 64 : kFewRows;
+    const int pieces = (J + piece - 1) / piece;
     const int parts = std::min(pieces, std::max(1, (pieces * d.g.tile_room <= 2048 ? 512 : 2048) / d.g.tile_room));
-    const int rows = (pieces + parts - 1) / parts * kFewRows;
+    const int rows = (pieces + parts - 1) / parts * piece;
     const int more = spread_u_bytes(16, d.g.R), stage = spread_stage_bytes<LAM, KS, 16>(d.g.R), stages = ring_stages(stage, more);
     const int lds = std::max(d.g.T > kFewTile ? stages * stage + more : 0, few_bytes(KS, d.g.T >= 3 ? 4 : d.g.T));
     k_spread_few<LAM, KS><<<dim3((J + rows - 1) / rows, d.g.tile_room), kFewThreads, lds, st>>>(d, rows, stages);
@@ -823,8 +825,10 @@ int spread_few_tokens(const SpreadDesc& d, hipStream_t st) {
 }
 template <int LAM, bool BACK>
 int spread_by_rank(const SpreadDesc& d, hipStream_t st) {
+    // the kernel for few tokens of a tile where the batch has so few for each adapter, as far as their number tells (167 tokens on two
+    // adapters: 66 us with it, 230 tokens 40)
     if constexpr (!BACK)
-        if (!d.u) return d.g.R <= 64 ? spread_few_tokens<LAM, 2>(d, st) : d.g.R <= 128 ? spread_few_tokens<LAM, 4>(d, st) : spread_few_tokens<LAM, 8>(d, st);
+        if (!d.u && d.g.T <= 8 * d.g.count) return d.g.R <= 64 ? spread_few_tokens<LAM, 2>(d, st) : d.g.R <= 128 ? spread_few_tokens<LAM, 4>(d, st) : spread_few_tokens<LAM, 8>(d, st);
     if (d.g.R <= 64) return spread<LAM, BACK, 2>(d, st);
     if (d.g.R <= 128) return spread<LAM, BACK, 4>(d, st);
     if (d.g.R <= 256) return spread<LAM, BACK, 8>(d, st);
@@ -851,7 +855,7 @@ int launch_adapter_groups(const GroupsDesc& d, hipStream_t st) {
 // 8192 with R = 256: 2 slices 73 us, 4 48, 6 66.
 int rank_splits(int tiles, int width, int R) {
     const int steps = width / 64, wanted = std::min((R <= 128 ? 768 : 512) / std::max(1, tiles), std::max(steps / 16, 512 / std::max(1, tiles)));
-    return std::max(1, std::min({steps, wanted, 16}));
+    return std::max(1, std::min({steps, wanted, std::max(16, std::min(steps / 4, 32))}));
 }
 
 int launch_rank_sums(const RankDesc& d, hipStream_t st) {

@@ -38,7 +38,7 @@ int check_rows(const void* p, int64_t ld, int width) {
 }
 // From so many tokens on, or inner ranks whose sums do not fit LDS beside the rest, sums that are cut into slices are added up once, in
 // a launch of their own, and not by every workgroup that needs them
-bool parts_pay(int64_t T, int R) { return T >= 1024 || R > 256; }
+bool parts_pay(const qblora_adapters* a, int64_t T) { return T >= 1024 || a->R > 256 || (T > 8 * (int64_t)a->count && a->R > 64); }
 
 int tile_room(int count, int64_t T) { return (int)((T + kTileTokens - 1) / kTileTokens + std::min<int64_t>(count, T)); }
 
@@ -169,7 +169,7 @@ int qblora_adapters_fwd(const qblora_adapters* a, const int32_t* first, const in
     if ((rc = launch_rank_sums(u, as_stream(stream)))) return rc;
     SpreadDesc v{};
     v.g = u.g; v.part = u.part; v.splits = u.splits;
-    if (saved || parts_pay(T, a->R)) {
+    if (saved || parts_pay(a, T)) {
         PartsDesc w{};
         w.g = u.g; w.part = u.part; w.splits = u.splits;
         w.out = saved ? saved : reinterpret_cast<qblora_bf16*>(reinterpret_cast<unsigned char*>(workspace) + s.part_x + s.part_y);
@@ -221,7 +221,7 @@ int qblora_adapters_bwd(const qblora_adapters* a, const int32_t* first, const in
     if ((rc = launch_rank_sums(u, st))) return rc;
     SpreadDesc v{};
     v.g = w.g; v.part = part_y; v.splits = u.splits;
-    if (gradients || parts_pay(T, a->R)) {
+    if (gradients || parts_pay(a, T)) {
         p.part = part_y; p.splits = u.splits; p.out = du;
         if ((rc = launch_rank_parts(p, st))) return rc;
         v.u = du;
