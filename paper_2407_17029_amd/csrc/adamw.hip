@@ -1,5 +1,10 @@
 // The optimizer's step over many tensors at once: the list on the device, the norm of all gradients, and AdamW with moments in
 // 32 or 8 bits (qblora_adamw_plan, qblora_grad_norm, qblora_adamw_step; the formulas stand in include/qblora.h).
+//
+// Bound by HBM: a step reads every gradient, moment and weight once and writes them once, the norm in front of it reads the gradients
+// once more.  120 million elements in 84 tensors, moments in 8 bits, fp32 masters and bf16 copies (18 bytes an element): the step 378 us,
+// 5.7 TB/s, the norm 95 to 127 + 5; 5 million in 14 tensors with moments in 32 bits (30 bytes): 23 us and 5 + 2.  Element by element
+// with pointers that might have been LDS ones the step took 784 and 39 us.
 #include <algorithm>
 
 #include "adapters.h"

@@ -5,6 +5,12 @@
 //
 // Mean and repetition are never made: a matrix operand's row of W serves lam inputs, a result lam outputs.  Both halves go tile
 // by tile, a tile being up to 64 tokens of one adapter, so that W is read once for them.
+//
+// What bounds them and what they take, on one MI355X (a large copy reaches 5.1 TB/s there, read + write): single tokens are the stream of
+// the adapters (256 tokens on 100 adapters, 8192 to 22016, R = 256: 210 MB of A in 41 us, 5.1 TB/s, 564 MB of B in 119, 4.7; eight tokens
+// on eight adapters, 4096 square, 6.3 and 7.0 us, where an empty launch takes 3.5).  Training batches are X, dY and the outputs (7810
+// tokens, 4096 square, R = 128: 64 MB in 21 us, 128 MB of outputs in and out in 38) until the products count (7842 tokens to 22016
+// features, R = 256: 88 GFLOP and 345 MB in 150 us, 88 GFLOP in two parts and 690 MB in 240).
 #include <algorithm>
 
 #include "adapters.h"
@@ -26,7 +32,7 @@ __global__ __launch_bounds__(64) void k_adapter_table(TableDesc d) {
 //
 // Every workgroup reads all requests into LDS and adds up the tokens of each adapter (integer sums: any order), scans them, and
 // then serves 64 requests of its own: 16 threads a request add up what earlier requests of its adapter have, a wave writes its
-// tokens.
+// tokens.  64 single tokens 5.5 us, 1000 requests with 50000 tokens 11.9: reads that wait for one another, not bytes.
 constexpr int kGroupThreads = 1024, kGroupRequests = kGroupThreads / 16;
 
 // exclusive scan over the workgroup of a value each thread brings, and the sum of all; `slots`: one int a wave
