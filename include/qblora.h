@@ -604,7 +604,7 @@ int qblora_adapter_groups(const int32_t* starts, const int32_t* which, int32_t n
  *   Y      bf16, likewise (ldy, d_out); no part of X
  *   first, order, tiles   as qblora_adapter_groups wrote them for this batch and this count.  A token must not be listed twice.
  *   saved  qblora_adapters_saved_bytes(), 16-byte aligned, or NULL: s U of every listed token, which the backward pass needs
- *   workspace   at least qblora_adapters_workspace_bytes(), 256-byte aligned; the size serves both directions
+ *   workspace   at least qblora_adapters_workspace_bytes(), 256-byte aligned; the size serves both directions and every smaller T
  * T = 0 is a no-op; T <= 2^20.
  */
 size_t qblora_adapters_saved_bytes(const qblora_adapters* adapters, int64_t T);
@@ -622,7 +622,8 @@ int qblora_adapters_fwd(const qblora_adapters* adapters, const int32_t* first, c
  *           overwritten, with zeros where the batch has no token of an adapter; sums in a fixed order, a repeated call repeats
  *           its bits
  *   saved   what qblora_adapters_fwd wrote for the same X, adapters and groups; NULL: s U is computed again from X
- * T = 0: gradients are zero, nothing else happens.
+ * T = 0: gradients are zero, nothing else happens.  A token whose X or dY is not finite makes the gradients that it counts in
+ * NaN or infinite, and which of the two is not specified.
  */
 int qblora_adapters_bwd(const qblora_adapters* adapters, const int32_t* first, const int32_t* order, const int32_t* tiles,
                         const qblora_bf16* X, int64_t ldx, const qblora_bf16* dY, int64_t lddy, int64_t T,

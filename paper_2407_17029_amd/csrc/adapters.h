@@ -53,6 +53,8 @@ struct RankDesc {
     float* part; int splits;
 };
 int rank_splits(int tiles, int width, int R);
+// no fewer rows of partial sums, slices x tokens, than any number of tokens up to T takes
+int64_t rank_part_rows(int64_t T, int width);
 int launch_rank_sums(const RankDesc& d, hipStream_t st);
 
 // U, the sum of the slices, as three bf16 parts [3][T][R]: high part and what is left of it, twice.  The second array may be absent.

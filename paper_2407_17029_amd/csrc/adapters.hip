@@ -20,7 +20,6 @@ namespace qblora {
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
-typedef __attribute__((ext_vector_type(8))) short s16x8;
 
 // ---- the table ---------------------------------------------------------------------------------------------------
 
@@ -60,8 +59,7 @@ __global__ __launch_bounds__(kGroupThreads) void k_adapter_groups(GroupsDesc d) 
     int* const slot = mem;                                     // of each request; -1: none
     int* const length = slot + ((d.n + 3) & ~3);
     int* const tokens = length + ((d.n + 3) & ~3);             // of each adapter, then where they begin
-    int* const begin_tile = tokens + d.count;
-    int* const slots = begin_tile + d.count;
+    int* const slots = tokens + d.count;
     const int t = threadIdx.x;
     for (int a = t; a < d.count; a += kGroupThreads) tokens[a] = 0;
     __syncthreads();
@@ -91,7 +89,6 @@ __global__ __launch_bounds__(kGroupThreads) void k_adapter_groups(GroupsDesc d) 
         if (a >= d.count) break;
         const int m = tokens[a];
         tokens[a] = at;
-        begin_tile[a] = at_tile;
         if (a % gridDim.x == blockIdx.x) {                     // the adapters' tiles are shared out among the workgroups
             d.first[a] = min(max(at, 0), d.T);
             for (int j = 0; j * kTileTokens < m; ++j) {
@@ -416,10 +413,17 @@ __host__ __device__ constexpr int spread_stage_bytes(int R) {
 // U of a tile in LDS, where the workgroup adds up the slices
 __host__ __device__ constexpr int spread_u_bytes(int tokens, int R) { return (tokens < kTileTokens ? tokens : kTileTokens) * 4 * R; }
 
+// The bf16 value next to v that a finite v leaves finite, and what it leaves: nothing of an infinity, which would make NaN of it
+__device__ __forceinline__ float high_part(float v) {
+    const float h = bf16_lo(pack_bf16(v, 0.0f));
+    return __builtin_isinf(h) && !__builtin_isinf(v) ? copysignf(0x1.fep127f, v) : h;
+}
+__device__ __forceinline__ float left_of(float v, float high) { return __builtin_isinf(high) ? 0.0f : v - high; }
 __device__ __forceinline__ void split_pair(float4 v, uint2* hi, uint2* lo) {
-    hi->x = pack_bf16(v.x, v.y); hi->y = pack_bf16(v.z, v.w);
-    lo->x = pack_bf16(v.x - bf16_lo(hi->x), v.y - bf16_hi(hi->x));
-    lo->y = pack_bf16(v.z - bf16_lo(hi->y), v.w - bf16_hi(hi->y));
+    const float4 h = make_float4(high_part(v.x), high_part(v.y), high_part(v.z), high_part(v.w));
+    hi->x = pack_bf16(h.x, h.y); hi->y = pack_bf16(h.z, h.w);
+    lo->x = pack_bf16(left_of(v.x, h.x), left_of(v.y, h.y));
+    lo->y = pack_bf16(left_of(v.z, h.z), left_of(v.w, h.w));
 }
 
 // Four neighbouring r of the sum of the slices, always in the same order; eight loads under way together
@@ -763,8 +767,8 @@ __global__ __launch_bounds__(256) void k_rank_parts(PartsDesc d) {
         const float4 v = sum_slices(part, splits, slice, at);
         uint2 h, m, l;
         split_pair(v, &h, &m);
-        l.x = pack_bf16(v.x - bf16_lo(h.x) - bf16_lo(m.x), v.y - bf16_hi(h.x) - bf16_hi(m.x));
-        l.y = pack_bf16(v.z - bf16_lo(h.y) - bf16_lo(m.y), v.w - bf16_hi(h.y) - bf16_hi(m.y));
+        l.x = pack_bf16(left_of(v.x, bf16_lo(h.x)) - bf16_lo(m.x), left_of(v.y, bf16_hi(h.x)) - bf16_hi(m.x));
+        l.y = pack_bf16(left_of(v.z, bf16_lo(h.y)) - bf16_lo(m.y), left_of(v.w, bf16_hi(h.y)) - bf16_hi(m.y));
         *reinterpret_cast<uint2*>(out + at) = h;
         *reinterpret_cast<uint2*>(out + slice + at) = m;
         *reinterpret_cast<uint2*>(out + 2 * slice + at) = l;
@@ -849,7 +853,7 @@ int launch_adapter_table(const TableDesc& d, hipStream_t st) {
 }
 
 int launch_adapter_groups(const GroupsDesc& d, hipStream_t st) {
-    const int lds = (2 * ((d.n + 3) & ~3) + 2 * d.count + kGroupRequests) * 4;
+    const int lds = (2 * ((d.n + 3) & ~3) + d.count + kGroupRequests) * 4;
     const int rc = allow_lds(k_adapter_groups);
     if (rc) return rc;
     k_adapter_groups<<<std::max(1, (d.n + kGroupRequests - 1) / kGroupRequests), kGroupThreads, lds, st>>>(d);
@@ -862,6 +866,10 @@ int launch_adapter_groups(const GroupsDesc& d, hipStream_t st) {
 int rank_splits(int tiles, int width, int R) {
     const int steps = width / 64, wanted = std::min((R <= 128 ? 768 : 512) / std::max(1, tiles), std::max(steps / 16, 512 / std::max(1, tiles)));
     return std::max(1, std::min({steps, wanted, std::max(16, std::min(steps / 4, 32))}));
+}
+
+int64_t rank_part_rows(int64_t T, int width) {
+    return std::max(T, std::min(std::min<int64_t>(32, width / 64) * T, (int64_t)768 * kTileTokens));
 }
 
 int launch_rank_sums(const RankDesc& d, hipStream_t st) {

@@ -49,15 +49,14 @@ Grouped grouped(const qblora_adapters* a, const int32_t* first, const int32_t* o
     return g;
 }
 
-// The workspace, in this order: partial sums of the rank sums on X and on dY, the bf16 parts of s U and dU, partial gradients
+// The workspace, in this order: partial sums of the rank sums on X and on dY, the bf16 parts of s U and dU, partial gradients.  No
+// size shrinks as T grows, so that one for the largest batch serves every smaller one.
 struct Space { size_t part_x, part_y, su, du, grads, all; };
 Space space_of(const qblora_adapters* a, int64_t T) {
-    const int tiles = tile_room(a->count, T);
-    const size_t rows = (size_t)T * a->R;
     Space s{};
-    s.part_x = up256(rows * 4 * rank_splits(tiles, a->d_in, a->R));
-    s.part_y = up256(rows * 4 * rank_splits(tiles, a->d_out, a->R));
-    s.su = s.du = up256(rows * 6);
+    s.part_x = up256((size_t)rank_part_rows(T, a->d_in) * a->R * 4);
+    s.part_y = up256((size_t)rank_part_rows(T, a->d_out) * a->R * 4);
+    s.su = s.du = up256((size_t)T * a->R * 6);
     const int splits = adapter_grad_splits(a->count, T, a->d_in, a->d_out, a->R);
     if (splits > 1)
         s.grads = up256((size_t)splits * a->count * ((size_t)a->d_in / a->lambda1 + a->d_out / a->lambda2) * a->R * 4);

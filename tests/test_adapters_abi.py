@@ -131,6 +131,11 @@ def test_sizes(qb):
     sizes = [L.qblora_adapters_saved_bytes(C.byref(a), T) for T in (0, 1, 100)]
     assert sizes[0] == 0 and sizes[2] == 100 * sizes[1] and sizes[1] >= 64 * 4
     assert [L.qblora_adapters_workspace_bytes(C.byref(a), T) for T in (-1, 0, (1 << 20) + 1)] == [0, 0, 0]
+    # a workspace for the largest batch serves every smaller one
+    for kw in (dict(), dict(count=1, d_in=13824, d_out=5120, R=256), dict(count=500, R=8), dict(count=3, d_in=64, d_out=64, R=512)):
+        a = adapters(qb, **kw)
+        sizes = [L.qblora_adapters_workspace_bytes(C.byref(a), T) for T in (*range(1, 1200), *range(1200, 60000, 37), 1 << 20)]
+        assert sizes == sorted(sizes) and sizes[0] > 0
     bad = adapters(qb, d_in=100)
     assert L.qblora_adapters_workspace_bytes(C.byref(bad), 10) == 0 and L.qblora_adapters_saved_bytes(None, 10) == 0
 

@@ -263,6 +263,53 @@ def test_infinite_and_nan_rows_stay_theirs(qb):
     au.assert_rows(au.dev_bf16(got[keep]), want[keep], size[keep], b.owner[keep], b.Y[keep], b.d_in, 64, "Y")
 
 
+@pytest.mark.parametrize("saved", [False, True])
+@pytest.mark.parametrize("tokens", [1, 4, 6, 20, 70])
+def test_infinite_sums_pass(qb, tokens, saved):
+    """An infinite rank sum, and one next to fp32's largest number, through the parts that the second product takes: what fp32
+    products give, no NaN."""
+    b = au.Batch(42, 128, 192, 1, 2, [16], [tokens], [0])
+    b.A[0], b.B[0], b.s = np.abs(b.A[0]) + 0.25, np.abs(b.B[0]) + 0.25, [1.0]
+    b.A[0], b.B[0] = au.bf16(b.A[0]), au.bf16(b.B[0])
+    b.X[0, 5] = np.inf
+    last = tokens - 1
+    if last:
+        b.X[last] = 0.0
+        b.A[0][7] = 1.0
+        b.X[last, 7] = float(torch.finfo(torch.bfloat16).max)
+        b.B[0][:, :] = 2.0 ** -6
+    table, groups = b.table(qb), b.groups(qb)
+    keep = torch.empty(qb.qblora_adapters_saved_bytes(table, b.T), dtype=torch.uint8, device=au.DEV) if saved else None
+    Y = au.dev_bf16(b.Y)
+    qb.qblora_adapters_fwd(table, groups, au.dev_bf16(b.X), Y, saved=keep)
+    got = au.host(Y)
+    assert (got[0] == np.inf).all()
+    if last:
+        want = b.X[last, 7] * 16 * 2.0 ** -6
+        assert np.abs(got[last] - want).max() <= want * 2.0 ** -7
+
+
+def test_workspace_of_a_larger_batch(qb):
+    """One workspace, asked for once for the largest batch, full of NaN before every call."""
+    b = au.Batch(*LAYERS[10])
+    grads = b.grads()
+    table = b.table(qb, grads=grads)
+    ws = torch.empty(qb.qblora_adapters_workspace_bytes(table, 1500) // 4, device=au.DEV)
+    X, dY, dX = au.dev_bf16(b.X), au.dev_bf16(b.dY), au.dev_bf16(b.dX)
+    Y, groups = au.dev_bf16(b.Y), b.groups(qb)
+    ws.fill_(float("nan"))
+    qb.qblora_adapters_fwd(table, groups, X, Y, workspace=ws)
+    ws.fill_(float("nan"))
+    qb.qblora_adapters_bwd(table, groups, X, dY, dX=dX, workspace=ws)
+    want, size = b.forward()
+    au.assert_rows(Y, want, size, b.owner, b.Y, b.d_in, 96, "Y")
+    wX, wA, wB, sX, sA, sB = b.backward()
+    au.assert_rows(dX, wX, sX, b.owner, b.dX, b.d_out, 96, "dX")
+    for a, g in enumerate(grads):
+        au.assert_grad(g[0], wA[a], sA[a], b.d_out + b.T, "dA")
+        au.assert_grad(g[1], wB[a], sB[a], b.d_in + b.T, "dB")
+
+
 def test_broken_groups_stay_inside(qb):
     """Tiles and token numbers out of range do nothing; rows around the arrays stay."""
     b = au.Batch(41, 128, 128, 2, 2, [16, 8], [70, 5], [0, 1])
