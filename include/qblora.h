@@ -592,7 +592,7 @@ int qblora_adapter_table(const qblora_adapters* adapters, int32_t first, int32_t
  * All are written whole.  Tokens of no request, or with a number of T and above, belong to none.  Once for a batch: all projections
  * of a model read the same.  n <= 8192, count <= 8192, T <= 2^20.
  */
-int32_t qblora_adapter_tiles(int32_t count, int64_t T);
+int32_t qblora_adapter_tiles(int32_t count, int64_t T);                 /* ceil(T / 64) + min(count, T) */
 int qblora_adapter_groups(const int32_t* starts, const int32_t* which, int32_t n, int32_t count, int64_t T, int32_t* first,
                           int32_t* order, int32_t* tiles, void* stream);
 

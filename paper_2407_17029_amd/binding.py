@@ -881,6 +881,17 @@ def qblora_rms_norm_bwd(total: torch.Tensor, w: torch.Tensor, rstd: torch.Tensor
 
 # ---- many adapters on one frozen projection -------------------------------------------------------------
 
+def _current_device() -> int:
+    return torch._C._cuda_getDevice()
+
+
+def _here(*tensors) -> None:
+    """The calls below launch on the current device: what they are given has to lie there."""
+    device = _current_device()
+    for t in tensors:
+        assert t.get_device() == device
+
+
 class Adapters:
     """The adapters of one projection, by number, and the device table that describes them (qblora_adapter_table)."""
 
@@ -908,6 +919,7 @@ def qblora_adapter_table(adapters, d_in: int, d_out: int, lambda1: int = None, l
         table = torch.zeros(int(lib().qblora_adapter_table_bytes(count)), dtype=torch.uint8, device=device)
         into = Adapters(count, d_in, d_out, lambda1, lambda2, R, table)
     assert (into.d_in, into.d_out) == (d_in, d_out)
+    _here(into.table)
     n = len(adapters)
     empty = Adapter(None, None, into.lambda1, into.lambda2, 0.0)
     for a in adapters:
@@ -931,8 +943,9 @@ def qblora_adapter_groups(starts: torch.Tensor, which: torch.Tensor, count: int,
                           order: torch.Tensor = None, tiles: torch.Tensor = None):
     """(first, order, tiles): the T tokens of a batch by adapter, which all projections share.  starts [n + 1], which [n]."""
     n, = which.shape
+    _here(starts, which)
     L = lib()
-    room = L.qblora_adapter_tiles(count, T)
+    room = _tile_room(count, T)
     if first is None and order is None and tiles is None:                # one allocation; the tiles, which are 16 bytes each, lead it
         whole = torch.empty(4 * room + count + 1 + T, dtype=_I32, device=which.device)
         tiles, first, order = whole.split_with_sizes((4 * room, count + 1, T))
@@ -961,9 +974,14 @@ def _rows(t, T, width) -> int:
     return row if T > 1 else max(row, width)
 
 
+def _tile_room(count, T) -> int:
+    """qblora_adapter_tiles, without the call."""
+    return -(-T // 64) + min(count, T)
+
+
 def _groups(ads, groups, T):
     first, order, tiles = groups
-    assert tiles.dim() == 2 and tiles.shape[0] == lib().qblora_adapter_tiles(ads.count, T)
+    assert tiles.dim() == 2 and tiles.shape[0] == _tile_room(ads.count, T)
     return (_address(first, _I32, (ads.count + 1,)), _address(order, _I32, (T,)), _address(tiles, _I32, (tiles.shape[0], 4)))
 
 
@@ -993,6 +1011,7 @@ def qblora_adapters_fwd(ads: Adapters, groups, X: torch.Tensor, Y: torch.Tensor,
                         workspace: torch.Tensor = None):
     """Adds every token's adapter term to Y [T, d_out], in place.  groups: what qblora_adapter_groups returned."""
     T = X.shape[0]
+    _here(X, Y, ads.table)
     L, a = lib(), ads.c_bytes()
     ldx, ldy = _rows(X, T, ads.d_in), _rows(Y, T, ads.d_out)
     first, order, tiles = _groups(ads, groups, T)
@@ -1009,6 +1028,7 @@ def qblora_adapters_bwd(ads: Adapters, groups, X, dY: torch.Tensor, dX: torch.Te
     """Adds the adapters' part to dX [T, d_in] (if given), in place, and writes the gradients of the table's adapters.  X may be
     None without gradients; saved: what the forward call filled."""
     T = dY.shape[0]
+    _here(dY, ads.table)
     L, a = lib(), ads.c_bytes()
     ldx = 0 if X is None else _rows(X, T, ads.d_in)
     lddx = 0 if dX is None else _rows(dX, T, ads.d_in)
@@ -1043,6 +1063,7 @@ def qblora_adamw_list(params, grads, m, v, master=None, m_scale=None, v_scale=No
     bits = 8 if n and m[0].dtype is torch.float8_e4m3fn else 32
     types = (torch.float8_e4m3fn, torch.float8_e5m2) if bits == 8 else (_F32, _F32)
     assert all(len(x) == n for x in (params, m, v, master, m_scale, v_scale, rate, decay))
+    _here(*grads)
     c = (CAdamWTensor * max(n, 1))()
     for i in range(n):
         shape = grads[i].shape
@@ -1064,6 +1085,7 @@ def qblora_adamw_list(params, grads, m, v, master=None, m_scale=None, v_scale=No
 def qblora_grad_norm(tensors: AdamWList, max_norm: float, out: torch.Tensor = None, workspace: torch.Tensor = None):
     """fp32 [2] on the device: the norm of all gradients, and the factor that clips it to max_norm."""
     dev = tensors.plan.device
+    _here(tensors.plan)
     if out is None:
         out = torch.empty(2, dtype=_F32, device=dev)
     if workspace is None:
@@ -1080,6 +1102,7 @@ def qblora_adamw_step(tensors: AdamWList, step, lr, beta1: float = 0.9, beta2: f
     """One AdamW step on every tensor of the list, in place.  step, lr: numbers, or one-element tensors on the device (int64 and
     fp32) that the call reads when it runs, as a captured graph needs; clip: what qblora_grad_norm returned."""
     p_step = p_lr = 0
+    _here(tensors.plan)
     if isinstance(step, torch.Tensor):
         assert step.numel() == 1
         step, p_step = 1, _address(step, _I64, step.shape)

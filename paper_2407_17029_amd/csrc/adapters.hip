@@ -775,17 +775,17 @@ __global__ __launch_bounds__(256) void k_rank_parts(PartsDesc d) {
     }
 }
 
-// Every CU's whole LDS may be asked for
+// More than 64 KB of LDS has to be asked for, up to the whole of a CU's
 template <typename K>
-int allow_lds(K kernel) {
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess
+int allow_lds(K kernel, int bytes) {
+    return bytes <= 64 * 1024 || hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess
                ? QBLORA_OK : QBLORA_ERR_LAUNCH;
 }
 
 template <int LAM, bool BACK>
 int rank_sums(const RankDesc& d, hipStream_t st) {
     const int lds = rank_lds<LAM>(d.g.R);
-    const int rc = allow_lds(k_rank_sums<LAM, BACK>);
+    const int rc = allow_lds(k_rank_sums<LAM, BACK>, lds);
     if (rc) return rc;
     k_rank_sums<LAM, BACK><<<dim3(d.g.tile_room, d.splits, (d.g.R + kRankRows - 1) / kRankRows), kRankThreads, lds, st>>>(d);
     return launch_status();
@@ -799,12 +799,12 @@ int ring_stages(int stage, int more) {
 
 template <int LAM, bool BACK, int KS>
 int spread(const SpreadDesc& d, hipStream_t st) {
-    const int rc = allow_lds(k_spread<LAM, BACK, KS>);
-    if (rc) return rc;
     constexpr int kRows = spread_rows<LAM, KS, kTileTokens>();
     const int J = d.width / LAM, steps = (J + kRows - 1) / kRows;
     const int more = d.u ? 0 : spread_u_bytes(std::min(d.g.T, kTileTokens), d.g.R), stage = spread_stage_bytes<LAM, KS, kTileTokens>(d.g.R);
     const int stages = ring_stages(stage, more);
+    const int rc = allow_lds(k_spread<LAM, BACK, KS>, stages * stage + more);
+    if (rc) return rc;
     // one round of workgroups where that fills nine tenths of the chip with eight steps each at least, else smaller ones in about
     // 1024: 125 tiles of 2048 rows 39 us with 500 workgroups, 42 with 1000 (4096 rows, R = 256: 94 with 250, 106 with 1000);
     // 88 of 2560 rows 25.4 with 440, 22.4 with 970
@@ -819,8 +819,6 @@ int spread(const SpreadDesc& d, hipStream_t st) {
 
 template <int LAM, int KS>
 int spread_few_tokens(const SpreadDesc& d, hipStream_t st) {
-    const int rc = allow_lds(k_spread_few<LAM, KS>);
-    if (rc) return rc;
     // Pieces of 256 rows of outputs, or of 64 where those would leave most CUs idle.  One round of workgroups, two a CU, while that gives
     // each few pieces (40 adapters, 860 pieces: 512 workgroups 12.6 us, 2048 16.2); else more and smaller ones, which even out at
     // the end (100 adapters, 4500 pieces: 1024 125 us, 2048 119).
@@ -830,6 +828,8 @@ int spread_few_tokens(const SpreadDesc& d, hipStream_t st) {
     const int rows = (pieces + parts - 1) / parts * piece;
     const int more = spread_u_bytes(16, d.g.R), stage = spread_stage_bytes<LAM, KS, 16>(d.g.R), stages = ring_stages(stage, more);
     const int lds = std::max(d.g.T > kFewTile ? stages * stage + more : 0, few_bytes(KS, d.g.T >= 3 ? 4 : d.g.T));
+    const int rc = allow_lds(k_spread_few<LAM, KS>, lds);
+    if (rc) return rc;
     k_spread_few<LAM, KS><<<dim3((J + rows - 1) / rows, d.g.tile_room), kFewThreads, lds, st>>>(d, rows, stages);
     return launch_status();
 }
@@ -854,7 +854,7 @@ int launch_adapter_table(const TableDesc& d, hipStream_t st) {
 
 int launch_adapter_groups(const GroupsDesc& d, hipStream_t st) {
     const int lds = (2 * ((d.n + 3) & ~3) + d.count + kGroupRequests) * 4;
-    const int rc = allow_lds(k_adapter_groups);
+    const int rc = allow_lds(k_adapter_groups, lds);
     if (rc) return rc;
     k_adapter_groups<<<std::max(1, (d.n + kGroupRequests - 1) / kGroupRequests), kGroupThreads, lds, st>>>(d);
     return launch_status();

@@ -153,6 +153,16 @@ def test_norm_of_many_units(qb):
     assert torch.equal(a, b) and abs(float(a[0]) - norm) <= 2.0 ** -23 * norm
 
 
+@pytest.mark.parametrize("units", [1, 3, 4, 5, 31, 32, 33])
+def test_norm_around_its_rule(qb, units):
+    """Lists of few units, which one workgroup adds up, and of more; the last unit is not a whole one."""
+    g = [torch.randn(4096 * (units - 1) + 100, device=au.DEV, generator=torch.Generator(au.DEV).manual_seed(units))]
+    zeros = [torch.zeros_like(x) for x in g]
+    got = qb.qblora_grad_norm(qb.qblora_adamw_list([None], g, zeros, zeros, master=zeros), 1.0)
+    norm = float((g[0].double() ** 2).sum()) ** 0.5
+    assert abs(float(got[0]) - norm) <= 2.0 ** -23 * norm
+
+
 def test_norm_of_large_and_small_gradients(qb):
     """Squares that pass fp32 both ways."""
     for scale in (1e30, 1e-30):

@@ -343,6 +343,21 @@ def test_refusals_of_the_binding(qb):
         qb.qblora_adapters_fwd(table, groups, X, Y, workspace=torch.empty(256, dtype=torch.uint8, device=au.DEV))
 
 
+def test_another_device(qb, monkeypatch):
+    """Arrays of a device that is not the current one are refused (here the current one is said to be another)."""
+    b = au.Batch(*LAYERS[1])
+    table, groups = b.table(qb), b.groups(qb)
+    X, Y = au.dev_bf16(b.X), au.dev_bf16(b.Y)
+    w = [torch.zeros(5, device=au.DEV)]
+    lst = qb.qblora_adamw_list([None], w, w, w, master=w)
+    monkeypatch.setattr(qb, "_current_device", lambda: 1)
+    for call in (lambda: qb.qblora_adapters_fwd(table, groups, X, Y), lambda: qb.qblora_adapters_bwd(table, groups, X, Y),
+                 lambda: b.groups(qb), lambda: b.table(qb), lambda: qb.qblora_adamw_list([None], w, w, w, master=w),
+                 lambda: qb.qblora_grad_norm(lst, 1.0), lambda: qb.qblora_adamw_step(lst, 1, 1e-3)):
+        with pytest.raises(AssertionError):
+            call()
+
+
 # ---- streams and graphs --------------------------------------------------------------------------------------
 
 def test_captured_steps(qb):
