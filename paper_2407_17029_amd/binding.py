@@ -886,10 +886,10 @@ def _current_device() -> int:
 
 
 def _here(*tensors) -> None:
-    """The calls below launch on the current device: what they are given has to lie there."""
+    """The calls below launch on the current device: what they are given (None: nothing) has to lie there."""
     device = _current_device()
     for t in tensors:
-        assert t.get_device() == device
+        assert t is None or t.get_device() == device
 
 
 class Adapters:
@@ -924,12 +924,14 @@ def qblora_adapter_table(adapters, d_in: int, d_out: int, lambda1: int = None, l
     empty = Adapter(None, None, into.lambda1, into.lambda2, 0.0)
     for a in adapters:
         if a is not None and a.A is not None and a.B is not None:
+            _here(a.A, a.B)
             _address(a.A, _BF16, (d_in // into.lambda1, a.R))
             _address(a.B, _BF16, (a.R, d_out // into.lambda2))
     pairs = [None] * n if grads is None else list(grads)
     assert len(pairs) == n
     for a, g in zip(adapters, pairs):
         if g is not None:
+            _here(*g)
             _address(g[0], _F32, tuple(a.A.shape))
             _address(g[1], _F32, tuple(a.B.shape))
     raw = b"".join((empty if a is None else a).c_bytes() for a in adapters)
@@ -943,7 +945,7 @@ def qblora_adapter_groups(starts: torch.Tensor, which: torch.Tensor, count: int,
                           order: torch.Tensor = None, tiles: torch.Tensor = None):
     """(first, order, tiles): the T tokens of a batch by adapter, which all projections share.  starts [n + 1], which [n]."""
     n, = which.shape
-    _here(starts, which)
+    _here(starts, which, first, order, tiles)
     L = lib()
     room = _tile_room(count, T)
     if first is None and order is None and tiles is None:                # one allocation; the tiles, which are 16 bytes each, lead it
@@ -1004,6 +1006,7 @@ def _adapters_workspace(workspace, L, a, T, device):
     if workspace is None:
         nbytes = L.qblora_adapters_workspace_bytes(a, T)
         return torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes
+    assert workspace.is_contiguous()
     return workspace, workspace.numel() * workspace.element_size()
 
 
@@ -1011,7 +1014,7 @@ def qblora_adapters_fwd(ads: Adapters, groups, X: torch.Tensor, Y: torch.Tensor,
                         workspace: torch.Tensor = None):
     """Adds every token's adapter term to Y [T, d_out], in place.  groups: what qblora_adapter_groups returned."""
     T = X.shape[0]
-    _here(X, Y, ads.table)
+    _here(X, Y, ads.table, *groups, saved, workspace)
     L, a = lib(), ads.c_bytes()
     ldx, ldy = _rows(X, T, ads.d_in), _rows(Y, T, ads.d_out)
     first, order, tiles = _groups(ads, groups, T)
@@ -1028,7 +1031,7 @@ def qblora_adapters_bwd(ads: Adapters, groups, X, dY: torch.Tensor, dX: torch.Te
     """Adds the adapters' part to dX [T, d_in] (if given), in place, and writes the gradients of the table's adapters.  X may be
     None without gradients; saved: what the forward call filled."""
     T = dY.shape[0]
-    _here(dY, ads.table)
+    _here(X, dY, dX, ads.table, *groups, saved, workspace)
     L, a = lib(), ads.c_bytes()
     ldx = 0 if X is None else _rows(X, T, ads.d_in)
     lddx = 0 if dX is None else _rows(dX, T, ads.d_in)
@@ -1063,7 +1066,7 @@ def qblora_adamw_list(params, grads, m, v, master=None, m_scale=None, v_scale=No
     bits = 8 if n and m[0].dtype is torch.float8_e4m3fn else 32
     types = (torch.float8_e4m3fn, torch.float8_e5m2) if bits == 8 else (_F32, _F32)
     assert all(len(x) == n for x in (params, m, v, master, m_scale, v_scale, rate, decay))
-    _here(*grads)
+    _here(*params, *grads, *m, *v, *master, *m_scale, *v_scale)
     c = (CAdamWTensor * max(n, 1))()
     for i in range(n):
         shape = grads[i].shape
@@ -1085,11 +1088,12 @@ def qblora_adamw_list(params, grads, m, v, master=None, m_scale=None, v_scale=No
 def qblora_grad_norm(tensors: AdamWList, max_norm: float, out: torch.Tensor = None, workspace: torch.Tensor = None):
     """fp32 [2] on the device: the norm of all gradients, and the factor that clips it to max_norm."""
     dev = tensors.plan.device
-    _here(tensors.plan)
+    _here(tensors.plan, out, workspace)
     if out is None:
         out = torch.empty(2, dtype=_F32, device=dev)
     if workspace is None:
         workspace = torch.empty(tensors.norm_bytes, dtype=torch.uint8, device=dev)
+    assert workspace.is_contiguous()
     rc = lib().qblora_grad_norm(tensors.raw, max_norm, _address(out, _F32, (2,)), workspace.data_ptr(),
                                 workspace.numel() * workspace.element_size(), _current_stream())
     if rc:
@@ -1102,11 +1106,13 @@ def qblora_adamw_step(tensors: AdamWList, step, lr, beta1: float = 0.9, beta2: f
     """One AdamW step on every tensor of the list, in place.  step, lr: numbers, or one-element tensors on the device (int64 and
     fp32) that the call reads when it runs, as a captured graph needs; clip: what qblora_grad_norm returned."""
     p_step = p_lr = 0
-    _here(tensors.plan)
+    _here(tensors.plan, clip)
     if isinstance(step, torch.Tensor):
+        _here(step)
         assert step.numel() == 1
         step, p_step = 1, _address(step, _I64, step.shape)
     if isinstance(lr, torch.Tensor):
+        _here(lr)
         assert lr.numel() == 1
         lr, p_lr = 0.0, _address(lr, _F32, lr.shape)
     how = _ADAMW.pack(lr, beta1, beta2, eps, step, p_step, p_lr, seed & 0xffffffff)

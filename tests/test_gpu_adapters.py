@@ -358,6 +358,45 @@ def test_another_device(qb, monkeypatch):
             call()
 
 
+def test_arrays_in_host_memory(qb):
+    """Each array that a call takes, in host memory instead: refused before anything is launched."""
+    b = au.Batch(*LAYERS[1])
+    grads = b.grads()
+    table, groups = b.table(qb, grads=grads), b.groups(qb)
+    X, Y = au.dev_bf16(b.X), au.dev_bf16(b.Y)
+    dY, dX = au.dev_bf16(b.dY), au.dev_bf16(b.dX)
+    saved = torch.empty(qb.qblora_adapters_saved_bytes(table, b.T), dtype=torch.uint8, device=au.DEV)
+    workspace = torch.empty(qb.qblora_adapters_workspace_bytes(table, b.T), dtype=torch.uint8, device=au.DEV)
+    first, order, tiles = groups
+    starts, which = au.dev(b.starts), au.dev(b.which)
+    calls = [(qb.qblora_adapters_fwd, dict(groups=groups, X=X, Y=Y, saved=saved, workspace=workspace)),
+             (qb.qblora_adapters_bwd, dict(groups=groups, X=X, dY=dY, dX=dX, saved=saved, workspace=workspace))]
+    for call, arrays in calls:
+        for name, value in arrays.items():
+            others = [value.cpu()] if name != "groups" else [(first.cpu(), order, tiles), (first, order.cpu(), tiles), (first, order, tiles.cpu())]
+            for other in others:
+                with pytest.raises(AssertionError):
+                    call(table, **{**arrays, name: other})
+        with pytest.raises(AssertionError):                  # every other byte of an array
+            call(table, **{**arrays, "workspace": workspace.repeat(2)[::2]})
+    for other in (dict(starts=starts.cpu()), dict(which=which.cpu()), dict(first=first.cpu()), dict(order=order.cpu()), dict(tiles=tiles.cpu())):
+        with pytest.raises(AssertionError):
+            qb.qblora_adapter_groups(**{**dict(starts=starts, which=which, count=table.count, T=b.T), **other})
+
+    w = [torch.zeros(5, device=au.DEV)]
+    lst = qb.qblora_adamw_list([None], w, w, w, master=w)
+    for at in range(4):
+        lists = [[t.cpu()] if i == at else w for i, t in enumerate(w * 4)]
+        with pytest.raises(AssertionError):
+            qb.qblora_adamw_list([None], *lists[:3], master=lists[3])
+    room = torch.empty(lst.norm_bytes, dtype=torch.uint8)
+    for call in (lambda: qb.qblora_grad_norm(lst, 1.0, workspace=room), lambda: qb.qblora_grad_norm(lst, 1.0, out=torch.empty(2)),
+                 lambda: qb.qblora_adamw_step(lst, torch.ones(1, dtype=torch.int64), 1e-3),
+                 lambda: qb.qblora_adamw_step(lst, 1, torch.ones(1)), lambda: qb.qblora_adamw_step(lst, 1, 1e-3, clip=torch.ones(2))):
+        with pytest.raises(AssertionError):
+            call()
+
+
 # ---- streams and graphs --------------------------------------------------------------------------------------
 
 def test_captured_steps(qb):
