@@ -64,6 +64,8 @@ struct PartsDesc {
     const float* part2; int splits2; qblora_bf16* out2;
 };
 int launch_rank_parts(const PartsDesc& d, hipStream_t st);
+// Whether a call makes the parts although nobody keeps them; every call with an inner rank above 256 does
+bool rank_parts_pay(int count, int64_t T, int R);
 
 // out[token][n] += factor * sum_r U[place][r] * W[r][n / lam], U the parts that launch_rank_parts made, or (u NULL) the sum of
 // `splits` slices of part; W is B, or (back) the transpose of A
@@ -75,6 +77,8 @@ struct SpreadDesc {
     float factor;
 };
 int launch_spread(const SpreadDesc& d, hipStream_t st);
+// Whether W = B without parts goes through the form for few tokens of a tile
+bool spread_few_applies(int count, int64_t T);
 
 // dA and dB of every entry that has a place for them, from X, dY and the three bf16 parts of s U and of dU
 struct AdapterGradDesc {

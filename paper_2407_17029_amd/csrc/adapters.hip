@@ -835,10 +835,8 @@ int spread_few_tokens(const SpreadDesc& d, hipStream_t st) {
 }
 template <int LAM, bool BACK>
 int spread_by_rank(const SpreadDesc& d, hipStream_t st) {
-    // the kernel for few tokens of a tile where the batch has so few for each adapter, as far as their number tells (167 tokens on two
-    // adapters: 66 us with it, 230 tokens 40)
     if constexpr (!BACK)
-        if (!d.u && d.g.T <= 8 * d.g.count) return d.g.R <= 64 ? spread_few_tokens<LAM, 2>(d, st) : d.g.R <= 128 ? spread_few_tokens<LAM, 4>(d, st) : spread_few_tokens<LAM, 8>(d, st);
+        if (!d.u && spread_few_applies(d.g.count, d.g.T)) return d.g.R <= 64 ? spread_few_tokens<LAM, 2>(d, st) : d.g.R <= 128 ? spread_few_tokens<LAM, 4>(d, st) : spread_few_tokens<LAM, 8>(d, st);
     if (d.g.R <= 64) return spread<LAM, BACK, 2>(d, st);
     if (d.g.R <= 128) return spread<LAM, BACK, 4>(d, st);
     if (d.g.R <= 256) return spread<LAM, BACK, 8>(d, st);
@@ -892,6 +890,14 @@ int launch_rank_parts(const PartsDesc& d, hipStream_t st) {
     k_rank_parts<<<dim3(d.g.tile_room, d.out2 ? 2 : 1, z), 256, 0, st>>>(d);
     return launch_status();
 }
+
+// From so many tokens on, or inner ranks whose sums do not fit LDS beside the rest, sums that are cut into slices are added up once, in
+// a launch of their own, and not by every workgroup that needs them
+bool rank_parts_pay(int count, int64_t T, int R) { return T >= 1024 || R > 256 || (T > 8 * (int64_t)count && R > 64); }
+
+// The kernel for few tokens of a tile where the batch has so few for each adapter, as far as their number tells (167 tokens on two
+// adapters: 66 us with it, 230 tokens 40)
+bool spread_few_applies(int count, int64_t T) { return T <= 8 * (int64_t)count; }
 
 int launch_spread(const SpreadDesc& d, hipStream_t st) {
     if (d.back) switch (d.lam) {

@@ -36,10 +36,6 @@ int check_rows(const void* p, int64_t ld, int width) {
     if (ld < width || ld % 8 || !aligned(p, 16)) return QBLORA_ERR_SHAPE;
     return QBLORA_OK;
 }
-// From so many tokens on, or inner ranks whose sums do not fit LDS beside the rest, sums that are cut into slices are added up once, in
-// a launch of their own, and not by every workgroup that needs them
-bool parts_pay(const qblora_adapters* a, int64_t T) { return T >= 1024 || a->R > 256 || (T > 8 * (int64_t)a->count && a->R > 64); }
-
 int tile_room(int count, int64_t T) { return (int)((T + kTileTokens - 1) / kTileTokens + std::min<int64_t>(count, T)); }
 
 Grouped grouped(const qblora_adapters* a, const int32_t* first, const int32_t* order, const int32_t* tiles, int64_t T) {
@@ -168,7 +164,7 @@ int qblora_adapters_fwd(const qblora_adapters* a, const int32_t* first, const in
     if ((rc = launch_rank_sums(u, as_stream(stream)))) return rc;
     SpreadDesc v{};
     v.g = u.g; v.part = u.part; v.splits = u.splits;
-    if (saved || parts_pay(a, T)) {
+    if (saved || rank_parts_pay(a->count, T, a->R)) {
         PartsDesc w{};
         w.g = u.g; w.part = u.part; w.splits = u.splits;
         w.out = saved ? saved : reinterpret_cast<qblora_bf16*>(reinterpret_cast<unsigned char*>(workspace) + s.part_x + s.part_y);
@@ -220,7 +216,7 @@ int qblora_adapters_bwd(const qblora_adapters* a, const int32_t* first, const in
     if ((rc = launch_rank_sums(u, st))) return rc;
     SpreadDesc v{};
     v.g = w.g; v.part = part_y; v.splits = u.splits;
-    if (gradients || parts_pay(a, T)) {
+    if (gradients || rank_parts_pay(a->count, T, a->R)) {
         p.part = part_y; p.splits = u.splits; p.out = du;
         if ((rc = launch_rank_parts(p, st))) return rc;
         v.u = du;
