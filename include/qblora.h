@@ -605,7 +605,9 @@ int qblora_adapter_groups(const int32_t* starts, const int32_t* which, int32_t n
  *   first, order, tiles   as qblora_adapter_groups wrote them for this batch and this count.  A token must not be listed twice.
  *   saved  qblora_adapters_saved_bytes(), 16-byte aligned, or NULL: s U of every listed token, which the backward pass needs
  *   workspace   at least qblora_adapters_workspace_bytes(), 256-byte aligned; the size serves both directions and every smaller T
- * T = 0 is a no-op; T <= 2^20.
+ * T = 0 is a no-op; T <= 2^20.  A repeated call repeats its bits; with another T or count, or with `saved` there or not, sums may be taken in
+ * another order and s U with more of its bits.  Launches are sized by T and count, as only the device knows who has how many
+ * tokens: a table that holds few more adapters than a batch has is faster than one of many.
  */
 size_t qblora_adapters_saved_bytes(const qblora_adapters* adapters, int64_t T);
 size_t qblora_adapters_workspace_bytes(const qblora_adapters* adapters, int64_t T);
@@ -676,7 +678,7 @@ int qblora_adamw_plan(const qblora_adamw_tensor* tensors, int32_t count, int32_t
 
 /*
  * Norm of all gradients of a list and the factor that clips it:
- *   out[0] = N = sqrt( sum g^2 ),  out[1] = min( 1, max_norm / (N + 1e-6) )   (NaN where N is not finite)
+ *   out[0] = N = sqrt( sum g^2 ),  out[1] = min( 1, max_norm / (N + 1e-6) )   (NaN where out[0], N in fp32, is not finite)
  * computed in 64 bits in a fixed order (a repeated call repeats its bits) and rounded once.  out: fp32 [2], device.  max_norm > 0.
  * workspace: at least qblora_grad_norm_workspace_bytes(), 16-byte aligned.
  */
@@ -691,7 +693,8 @@ int qblora_grad_norm(const qblora_adamw_list* list, double max_norm, float* out,
  *   rounded up stays finite)
  *   w = w * (1 - lr * rate * decay) - lr * rate / (1 - beta1^t) * m / ( sqrt(v) / sqrt(1 - beta2^t) + eps )
  * in fp32, each operation of m and v rounded by itself in the order written, factors formed in 64 bits and rounded once.  w is
- * the master copy, or param where there is none.  An element whose gradient is not finite keeps its weight and moments.
+ * the master copy, or param where there is none.  An element whose gradient is not finite keeps its weight and moments; in 8 bits
+ * its moments are written anew with their block: the same values, or where the block's scale has grown rounded by chance in that scale.
  *
  * Moments in 8 bits.  The step uses the moments before they are rounded.  A block's scale is the smallest power of two, 2^-126 at
  * least, that brings its largest value within 448 (m) or 57344 (v).  In units of it a value is rounded to one of its two neighbours

@@ -9,8 +9,9 @@
 //
 // Bound by the matrix pipe, which contracts every product three times: two parts (16 bits) left dA and dB 1.5 to 2 times as far from
 // 64 bits as fp32 products are, three (24 bits) are closer than those (4e-7
-// against 9e-7, 7810 tokens).  7842 tokens, 8192 + 22016 features, R = 256: 364 GFLOP in
-// 320 us (1130 TFLOP/s, where a large library product reaches 1210); 7810 tokens of 4096 + 4096, R = 128, four adapters: 60 us.
+// against 9e-7, 7810 tokens).  7842 tokens, 8192 + 22016 features, R = 256: 364 GFLOP in 342 us, 312 at best
+// (1060 and 1170 TFLOP/s, where a large library product reaches 1210); 7810 tokens of 4096 + 4096, R = 128, four adapters: 60 us.
+// The slices follow the adapters of the table: 8192 tokens of one adapter take 59 + 5 us in a table of one, 304 in one of 16.
 // Tiles of 128 x 128 through registers took 510 and 84, with 1.6 times the traffic into LDS and no copy under way during a product.
 #include <algorithm>
 

@@ -10,7 +10,8 @@
 // the adapters (256 tokens on 100 adapters, 8192 to 22016, R = 256: 210 MB of A in 41 us, 5.1 TB/s, 564 MB of B in 119, 4.7; eight tokens
 // on eight adapters, 4096 square, 6.3 and 7.0 us, where an empty launch takes 3.5).  Training batches are X, dY and the outputs (7810
 // tokens, 4096 square, R = 128: 64 MB in 21 us, 128 MB of outputs in and out in 38) until the products count (7842 tokens to 22016
-// features, R = 256: 88 GFLOP and 345 MB in 150 us, 88 GFLOP in two parts and 690 MB in 240).
+// features, R = 256: 88 GFLOP and 345 MB in 153 us, 88 GFLOP in two parts and 690 MB in 240).  Grids are sized by the adapters of the table:
+// 1500 tokens of one of them, 4096 square, R = 128, take 11 + 5 + 15 us in a table of one and 49 + 9 + 51 in one of 500.
 #include <algorithm>
 
 #include "adapters.h"
@@ -386,8 +387,9 @@ __global__ __launch_bounds__(kRankThreads) void k_rank_sums(RankDesc d) {
 // around are then its copies alone, whose number it knows.
 constexpr int kWideWaves = 8, kFewWaves = 4;                                  // of a workgroup, for tiles of up to 64 tokens and of up to 16
 constexpr int kFewThreads = 64 * kFewWaves;
-// Rows of W for a step of a tile of up to ROOM tokens; half as many where the inner rank is so large that the ring would leave room for
-// one workgroup a CU only
+// Rows of W for a step of a tile of up to ROOM tokens.  Half as many for inner ranks above 256, of which two whole stages would take all of a
+// CU's LDS, and with ROOM = 16 above 128, where they would leave a CU one workgroup.  Tiles of 64 tokens keep whole steps up to 256
+// although a CU then has one workgroup too (R = 256, lambda = 2: three stages of 48 KB).
 template <int LAM, int KS, int ROOM>
 __host__ __device__ constexpr int spread_rows() {
     return (ROOM == 16 ? KS < 8 : KS <= 8) ? (LAM == 1 ? 64 : 128 / LAM) : LAM == 1 ? 32 : LAM == 8 ? 16 : 64 / LAM;

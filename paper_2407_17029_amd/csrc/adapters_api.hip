@@ -36,6 +36,7 @@ int check_rows(const void* p, int64_t ld, int width) {
     if (ld < width || ld % 8 || !aligned(p, 16)) return QBLORA_ERR_SHAPE;
     return QBLORA_OK;
 }
+// Runs of at most 64 tokens that a batch may have: any of the adapters may have tokens, which of them do is known on the device only
 int tile_room(int count, int64_t T) { return (int)((T + kTileTokens - 1) / kTileTokens + std::min<int64_t>(count, T)); }
 
 Grouped grouped(const qblora_adapters* a, const int32_t* first, const int32_t* order, const int32_t* tiles, int64_t T) {
